@@ -4,12 +4,12 @@ Each case is one operator as a decode loop uses it, in a plain form of
 elementary torch operations and, where ``own`` is true, through the public
 binding ``paper_2601_09083_amd.srt``:
 
-* ``attn``    srt_tree_attn_q8: every tree node against a paged cache held in
+* ``attn``    srt_tree_attn_quant: every tree node against a paged cache held in
   8 bits (a scale for each page and KV head) and the tree's own K/V;
-* ``append``  srt_kv_append_q8: new tokens into that cache (a page is quantised
-  when it is full, the rest waits in bf16), then srt_kv_read_q8: the positions
+* ``append``  srt_kv_append: new tokens into that cache (a page is quantised
+  when it is full, the rest waits in bf16), then srt_kv_read: the positions
   just written, back as bf16;
-* ``commit``  srt_commit_q8: the accepted path into the cache, the draft inputs
+* ``commit``  srt_commit_quant: the accepted path into the cache, the draft inputs
   advanced, then the touched positions read back;
 * ``rules``   srt_accept_rules: the acceptance walk with penalties for repeated
   tokens, biases and grammar masks on the rows it visits;
@@ -518,7 +518,7 @@ def _kept(s, key, make):
 
 def _handle(s):
     from paper_2601_09083_amd import srt
-    return _kept(s, "handle", lambda: srt.KvQ8(s["k"], s["v"], s["ks"], s["vs"], s["tail"][0], s["tail"][1], s["bt"],
+    return _kept(s, "handle", lambda: srt.KvQuant(s["k"], s["v"], s["ks"], s["vs"], s["tail"][0], s["tail"][1], s["bt"],
                                                s["ctx_len"]))
 
 
@@ -527,17 +527,17 @@ def _own_run(s):
     c = s["case"]
     if c["kind"] == "attn":
         kv = _handle(s)
-        scratch = _kept(s, "scratch", lambda: torch.empty(srt.srt_tree_attn_q8_scratch_bytes(kv, c["N"], c["hq"]),
+        scratch = _kept(s, "scratch", lambda: torch.empty(srt.srt_tree_attn_quant_scratch_bytes(kv, c["N"], c["hq"]),
                                                           dtype=torch.uint8, device=DEV))
-        return srt.srt_tree_attn_q8(s["q"], kv, s["k_new"], s["v_new"], s["parent"], s["n"], s["scale"], out=s["out"],
+        return srt.srt_tree_attn_quant(s["q"], kv, s["k_new"], s["v_new"], s["parent"], s["n"], s["scale"], out=s["out"],
                                     scratch=scratch)
     if c["kind"] == "append":
-        srt.srt_kv_append_q8(_handle(s), s["k_new"], s["v_new"], s["counts"])
+        srt.srt_kv_append(_handle(s), s["k_new"], s["v_new"], s["counts"])
     if c["kind"] == "commit":
-        srt.srt_commit_q8(_handle(s), s["k_new"], s["v_new"], s["acc"], s["emitted"], s["nodes"],
+        srt.srt_commit_quant(_handle(s), s["k_new"], s["v_new"], s["acc"], s["emitted"], s["nodes"],
                           ctx_tail=s["ctx_tail"], draft_len=s["draft_len"])
     if c["kind"] in ("append", "commit"):
-        return srt.srt_kv_read_q8(_handle(s), s["start"], s["out"][0].shape[1], out=s["out"])
+        return srt.srt_kv_read(_handle(s), s["start"], s["out"][0].shape[1], out=s["out"])
     if c["kind"] == "rules":
         rules = _kept(s, "rules", lambda: srt.Rules(
             seen=s["seen"], repetition=s["repetition"], frequency=s["frequency"], presence=s["presence"],
