@@ -99,24 +99,10 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
     __syncthreads();
   }
 
-  // Draft tail: shift left by the k + 1 emitted tokens and append them.
   const int e = k + 1;
-  if (a.ctx_tail) {
-    const int64_t t = a.draft_len[b];
-    int32_t* row = a.ctx_tail + static_cast<int64_t>(b) * a.Qmax;
-    const int32_t* emitted = a.out_tokens + static_cast<int64_t>(b) * (a.Dmax + 1);
-    int32_t nv = -1;
-    const int i = tid;
-    if (i < a.Qmax) {
-      const int src = i + e;  // in the frame old tail [0, Qmax) ++ emitted [Qmax, Qmax + e)
-      const int64_t valid_from = a.Qmax - min<int64_t>(max<int64_t>(t, 0), a.Qmax);
-      if (src >= a.Qmax) nv = emitted[src - a.Qmax];
-      else if (src >= valid_from) nv = row[src];
-    }
-    __syncthreads();
-    if (i < a.Qmax) row[i] = nv;
-    if (tid == 0) a.draft_len[b] = static_cast<int32_t>(t + e);
-  }
+  if (a.ctx_tail)
+    advance_draft(a.ctx_tail + static_cast<int64_t>(b) * a.Qmax, a.Qmax, a.draft_len + b,
+                  a.out_tokens + static_cast<int64_t>(b) * (a.Dmax + 1), e);
   __syncthreads();  // every thread has read ctx_len[b]
   if (tid == 0) a.ctx_len[b] = static_cast<int32_t>(L + e);
 }
