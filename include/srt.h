@@ -352,6 +352,169 @@ int srt_commit(int32_t B, int32_t N, int32_t Hkv, int32_t d, int32_t page, int32
                const int32_t* out_nodes, int32_t max_match, int32_t* ctx_tail, int32_t* draft_len,
                void* stream);
 
+/* ------------------------------------------------------------------------
+ * KV cache held in 8 bits, with a scale for each page and KV head.
+ *
+ * Position p of sequence b with L = ctx_len[b] committed positions lies
+ *   - in a page, if its page is full (p < F = L - L % page): the code at slot
+ *     p % page of page block_table[b, p / page], whose value is code * scale
+ *     with the scale of that page, KV head and tensor;
+ *   - else in the sequence's tail, row p % page, in bf16.
+ * A page is quantised once, when it is full, from the bf16 vectors in the
+ * tail: with amp = max(max |x| over the page's page x d values of a KV head,
+ * 2^-60) and top = 448 (SRT_KV_E4M3) or 127 (SRT_KV_INT8),
+ *   scale = fl(amp / top),
+ *   code  = round to nearest even(min(max(fl(x * fl(top / amp)), -top), top)).
+ * So every value is rounded once, the cache does not depend on how its tokens
+ * arrived (a prompt at once, single tokens, accepted paths of any length), and
+ * the K/V of draft-tree nodes that are not accepted never touch it.  Vectors
+ * must be finite; those of a page that holds an infinity or a NaN read back as
+ * anything.
+ *
+ * The struct is read on the host during a call and not kept; its pointers are
+ * device pointers:
+ *   k_pages, v_pages [num_pages, Hkv, page, d] e4m3 (OCP, no infinities) or int8
+ *   k_scale, v_scale [num_pages, Hkv] fp32, positive
+ *   k_tail, v_tail [B, Hkv, page, d] bf16 bits
+ *   block_table [B, max_pages] int32 (an entry is read once its page is full)
+ *   ctx_len [B] int32
+ * Pages and tails are 16-byte aligned (else SRT_ERR_INVALID).  d is 64 or 128,
+ * page a power of two of 16 to 256 (else SRT_ERR_UNSUPPORTED).  ctx_len[b]
+ * must be in [0, (max_pages + 1) * page - 1] and is clamped to it; pages
+ * outside [0, num_pages) read as zero and are not written.  No page may belong
+ * to two sequences that are written in one call.
+ * New vectors (k_new, v_new) are bf16 rows of a token's KV heads, [B, T, Hkv, d]
+ * with `ld` elements from one token to the next (>= Hkv * d; the sequences are
+ * T * ld apart), so that a fused projection's output is read where it lies;
+ * 16-byte aligned, ld a multiple of 8 (else SRT_ERR_INVALID).
+ * ---------------------------------------------------------------------- */
+#define SRT_KV_E4M3 0
+#define SRT_KV_INT8 1
+
+typedef struct {
+  int32_t kv_type;    /* SRT_KV_E4M3 or SRT_KV_INT8 */
+  int32_t Hkv;        /* KV heads, 1..255 */
+  int32_t d;          /* head size: 64 or 128 */
+  int32_t page;       /* tokens per page */
+  int32_t max_pages;  /* columns of block_table, >= 1 */
+  int32_t reserved;   /* must be 0 */
+  int64_t num_pages;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  float* k_scale;
+  float* v_scale;
+  uint16_t* k_tail;
+  uint16_t* v_tail;
+  const int32_t* block_table;
+  int32_t* ctx_len;
+} srt_kv_quant;
+
+/* Tree-masked attention as srt_tree_attn's, over that cache: the keys and
+ * values of sequence b are its L context positions and, for tree node
+ * i < n_nodes[b], the rows j of k_new, v_new [B, N, Hkv, d] of i's
+ * ancestors-or-self (the tree's vectors stay where the projection wrote them;
+ * N = 1 is plain decoding of one token).  Codes enter the products exactly;
+ * the scales are applied to the fp32 scores and, in the exponent, to the
+ * probabilities before those are rounded to bf16 for the second product.
+ * v_scale is taken as at least 2^-70 and at most 2^100.
+ * q, out [B, N, Hq, d] bf16; tree_parent [B, N], n_nodes [B], scale, scratch,
+ * limits and errors as srt_tree_attn, with max_pages * page + page + N - 1
+ * in the place of max_pages * page. */
+size_t srt_tree_attn_quant_scratch_bytes(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq);
+
+int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq, const uint16_t* q,
+                        const uint16_t* k_new, const uint16_t* v_new, int64_t ld,
+                        const int32_t* tree_parent, const int32_t* n_nodes, float scale,
+                        uint16_t* out, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Appends min(counts[b], T) new tokens (rows 0.. of k_new, v_new [B, T, Hkv, d],
+ * their positional encoding applied) to every sequence: pages that become full
+ * are quantised, the rest goes to the tail, ctx_len[b] grows.  counts [B] int32,
+ * negative ones as 0; tokens past max_pages * page + page - 1 positions are
+ * dropped.  Rows past counts[b] are not read.  T up to 64 takes one launch. */
+int srt_kv_append(const srt_kv_quant* kv, int32_t B, int32_t T, const uint16_t* k_new,
+                  const uint16_t* v_new, int64_t ld, const int32_t* counts, void* stream);
+
+/* srt_commit for this cache: the root and the k = n_accepted[b] accepted nodes
+ * out_nodes[b, 0..k-1] of the tree whose vectors are k_new, v_new [B, N, Hkv, d]
+ * are appended as by srt_kv_append (rows 0, c_1, .., c_k; a node index outside
+ * [0, N) is clamped), so ctx_len[b] += k + 1; and, if ctx_tail is not NULL, the
+ * draft inputs advance as in srt_commit.  k is clamped to [0, min(Dmax, N - 1)].
+ * out_tokens, out_nodes [B, Dmax + 1] int32. */
+int srt_commit_quant(const srt_kv_quant* kv, int32_t B, int32_t N, const uint16_t* k_new,
+                     const uint16_t* v_new, int64_t ld, int32_t Dmax, const int32_t* n_accepted,
+                     const int32_t* out_tokens, const int32_t* out_nodes, int32_t max_match,
+                     int32_t* ctx_tail, int32_t* draft_len, void* stream);
+
+/* Positions start[b] .. start[b] + T - 1 of every sequence as bf16 rows
+ * (fl(code * scale) rounded to bf16, tail rows as they are) in k_out, v_out
+ * [B, T, Hkv, d], 16-byte aligned; rows of positions outside [0, ctx_len[b])
+ * are left as they were.  start [B] int32.  For a prompt's next chunk, a
+ * transfer to another cache, a checkpoint. */
+int srt_kv_read(const srt_kv_quant* kv, int32_t B, int32_t T, const int32_t* start, uint16_t* k_out,
+                uint16_t* v_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Acceptance walk under sampling rules: srt_accept where the policy decodes
+ * with penalties for repeated tokens, biases and a mask of allowed tokens.  A
+ * penalty depends on what the walk has emitted so far, so the rules are applied
+ * to the rows that it visits; nothing is stored.
+ *
+ * At step k on node u, for token j, every operation rounded to fp32:
+ *   word = seen[b, j]; prompt = bit 15 of it (the token is in the prompt),
+ *   count = its bits 0..14 (times in the output so far, srt_seen_add) plus the
+ *           times j is among out_tokens[b, 0..k-1];
+ *   y = logits[b, u, j]
+ *   if prompt or count > 0:  y = y > 0 ? y / repetition[b] : y * repetition[b]
+ *   y = y - frequency[b] * count;   if count > 0:  y = y - presence[b]
+ *   y = y + bias, for each entry of j in the sequence's list, in its order
+ *   x_j = y (greedy) or y * inv_temperature + gumbel[b, k, j]
+ *   and x_j takes part if bit j % 32 of mask[b, u, j / 32] is set.
+ * tok = arg-max, lowest j on ties, among the tokens that take part and are
+ * neither NaN nor -inf; the walk goes on as srt_accept's.  Where none is left
+ * the walk ends without a bonus token: out_tokens[b, k] = -1, n_accepted[b] = k
+ * and n_emitted[b] = k (the caller ends such a sequence).
+ * Any pointer of the rules may be NULL: no such rule (repetition 1, frequency
+ * and presence 0).  seen [B, V] uint16; repetition (> 0), frequency, presence
+ * [B] fp32, finite; mask [B, N, (V + 31) / 32] uint32; bias entries of sequence
+ * b: bias_offsets[b] .. bias_offsets[b + 1] - 1 of bias_tokens, bias_values
+ * [n_bias] (offsets are clamped to [0, n_bias]; entries of one token must be
+ * next to each other, as in a sorted list; tokens outside [0, V) are ignored).
+ * Masked logits may hold anything, infinities and NaN included.
+ * Other arguments, outputs, scratch and launches as srt_accept; V up to 2^21
+ * (else SRT_ERR_UNSUPPORTED).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const uint16_t* seen;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_offsets;
+  const int32_t* bias_tokens;
+  const float* bias_values;
+  const uint32_t* mask;
+  int32_t n_bias;    /* entries of bias_tokens and bias_values */
+  int32_t reserved;  /* must be 0 */
+} srt_rules;
+
+int srt_accept_rules(int32_t B, int32_t N, int32_t V, int32_t Dmax, const float* logits,
+                     const float* gumbel, float inv_temperature, const srt_rules* rules,
+                     const int32_t* tree_tokens, const int32_t* tree_parent,
+                     const int32_t* n_nodes, int32_t* n_accepted, int32_t* out_tokens,
+                     int32_t* out_nodes, int32_t* n_emitted, void* scratch, size_t scratch_bytes,
+                     void* stream);
+
+/* Enters tokens[b, 0..lengths[b]-1] of every sequence into its count row
+ * seen[b, 0..V-1]: prompt = 1 sets bit 15 of their words, prompt = 0 counts them
+ * in bits 0..14 (which stop at 32767).  reset = 1 builds the row from these tokens
+ * alone (a new sequence takes the row), reset = 0 adds to it.  tokens
+ * [B, stride] int32, tokens outside [0, V) ignored; lengths [B] int32, clamped
+ * to [0, stride]; the outputs of srt_accept* fit as they are (tokens =
+ * out_tokens, lengths = n_emitted, stride = Dmax + 1). */
+int srt_seen_add(uint16_t* seen, int32_t B, int32_t V, const int32_t* tokens,
+                 const int32_t* lengths, int32_t stride, int32_t prompt, int32_t reset,
+                 void* stream);
+
 /* Library version string (host only). */
 const char* srt_version(void);
 

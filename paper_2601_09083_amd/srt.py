@@ -27,7 +27,9 @@ _NAMES = {SRT_ERR_INVALID: "SRT_ERR_INVALID", SRT_ERR_CAPACITY: "SRT_ERR_CAPACIT
 EXPORTS = ("srt_trie_workspace_bytes", "srt_trie_init", "srt_trie_insert", "srt_trie_reset_streams",
            "srt_trie_status", "srt_trie_export", "srt_draft", "srt_tree_attn_scratch_bytes",
            "srt_tree_attn", "srt_accept_scratch_bytes", "srt_accept", "srt_accept_lmhead_scratch_bytes",
-           "srt_accept_lmhead", "srt_commit", "srt_version", "srt_accept_noalloc")
+           "srt_accept_lmhead", "srt_commit", "srt_version", "srt_accept_noalloc",
+           "srt_tree_attn_quant_scratch_bytes", "srt_tree_attn_quant", "srt_kv_append", "srt_commit_quant",
+           "srt_kv_read", "srt_accept_rules", "srt_seen_add")
 SRT_ACCEPT_NOALLOC_MAX_BATCH = 4096  # include/srt.h
 
 
@@ -47,6 +49,19 @@ class DraftParams(ctypes.Structure):
     _fields_ = [("max_match", ctypes.c_int32), ("max_nodes", ctypes.c_int32),
                 ("max_depth", ctypes.c_int32), ("chain", ctypes.c_int32),
                 ("budget_alpha", ctypes.c_double), ("min_score", ctypes.c_double)]
+
+
+class KvQuantArgs(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in ("kv_type", "Hkv", "d", "page", "max_pages", "reserved")] +
+                [("num_pages", ctypes.c_int64)] +
+                [(k, ctypes.c_void_p) for k in ("k_pages", "v_pages", "k_scale", "v_scale", "k_tail", "v_tail",
+                                                "block_table", "ctx_len")])
+
+
+class RulesArgs(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("seen", "repetition", "frequency", "presence", "bias_offsets",
+                                                "bias_tokens", "bias_values", "mask")] +
+                [("n_bias", ctypes.c_int32), ("reserved", ctypes.c_int32)])
 
 
 _lib = None
@@ -76,6 +91,16 @@ def lib() -> ctypes.CDLL:
             "srt_accept_lmhead_scratch_bytes": (_SZ, [_I32, _I32, _I32]),
             "srt_accept_lmhead": (ctypes.c_int, [_I32] * 5 + [_P, _P, _P, ctypes.c_float] + [_P] * 7 + [_P, _SZ, _P]),
             "srt_commit": (ctypes.c_int, [_I32] * 6 + [_I64] + [_P] * 4 + [_I32] + [_P] * 3 + [_I32, _P, _P, _P]),
+            "srt_tree_attn_quant_scratch_bytes": (_SZ, [ctypes.POINTER(KvQuantArgs)] + [_I32] * 3),
+            "srt_tree_attn_quant": (ctypes.c_int, [ctypes.POINTER(KvQuantArgs)] + [_I32] * 3 + [_P] * 3 + [_I64, _P, _P] +
+                                    [ctypes.c_float, _P, _P, _SZ, _P]),
+            "srt_kv_append": (ctypes.c_int, [ctypes.POINTER(KvQuantArgs), _I32, _I32, _P, _P, _I64, _P, _P]),
+            "srt_commit_quant": (ctypes.c_int, [ctypes.POINTER(KvQuantArgs), _I32, _I32, _P, _P, _I64, _I32] + [_P] * 3 +
+                                 [_I32] + [_P] * 3),
+            "srt_kv_read": (ctypes.c_int, [ctypes.POINTER(KvQuantArgs), _I32, _I32] + [_P] * 4),
+            "srt_accept_rules": (ctypes.c_int, [_I32] * 4 + [_P, _P, ctypes.c_float, ctypes.POINTER(RulesArgs)] +
+                                 [_P] * 8 + [_SZ, _P]),
+            "srt_seen_add": (ctypes.c_int, [_P, _I32, _I32, _P, _P, _I32, _I32, _I32, _P]),
             "srt_version": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -336,6 +361,239 @@ def srt_commit(k_cache, v_cache, block_table, ctx_len, n_accepted, out_tokens, o
         _ptr(n_accepted, torch.int32, "n_accepted"), _ptr(out_tokens, torch.int32, "out_tokens"),
         _ptr(out_nodes, torch.int32, "out_nodes"), qmax, _ptr(ctx_tail, torch.int32, "ctx_tail"),
         _ptr(draft_len, torch.int32, "draft_len"), _stream(stream)))
+
+
+# --------------------------------------------------------------------------- 8-bit KV cache
+
+KV_TYPES = {torch.float8_e4m3fn: 0, torch.int8: 1}  # SRT_KV_E4M3, SRT_KV_INT8
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _device(device):
+    """Context in which the library's current device is the tensors' own."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+class KvQuant:
+    """A KV cache held in 8 bits (srt_kv_quant of include/srt.h): pages
+    [P,Hkv,page,d] of torch.float8_e4m3fn or torch.int8, a scale for each page
+    and KV head [P,Hkv] fp32, the open page of every sequence [B,Hkv,page,d]
+    bf16, block_table [B,max_pages] and ctx_len [B] int32.  It keeps the tensors
+    it is made of; they are updated in place."""
+
+    def __init__(self, k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len):
+        if k_pages.dim() != 4 or k_pages.dtype not in KV_TYPES:
+            raise ValueError("k_pages must be [P, Hkv, page, d] of torch.float8_e4m3fn or torch.int8")
+        P, Hkv, page, d = k_pages.shape
+        B = int(ctx_len.numel())
+        if v_pages.shape != k_pages.shape or tuple(k_scale.shape) != (P, Hkv) or v_scale.shape != k_scale.shape:
+            raise ValueError("pages or scales: shape mismatch")
+        if tuple(k_tail.shape) != (B, Hkv, page, d) or v_tail.shape != k_tail.shape:
+            raise ValueError("tails must be [B, Hkv, page, d]")
+        if block_table.dim() != 2 or block_table.shape[0] != B or ctx_len.dim() != 1:
+            raise ValueError("block_table must be [B, max_pages], ctx_len [B]")
+        self.B, self.num_pages, self.Hkv, self.page, self.d = B, P, Hkv, page, d
+        self.max_pages, self.device = int(block_table.shape[1]), k_pages.device
+        _same_device(self.device, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale, k_tail=k_tail, v_tail=v_tail,
+                     block_table=block_table, ctx_len=ctx_len)
+        self.tensors = (k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len)
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = self.tensors[:4]
+        self.k_tail, self.v_tail, self.block_table, self.ctx_len = self.tensors[4:]
+        types = (k_pages.dtype,) * 2 + (torch.float32,) * 2 + (torch.bfloat16,) * 2 + (torch.int32,) * 2
+        names = [k for k, _ in KvQuantArgs._fields_[7:]]
+        self._args = KvQuantArgs(KV_TYPES[k_pages.dtype], Hkv, d, page, self.max_pages, 0, P,
+                                 *[_ptr(t, x, n) for t, x, n in zip(self.tensors, types, names)])
+        self._ref = ctypes.byref(self._args)
+
+
+def _new_rows(kv: KvQuant, k_new, v_new):
+    """(T, elements from one token to the next) of new vectors [B,T,Hkv,d]:
+    a token's heads side by side, sequences T tokens apart."""
+    B, T = int(k_new.shape[0]), int(k_new.shape[1]) if k_new.dim() == 4 else 0
+    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+        if tuple(t.shape) != (kv.B, T, kv.Hkv, kv.d) or T < 1:
+            raise ValueError(f"{name} must be [B, T, Hkv, d]")
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise ValueError(f"{name} must be a bfloat16 CUDA (HIP) tensor")
+        s = t.stride()
+        ld = s[1] if T > 1 else s[0] if B > 1 else kv.Hkv * kv.d
+        if s[3] != 1 or (kv.Hkv > 1 and s[2] != kv.d) or (B > 1 and s[0] != T * ld) or ld < kv.Hkv * kv.d:
+            raise ValueError(f"{name}: a token's heads must lie side by side, sequences T tokens apart")
+        if t is k_new:
+            lead = ld
+        elif ld != lead:
+            raise ValueError("k_new and v_new must have the same strides")
+    _same_device(kv.device, k_new=k_new, v_new=v_new)
+    return T, lead
+
+
+def _addr(t):
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def srt_tree_attn_quant_scratch_bytes(kv: KvQuant, N: int, Hq: int) -> int:
+    return int(lib().srt_tree_attn_quant_scratch_bytes(kv._ref, kv.B, N, Hq))
+
+
+def srt_tree_attn_quant(q, kv: KvQuant, k_new, v_new, tree_parent, n_nodes, scale: float, out=None, scratch=None,
+                        stream=None):
+    """q [B,N,Hq,d] bf16; k_new, v_new [B,N,Hkv,d] bf16: the tree's own vectors."""
+    N, ld = _new_rows(kv, k_new, v_new)
+    B, _, Hq, d = q.shape
+    if tuple(q.shape) != (kv.B, N, Hq, kv.d) or (out is not None and out.shape != q.shape):
+        raise ValueError("q and out must be [B, N, Hq, d]")
+    if tuple(tree_parent.shape) != (B, N) or n_nodes.numel() != B:
+        raise ValueError("tree_parent must be [B, N], n_nodes [B]")
+    _same_device(kv.device, q=q, out=out, tree_parent=tree_parent, n_nodes=n_nodes, scratch=scratch)
+    with _device(kv.device):
+        if out is None:
+            with _on(stream):
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        args = (kv._ref, B, N, Hq, _ptr(q, torch.bfloat16, "q"), _addr(k_new), _addr(v_new), ld,
+                _ptr(tree_parent, torch.int32, "tree_parent"), _ptr(n_nodes, torch.int32, "n_nodes"), float(scale),
+                _ptr(out, torch.bfloat16, "out"))
+        need = srt_tree_attn_quant_scratch_bytes(kv, N, Hq)
+        _scratch_call("srt_tree_attn_quant",
+                      lambda x: lib().srt_tree_attn_quant(*args, _ptr(x, name="scratch"), x.numel() * x.element_size(),
+                                                          _stream(stream)), scratch, need, kv.device, stream)
+    return out
+
+
+def srt_kv_append(kv: KvQuant, k_new, v_new, counts, stream=None):
+    """Appends the first counts[b] of the rows k_new, v_new [B,T,Hkv,d]; ctx_len grows in place."""
+    T, ld = _new_rows(kv, k_new, v_new)
+    if counts.numel() != kv.B:
+        raise ValueError("counts must be [B]")
+    _same_device(kv.device, counts=counts)
+    with _device(kv.device):
+        _check("srt_kv_append", lib().srt_kv_append(kv._ref, kv.B, T, _addr(k_new), _addr(v_new), ld,
+                                                    _ptr(counts, torch.int32, "counts"), _stream(stream)))
+
+
+def srt_commit_quant(kv: KvQuant, k_new, v_new, n_accepted, out_tokens, out_nodes, ctx_tail=None, draft_len=None,
+                     stream=None):
+    """Appends the root and the accepted nodes of the tree whose vectors are
+    k_new, v_new [B,N,Hkv,d]; advances ctx_len (and, if given, ctx_tail [B,Qmax]
+    / draft_len [B]) in place."""
+    N, ld = _new_rows(kv, k_new, v_new)
+    if out_tokens.dim() != 2 or out_tokens.shape[0] != kv.B or out_nodes.shape != out_tokens.shape:
+        raise ValueError("out_tokens and out_nodes must be [B, Dmax + 1]")
+    if n_accepted.numel() != kv.B or (draft_len is not None and draft_len.numel() != kv.B):
+        raise ValueError("n_accepted and draft_len must be [B]")
+    if ctx_tail is not None and (ctx_tail.dim() != 2 or ctx_tail.shape[0] != kv.B):
+        raise ValueError("ctx_tail must be [B, Qmax]")
+    _same_device(kv.device, n_accepted=n_accepted, out_tokens=out_tokens, out_nodes=out_nodes, ctx_tail=ctx_tail,
+                 draft_len=draft_len)
+    qmax = int(ctx_tail.shape[1]) if ctx_tail is not None else 0
+    with _device(kv.device):
+        _check("srt_commit_quant", lib().srt_commit_quant(
+            kv._ref, kv.B, N, _addr(k_new), _addr(v_new), ld, int(out_tokens.shape[1]) - 1,
+            _ptr(n_accepted, torch.int32, "n_accepted"), _ptr(out_tokens, torch.int32, "out_tokens"),
+            _ptr(out_nodes, torch.int32, "out_nodes"), qmax, _ptr(ctx_tail, torch.int32, "ctx_tail"),
+            _ptr(draft_len, torch.int32, "draft_len"), _stream(stream)))
+
+
+def srt_kv_read(kv: KvQuant, start, T: int, out=None, stream=None):
+    """Positions start[b] .. start[b] + T - 1 as bf16 (k, v) [B,T,Hkv,d]; rows
+    outside the context are left as they are (zero if ``out`` is not given)."""
+    if start.numel() != kv.B or T < 1:
+        raise ValueError("start must be [B], T >= 1")
+    shape = (kv.B, T, kv.Hkv, kv.d)
+    with _device(kv.device):
+        if out is None:
+            with _on(stream):
+                out = [torch.zeros(shape, dtype=torch.bfloat16, device=kv.device) for _ in range(2)]
+        if any(tuple(x.shape) != shape for x in out):
+            raise ValueError("out must be two tensors [B, T, Hkv, d]")
+        _same_device(kv.device, start=start, k_out=out[0], v_out=out[1])
+        _check("srt_kv_read", lib().srt_kv_read(kv._ref, kv.B, T, _ptr(start, torch.int32, "start"),
+                                                _ptr(out[0], torch.bfloat16, "k_out"),
+                                                _ptr(out[1], torch.bfloat16, "v_out"), _stream(stream)))
+    return out
+
+
+# --------------------------------------------------------------------------- sampling rules
+
+class Rules:
+    """Sampling rules of a batch (srt_rules of include/srt.h), each optional:
+    seen [B,V] int16 (the bits of the count words), repetition, frequency,
+    presence [B] fp32, bias lists (bias_offsets [B+1] int32, bias_tokens int32,
+    bias_values fp32), mask [B,N,ceil(V/32)] int32 (bits of allowed tokens)."""
+
+    _TYPES = {"seen": torch.int16, "repetition": torch.float32, "frequency": torch.float32, "presence": torch.float32,
+              "bias_offsets": torch.int32, "bias_tokens": torch.int32, "bias_values": torch.float32,
+              "mask": torch.int32}
+
+    def __init__(self, **tensors):
+        for name in tensors:
+            if name not in self._TYPES:
+                raise ValueError(f"no such rule: {name}")
+        self.tensors = {k: tensors.get(k) for k in self._TYPES}
+        t = self.tensors
+        has = [t[k] is not None for k in ("bias_offsets", "bias_tokens", "bias_values")]
+        if any(has) != all(has):
+            raise ValueError("bias lists need bias_offsets, bias_tokens and bias_values")
+        if all(has) and t["bias_tokens"].numel() != t["bias_values"].numel():
+            raise ValueError("bias_tokens and bias_values differ in length")
+        n_bias = int(t["bias_tokens"].numel()) if all(has) else 0
+        self._args = RulesArgs(*[_ptr(t[k], x, k) for k, x in self._TYPES.items()], n_bias, 0)
+        self._ref = ctypes.byref(self._args)
+
+    def check(self, B: int, N: int, V: int, device):
+        want = {"seen": (B, V), "repetition": (B,), "frequency": (B,), "presence": (B,), "bias_offsets": (B + 1,),
+                "mask": (B, N, (V + 31) // 32)}
+        for name, shape in want.items():
+            if self.tensors[name] is not None and tuple(self.tensors[name].shape) != shape:
+                raise ValueError(f"{name} must be {list(shape)}")
+        _same_device(device, **self.tensors)
+
+
+def srt_accept_rules(logits, gumbel, inv_temperature: float, rules: Rules, tree_tokens, tree_parent, n_nodes,
+                     max_depth: int, out=None, scratch=None, stream=None) -> dict:
+    """srt_accept under sampling rules; a walk that finds every token forbidden
+    ends with -1 and n_emitted = n_accepted."""
+    B, N, V = logits.shape
+    if gumbel is not None and tuple(gumbel.shape) != (B, max_depth + 1, V):
+        raise ValueError("gumbel must be [B, max_depth+1, V]")
+    if tuple(tree_tokens.shape) != (B, N) or tuple(tree_parent.shape) != (B, N) or n_nodes.numel() != B:
+        raise ValueError("tree arrays must be [B, N], n_nodes [B]")
+    dev = logits.device
+    rules.check(B, N, V, dev)
+    _same_device(dev, gumbel=gumbel, tree_tokens=tree_tokens, tree_parent=tree_parent, n_nodes=n_nodes)
+    need = srt_accept_scratch_bytes(B)
+    with _device(dev):
+        with _on(stream):
+            if out is None:
+                out = _walk_outputs(B, max_depth, dev)
+            if scratch is None or scratch.numel() < need:
+                scratch = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        _check("srt_accept_rules", lib().srt_accept_rules(
+            B, N, V, max_depth, _ptr(logits, torch.float32, "logits"), _ptr(gumbel, torch.float32, "gumbel"),
+            float(inv_temperature), rules._ref, _ptr(tree_tokens, torch.int32, "tree_tokens"),
+            _ptr(tree_parent, torch.int32, "tree_parent"), _ptr(n_nodes, torch.int32, "n_nodes"),
+            _ptr(out["n_accepted"], torch.int32), _ptr(out["out_tokens"], torch.int32),
+            _ptr(out["out_nodes"], torch.int32), _ptr(out.get("n_emitted"), torch.int32), _ptr(scratch, name="scratch"),
+            scratch.numel() * scratch.element_size(), _stream(stream)))
+    return out
+
+
+def srt_seen_add(seen, tokens, lengths, prompt: bool = False, reset: bool = False, stream=None):
+    """Enters tokens [B,T] (the first lengths[b] of a row) into the count rows
+    seen [B,V] int16, in place."""
+    if seen.dim() != 2 or tokens.dim() != 2 or tokens.shape[0] != seen.shape[0] or lengths.numel() != seen.shape[0]:
+        raise ValueError("seen must be [B, V], tokens [B, T], lengths [B]")
+    B, V = seen.shape
+    _same_device(seen.device, tokens=tokens, lengths=lengths)
+    with _device(seen.device):
+        _check("srt_seen_add", lib().srt_seen_add(
+            _ptr(seen, torch.int16, "seen"), B, V, _ptr(tokens, torch.int32, "tokens"),
+            _ptr(lengths, torch.int32, "lengths"), int(tokens.shape[1]), int(bool(prompt)), int(bool(reset)),
+            _stream(stream)))
 
 
 def srt_version() -> str:
