@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   }
 
   const int e = k + 1;
-  if (a.ctx_tail)
+  if (a.ctx_tail && tid < SRT_WAVE)
     advance_draft(a.ctx_tail + static_cast<int64_t>(b) * a.Qmax, a.Qmax, a.draft_len + b,
                   a.out_tokens + static_cast<int64_t>(b) * (a.Dmax + 1), e);
   __syncthreads();  // every thread has read ctx_len[b]

@@ -184,19 +184,19 @@ __device__ inline uint32_t trie_find_or_create(const TrieView& t, uint64_t key, 
 // ---------------------------------------------------------------------------
 // Draft inputs
 // ---------------------------------------------------------------------------
-// Draft tail of one sequence: shift left by the e emitted tokens and append
-// them (all threads of a workgroup of at least Qmax; synchronises).
+// Draft tail of one sequence, at most 64 tokens: shift left by the e emitted
+// tokens and append them.  One wave, whose lanes all read before any writes.
 __device__ inline void advance_draft(int32_t* row, int Qmax, int32_t* draft_len, const int32_t* emitted, int e) {
   const int64_t t = *draft_len;
   int32_t nv = -1;
-  const int i = threadIdx.x;
+  const int i = threadIdx.x % SRT_WAVE;
   if (i < Qmax) {
     const int src = i + e;  // in the frame old tail [0, Qmax) ++ emitted [Qmax, Qmax + e)
     const int64_t valid_from = Qmax - min<int64_t>(max<int64_t>(t, 0), Qmax);
     if (src >= Qmax) nv = emitted[src - Qmax];
     else if (src >= valid_from) nv = row[src];
   }
-  __syncthreads();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (i < Qmax) row[i] = nv;
   if (i == 0) *draft_len = static_cast<int32_t>(t + e);
 }

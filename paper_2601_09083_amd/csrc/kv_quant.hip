@@ -82,11 +82,15 @@ __device__ inline uint2 codes8(const uint4& w, float inv, float top, bool e4m3) 
   return make_uint2(c0 | (c1 << 16), c2 | (c3 << 16));
 }
 
-__device__ inline float amp8(const uint4& w, float m) {
-  m = fmaxf(m, fmaxf(fabsf(bf16_lo(w.x)), fabsf(bf16_hi(w.x))));
-  m = fmaxf(m, fmaxf(fabsf(bf16_lo(w.y)), fabsf(bf16_hi(w.y))));
-  m = fmaxf(m, fmaxf(fabsf(bf16_lo(w.z)), fabsf(bf16_hi(w.z))));
-  return fmaxf(m, fmaxf(fabsf(bf16_lo(w.w)), fabsf(bf16_hi(w.w))));
+// Largest magnitude of 8 values so far, as bf16 bits in both halves of m (the
+// bits of magnitudes are ordered as the values are).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline u16x2 amp8(const uint4& w, u16x2 m) {
+  const uint32_t mag = 0x7fff7fffu;
+  m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w.x & mag));
+  m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w.y & mag));
+  m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w.z & mag));
+  return __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w.w & mag));
 }
 
 // One sequence, KV head and tensor, seen by one wave.
@@ -111,11 +115,12 @@ struct Head {
     return *reinterpret_cast<const uint4*>(p < s.L ? tail_row(p & (a.page - 1)) : new_row(p));
   }
 
-  // Quantises the full page that starts at position p0, 16 rows a time in
-  // registers; pages of up to kKeep * 16 rows are read once.
+  // Quantises the full page that starts at position p0.  Pages of 16, 32 and 64
+  // tokens (kKeep = 1, 2, 4 times 16 rows) are read once and held in registers,
+  // larger ones are read again for their codes.
+  template <int kKeep>
   __device__ void page(int p0) const {
     constexpr int kPer = 16 / kRows;  // loads per 16 rows
-    constexpr int kKeep = 4;
     const int pg = a.bt[static_cast<int64_t>(b) * a.max_pages + (p0 >> a.page_shift)];
     if (pg < 0 || pg >= a.num_pages) return;
     const float top = a.e4m3 ? 448.f : 127.f;
@@ -125,22 +130,21 @@ struct Head {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) y[i] = row(p0 + r0 + i * kRows + lr);
     };
-    float m = 0.f;
+    u16x2 m2 = {0, 0};
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k) load(k * 16, x[k]);
 #pragma unroll
     for (int k = 0; k < kKeep; ++k)
-      if (k * 16 < a.page) load(k * 16, x[k]);
 #pragma unroll
-    for (int k = 0; k < kKeep; ++k)
-      if (k * 16 < a.page) {
+      for (int i = 0; i < kPer; ++i) m2 = amp8(x[k][i], m2);
+    if constexpr (kKeep == 4)
+      for (int r0 = kKeep * 16; r0 < a.page; r0 += 16) {
+        uint4 y[kPer];
+        load(r0, y);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) m = amp8(x[k][i], m);
+        for (int i = 0; i < kPer; ++i) m2 = amp8(y[i], m2);
       }
-    for (int r0 = kKeep * 16; r0 < a.page; r0 += 16) {
-      uint4 y[kPer];
-      load(r0, y);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) m = amp8(y[i], m);
-    }
+    float m = __uint_as_float(static_cast<uint32_t>(max(m2[0], m2[1])) << 16);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, SRT_WAVE));
     m = fmaxf(m, kLeastAmp);
@@ -154,13 +158,13 @@ struct Head {
         *reinterpret_cast<uint2*>(out + static_cast<int64_t>(r0 + i * kRows + lr) * D) = codes8(y[i], inv, top, a.e4m3);
     };
 #pragma unroll
-    for (int k = 0; k < kKeep; ++k)
-      if (k * 16 < a.page) store(k * 16, x[k]);
-    for (int r0 = kKeep * 16; r0 < a.page; r0 += 16) {
-      uint4 y[kPer];
-      load(r0, y);
-      store(r0, y);
-    }
+    for (int k = 0; k < kKeep; ++k) store(k * 16, x[k]);
+    if constexpr (kKeep == 4)
+      for (int r0 = kKeep * 16; r0 < a.page; r0 += 16) {
+        uint4 y[kPer];
+        load(r0, y);
+        store(r0, y);
+      }
   }
 
   // The new rows of the page that stays open go to the tail.
@@ -175,18 +179,20 @@ struct Head {
   }
 };
 
-// Few new tokens: a workgroup per sequence.
-template <int D>
-__global__ __launch_bounds__(kThreads) void write_short_kernel(WriteArgs a) {
+// Few new tokens: a workgroup per sequence, and for a commit one wave more for
+// the draft inputs.
+template <int D, int kKeep>
+__global__ __launch_bounds__(kThreads + SRT_WAVE) void write_short_kernel(WriteArgs a) {
   const int b = blockIdx.x, wave = threadIdx.x / SRT_WAVE;
   const Span s = span_of(a, b);
   const int first = s.L & ~(a.page - 1), end = s.L + s.m;
-  for (int i = wave; i < 2 * a.Hkv; i += kWaves) {
-    const Head<D> head = {a, b, i >> 1, i & 1, static_cast<int>(threadIdx.x) % SRT_WAVE, s};
-    for (int p = first; p + a.page <= end; p += a.page) head.page(p);
-    head.rest();
-  }
-  if (a.nodes && a.ctx_tail) {
+  if (wave < kWaves) {
+    for (int i = wave; i < 2 * a.Hkv; i += kWaves) {
+      const Head<D> head = {a, b, i >> 1, i & 1, static_cast<int>(threadIdx.x) % SRT_WAVE, s};
+      for (int p = first; p + a.page <= end; p += a.page) head.template page<kKeep>(p);
+      head.rest();
+    }
+  } else {
     const int e = min(max(a.counts[b], 0), min(a.Dmax, a.T - 1)) + 1;
     advance_draft(a.ctx_tail + static_cast<int64_t>(b) * a.Qmax, a.Qmax, a.draft_len + b,
                   a.emitted + static_cast<int64_t>(b) * (a.Dmax + 1), e);
@@ -197,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void write_short_kernel(WriteArgs a) {
 
 // Many new tokens: a wave per page, KV head and tensor.  The wave of a
 // sequence's first page writes the tail too.
-template <int D>
+template <int D, int kKeep>
 __global__ __launch_bounds__(kThreads) void write_pages_kernel(WriteArgs a, int pages, int heads_at_once) {
   const int x = blockIdx.x / heads_at_once, y = blockIdx.x - x * heads_at_once;
   const int b = x / pages, i = x - b * pages;
@@ -206,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void write_pages_kernel(WriteArgs a, int 
   const Span s = span_of(a, b);
   const Head<D> head = {a, b, head_no >> 1, head_no & 1, static_cast<int>(threadIdx.x) % SRT_WAVE, s};
   const int p = (s.L & ~(a.page - 1)) + i * a.page;
-  if (p + a.page <= s.L + s.m) head.page(p);
+  if (p + a.page <= s.L + s.m) head.template page<kKeep>(p);
   if (i == 0) head.rest();
 }
 
@@ -294,6 +300,29 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
   }
 }
 
+template <int D, int kKeep>
+void launch_write(const WriteArgs& a, bool one_launch, int pages, int at_once, hipStream_t s) {
+  if (one_launch)
+    write_short_kernel<D, kKeep>
+        <<<static_cast<unsigned>(a.B), kThreads + (a.nodes && a.ctx_tail ? SRT_WAVE : 0), 0, s>>>(a);
+  else
+    write_pages_kernel<D, kKeep><<<static_cast<unsigned>(static_cast<int64_t>(pages) * at_once * a.B), kThreads, 0, s>>>(
+        a, pages, at_once);
+}
+
+int launch_write(const WriteArgs& a, int d, bool one_launch, int pages, int at_once, hipStream_t s) {
+  if (d == 128) {
+    if (a.page == 16) launch_write<128, 1>(a, one_launch, pages, at_once, s);
+    else if (a.page == 32) launch_write<128, 2>(a, one_launch, pages, at_once, s);
+    else launch_write<128, 4>(a, one_launch, pages, at_once, s);
+  } else {
+    if (a.page == 16) launch_write<64, 1>(a, one_launch, pages, at_once, s);
+    else if (a.page == 32) launch_write<64, 2>(a, one_launch, pages, at_once, s);
+    else launch_write<64, 4>(a, one_launch, pages, at_once, s);
+  }
+  return launch_status();
+}
+
 void fill(WriteArgs& a, const srt_kv_quant& kv, int32_t B, int32_t T, const uint16_t* k_new, const uint16_t* v_new,
           int64_t ld) {
   a.pages[0] = kv.k_pages;
@@ -340,18 +369,8 @@ extern "C" int srt_kv_append(const srt_kv_quant* kv, int32_t B, int32_t T, const
   fill(a, *kv, B, T, k_new, v_new, ld);
   a.counts = counts;
   hipStream_t s = as_stream(stream);
-  if (T <= kShort) {
-    if (kv->d == 128) write_short_kernel<128><<<static_cast<unsigned>(B), kThreads, 0, s>>>(a);
-    else write_short_kernel<64><<<static_cast<unsigned>(B), kThreads, 0, s>>>(a);
-    return launch_status();
-  }
-  const unsigned grid = static_cast<unsigned>(pages * at_once * B);
-  if (kv->d == 128)
-    write_pages_kernel<128><<<grid, kThreads, 0, s>>>(a, static_cast<int>(pages), static_cast<int>(at_once));
-  else
-    write_pages_kernel<64><<<grid, kThreads, 0, s>>>(a, static_cast<int>(pages), static_cast<int>(at_once));
-  st = launch_status();
-  if (st != SRT_OK) return st;
+  st = launch_write(a, kv->d, T <= kShort, static_cast<int>(pages), static_cast<int>(at_once), s);
+  if (st != SRT_OK || T <= kShort) return st;
   advance_kernel<<<static_cast<unsigned>((B + 255) / 256), 256, 0, s>>>(a);
   return launch_status();
 }
@@ -379,10 +398,7 @@ extern "C" int srt_commit_quant(const srt_kv_quant* kv, int32_t B, int32_t N, co
   a.draft_len = draft_len;
   a.Dmax = Dmax;
   a.Qmax = ctx_tail ? max_match : 0;
-  hipStream_t s = as_stream(stream);
-  if (kv->d == 128) write_short_kernel<128><<<static_cast<unsigned>(B), kThreads, 0, s>>>(a);
-  else write_short_kernel<64><<<static_cast<unsigned>(B), kThreads, 0, s>>>(a);
-  return launch_status();
+  return launch_write(a, kv->d, true, 0, 0, as_stream(stream));
 }
 
 extern "C" int srt_kv_read(const srt_kv_quant* kv, int32_t B, int32_t T, const int32_t* start, uint16_t* k_out,

@@ -94,47 +94,58 @@ struct Top {
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
 
+// Tokens emitted on this walk, and whether the bias list has an entry of them.
+struct Path {
+  int32_t tok[kMaxLevels];
+  int32_t biased[kMaxLevels];
+};
+
 // Marks of the chunk [lo, hi) (lo a multiple of 32) in `skip`: masked entries,
-// tokens of the path and tokens with a bias.  All threads; synchronises.
-__device__ inline void mark(const RulesArgs& a, const Row& w, const int32_t* path, int n_path, int lo, int hi,
-                            uint32_t* skip, int threads) {
+// tokens of the path (n of them) and tokens with a bias.  All threads; synchronises.
+__device__ inline void mark(const RulesArgs& a, const Row& w, Path& path, int n, int lo, int hi, uint32_t* skip,
+                            int threads) {
   const int words = (hi - lo + 31) / 32;
+  const int at = w.bias0 + static_cast<int>(threadIdx.x);
+  const int bias = at < w.bias1 ? a.bias_tokens[at] : -1;  // (under way together with the mask)
   for (int i = threadIdx.x; i < words; i += threads) skip[i] = w.mask ? ~w.mask[lo / 32 + i] : 0u;
+  if (static_cast<int>(threadIdx.x) < n) path.biased[threadIdx.x] = 0;
   __syncthreads();
-  auto set = [&](int t) {
-    if (t >= lo && t < hi) atomicOr(&skip[(t - lo) >> 5], 1u << ((t - lo) & 31));
+  auto set = [&](int t) { atomicOr(&skip[(t - lo) >> 5], 1u << ((t - lo) & 31)); };
+  auto set_bias = [&](int t) {
+    if (t < lo || t >= hi) return;
+    set(t);
+    for (int i = 0; i < n; ++i)
+      if (path.tok[i] == t) path.biased[i] = 1;
   };
-  for (int i = threadIdx.x; i < n_path; i += threads) set(path[i]);
-  for (int i = w.bias0 + threadIdx.x; i < w.bias1; i += threads) set(a.bias_tokens[i]);
+  if (static_cast<int>(threadIdx.x) < n) {  // n < 64 <= threads
+    const int t = path.tok[threadIdx.x];
+    if (t >= lo && t < hi) set(t);
+  }
+  set_bias(bias);
+  for (int i = at + threads; i < w.bias1; i += threads) set_bias(a.bias_tokens[i]);
   __syncthreads();
 }
 
-// Score of one marked token that is allowed (its path count and its biases, in
-// the order of the list: `from` is its first entry there, or -1 to look for it).
+// Score of one marked token that is allowed, with its path count and, where
+// `from` >= 0, the run of its biases that starts at that entry of the list.
 template <bool kNoise>
-__device__ inline void special(const RulesArgs& a, const Row& w, const int32_t* path, int n_path, int t, int from,
+__device__ inline void special(const RulesArgs& a, const Row& w, const Path& path, int n, int t, int from,
                                unsigned long long& key) {
-  if (w.mask && !((w.mask[t >> 5] >> (t & 31)) & 1u)) return;
+  const uint32_t allowed = w.mask ? w.mask[t >> 5] >> (t & 31) : 1u;
   const int word = w.seen ? w.seen[t] : 0;
+  const float l = w.logits[t], g = kNoise ? w.noise[t] : 0.f;
   int count = word & kCount;
-  for (int i = 0; i < n_path; ++i) count += path[i] == t;
-  float y = penalised(w, w.logits[t], word & kPrompt, count);
-  if (from >= 0) {
+  for (int i = 0; i < n; ++i) count += path.tok[i] == t;
+  float y = penalised(w, l, word & kPrompt, count);
+  if (from >= 0)
     for (int i = from; i < w.bias1 && a.bias_tokens[i] == t; ++i) y = __fadd_rn(y, a.bias_values[i]);
-  } else {
-    for (int i = w.bias0; i < w.bias1; ++i)
-      if (a.bias_tokens[i] == t) y = __fadd_rn(y, a.bias_values[i]);
-  }
-  const float x = noisy<kNoise>(w, y, kNoise ? w.noise[t] : 0.f);
-  if (x > -INFINITY) {
-    const unsigned long long k = pack_key(x, t);
-    key = k > key ? k : key;
-  }
+  const float x = noisy<kNoise>(w, y, g);
+  if ((allowed & 1u) && x > -INFINITY) key = max(key, pack_key(x, t));
 }
 
 // This thread's best entry of [lo, hi) of one row, packed (0: none).
 template <bool kNoise>
-__device__ inline unsigned long long part_best(const RulesArgs& a, const Row& w, const int32_t* path, int n_path,
+__device__ inline unsigned long long part_best(const RulesArgs& a, const Row& w, const Path& path, int n,
                                                const uint32_t* skip, int lo, int hi, int threads) {
   constexpr int kUnroll = 4;
   const int tid = threadIdx.x;
@@ -187,11 +198,13 @@ __device__ inline unsigned long long part_best(const RulesArgs& a, const Row& w,
     const float x = noisy<kNoise>(w, y, kNoise ? w.noise[j] : 0.f);
     if (x > -INFINITY) key = max(key, pack_key(x, j));
   }
-  for (int k = tid; k < n_path; k += threads)
-    if (path[k] >= lo && path[k] < hi) special<kNoise>(a, w, path, n_path, path[k], -1, key);
+  if (tid < n) {  // (one that the bias list has is scored there)
+    const int t = path.tok[tid];
+    if (t >= lo && t < hi && !path.biased[tid]) special<kNoise>(a, w, path, n, t, -1, key);
+  }
   for (int k = w.bias0 + tid; k < w.bias1; k += threads) {
     const int t = a.bias_tokens[k];
-    if (t >= lo && t < hi && (k == w.bias0 || a.bias_tokens[k - 1] != t)) special<kNoise>(a, w, path, n_path, t, k, key);
+    if (t >= lo && t < hi && (k == w.bias0 || a.bias_tokens[k - 1] != t)) special<kNoise>(a, w, path, n, t, k, key);
   }
   return key;
 }
@@ -230,7 +243,7 @@ __device__ inline void record_rules(const RulesArgs& a, int b, int level, const 
 template <bool kNoise>
 __global__ __launch_bounds__(kThreads) void rules_level_kernel(RulesArgs a, int level) {
   __shared__ uint32_t skip[kMaxChunk / 32];
-  __shared__ int32_t path[kMaxLevels];
+  __shared__ Path path;
   __shared__ unsigned long long s_key[kThreads / SRT_WAVE];
   __shared__ int s_child;
   const int g = blockIdx.x, tid = threadIdx.x;
@@ -260,9 +273,9 @@ __global__ __launch_bounds__(kThreads) void rules_level_kernel(RulesArgs a, int 
       const int prev = min(max(a.cur[(lv & 1) * a.B + b], 0), a.N - 1);
       const Step st = decide_rules(a, b, prev, lv, tid);
       // the path: earlier launches have written all of it but the last token
-      if (tid < lv) path[tid] = a.out_tokens[static_cast<int64_t>(b) * (a.Dmax + 1) + tid];
+      if (tid < lv) path.tok[tid] = a.out_tokens[static_cast<int64_t>(b) * (a.Dmax + 1) + tid];
       if (tid == 0) {
-        path[lv] = st.tok;
+        path.tok[lv] = st.tok;
         if (c == 0) record_rules(a, b, lv, st);
         s_child = st.child;
       }
@@ -299,7 +312,7 @@ __global__ __launch_bounds__(kWalkWaves * SRT_WAVE) void rules_walk_kernel(Rules
 template <bool kNoise>
 __global__ __launch_bounds__(1024) void rules_short_kernel(RulesArgs a) {
   __shared__ uint32_t skip[(kShortRow + 31) / 32];
-  __shared__ int32_t path[kMaxLevels];
+  __shared__ Path path;
   __shared__ int32_t s_par[kMaxN], s_tok[kMaxN];
   __shared__ unsigned long long s_key[1024 / SRT_WAVE];
   const int b = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
@@ -330,7 +343,7 @@ __global__ __launch_bounds__(1024) void rules_short_kernel(RulesArgs a) {
     if (tid == 0) {
       a.out_tokens[orow + k] = tok;
       a.out_nodes[orow + k] = child;  // -1 at the last step
-      if (child >= 0) path[k] = tok;
+      if (child >= 0) path.tok[k] = tok;
     }
     if (child < 0) break;
     u = child;

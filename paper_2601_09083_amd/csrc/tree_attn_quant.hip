@@ -106,6 +106,11 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
   constexpr int EPL = D / 8;                  // codes per lane and load
   constexpr int NPG = kChunk / kWaves / U / SRT_WAVE;  // registers of page ids
   constexpr int kTileBytes = T * (Sh::KSTRIDE + Sh::VSTRIDE);
+  // Few rows: the pages are read once, by this workgroup alone, and need no
+  // place in the caches (256 sequences of one node, 28 heads: 260 us with
+  // ordinary loads, 225 with non-temporal ones; other row blocks read wide
+  // trees' pages again: 531 and 543).
+  constexpr int kAux = WR == 8 ? 0 : 2;
   static_assert(NB * WK * T <= 256, "tiles fit the pool");
   static_assert(NPG * SRT_WAVE * U * kWaves == kChunk && NPG >= 1, "page ids of a split");
 
@@ -205,8 +210,8 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + off), 0, nbytes, 0x00020000);
 #pragma unroll
     for (int j = 0; j < LPU; ++j) {
-      if constexpr (EPL == 16) r[j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, gl_off + j * 8 * D, 0, 0);
-      else r[j] = __builtin_amdgcn_raw_buffer_load_b64(rsrc, gl_off + j * 8 * D, 0, 0);
+      if constexpr (EPL == 16) r[j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, gl_off + j * 8 * D, 0, kAux);
+      else r[j] = __builtin_amdgcn_raw_buffer_load_b64(rsrc, gl_off + j * 8 * D, 0, kAux);
     }
   };
   auto load_pages = [&](int it) {
