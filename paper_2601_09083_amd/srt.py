@@ -368,15 +368,37 @@ def srt_commit(k_cache, v_cache, block_table, ctx_len, n_accepted, out_tokens, o
 KV_TYPES = {torch.float8_e4m3fn: 0, torch.int8: 1}  # SRT_KV_E4M3, SRT_KV_INT8
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+def _arg(t, dtype, device, name):
+    """Address of a tensor of this type on this device, packed."""
+    if t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+    return t.data_ptr()
 
 
+def _maybe(t, dtype, device, name):
+    return None if t is None else _arg(t, dtype, device, name)
+
+
+def _stream_of(device, stream):
+    """The given stream, or the current one of the tensors' device."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+
+
+@contextlib.contextmanager
 def _device(device):
-    """Context in which the library's current device is the tensors' own."""
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    """The library's current device is the tensors' own."""
+    if not device.type == "cuda":
+        raise ValueError(f"the tensors must be CUDA (HIP) tensors, not on {device}")
+    with torch.cuda.device(device) if device.index != torch.cuda.current_device() else contextlib.nullcontext():
+        yield
+
+
+def _on_device(device, call, *args):
+    """call(*args) with the library's current device the tensors' own."""
+    if device.index == torch._C._cuda_getDevice():
+        return call(*args)
+    with torch.cuda.device(device):
+        return call(*args)
 
 
 class KvQuant:
@@ -399,41 +421,36 @@ class KvQuant:
             raise ValueError("block_table must be [B, max_pages], ctx_len [B]")
         self.B, self.num_pages, self.Hkv, self.page, self.d = B, P, Hkv, page, d
         self.max_pages, self.device = int(block_table.shape[1]), k_pages.device
-        _same_device(self.device, v_pages=v_pages, k_scale=k_scale, v_scale=v_scale, k_tail=k_tail, v_tail=v_tail,
-                     block_table=block_table, ctx_len=ctx_len)
+        if self.device.type != "cuda":
+            raise ValueError("k_pages must be a CUDA (HIP) tensor")
         self.tensors = (k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len)
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = self.tensors[:4]
         self.k_tail, self.v_tail, self.block_table, self.ctx_len = self.tensors[4:]
         types = (k_pages.dtype,) * 2 + (torch.float32,) * 2 + (torch.bfloat16,) * 2 + (torch.int32,) * 2
         names = [k for k, _ in KvQuantArgs._fields_[7:]]
         self._args = KvQuantArgs(KV_TYPES[k_pages.dtype], Hkv, d, page, self.max_pages, 0, P,
-                                 *[_ptr(t, x, n) for t, x, n in zip(self.tensors, types, names)])
+                                 *[_arg(t, x, self.device, n) for t, x, n in zip(self.tensors, types, names)])
         self._ref = ctypes.byref(self._args)
 
 
 def _new_rows(kv: KvQuant, k_new, v_new):
     """(T, elements from one token to the next) of new vectors [B,T,Hkv,d]:
     a token's heads side by side, sequences T tokens apart."""
-    B, T = int(k_new.shape[0]), int(k_new.shape[1]) if k_new.dim() == 4 else 0
-    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-        if tuple(t.shape) != (kv.B, T, kv.Hkv, kv.d) or T < 1:
-            raise ValueError(f"{name} must be [B, T, Hkv, d]")
-        if not t.is_cuda or t.dtype != torch.bfloat16:
-            raise ValueError(f"{name} must be a bfloat16 CUDA (HIP) tensor")
-        s = t.stride()
-        ld = s[1] if T > 1 else s[0] if B > 1 else kv.Hkv * kv.d
-        if s[3] != 1 or (kv.Hkv > 1 and s[2] != kv.d) or (B > 1 and s[0] != T * ld) or ld < kv.Hkv * kv.d:
-            raise ValueError(f"{name}: a token's heads must lie side by side, sequences T tokens apart")
-        if t is k_new:
-            lead = ld
-        elif ld != lead:
-            raise ValueError("k_new and v_new must have the same strides")
-    _same_device(kv.device, k_new=k_new, v_new=v_new)
-    return T, lead
+    if (k_new.dim() != 4 or v_new.shape != k_new.shape or k_new.dtype is not torch.bfloat16 or
+            v_new.dtype is not torch.bfloat16 or k_new.device != kv.device or v_new.device != kv.device):
+        raise ValueError(f"k_new and v_new must be [B, T, Hkv, d] of bfloat16 on {kv.device}")
+    B, T, H, d = k_new.shape
+    if B != kv.B or H != kv.Hkv or d != kv.d or T < 1:
+        raise ValueError("k_new and v_new must be [B, T, Hkv, d] of the cache's B, Hkv and d")
+    lead = [_lead(x.stride(), B, T, H, d) for x in (k_new, v_new)]
+    if lead[0] < 0 or lead[0] != lead[1]:
+        raise ValueError("k_new and v_new must have the same strides: a token's heads side by side, sequences T tokens apart")
+    return T, lead[0]
 
 
-def _addr(t):
-    return ctypes.c_void_p(t.data_ptr())
+def _lead(s, B, T, H, d):
+    ld = s[1] if T > 1 else s[0] if B > 1 else H * d
+    return -1 if s[3] != 1 or (H > 1 and s[2] != d) or (B > 1 and s[0] != T * ld) or ld < H * d else ld
 
 
 def srt_tree_attn_quant_scratch_bytes(kv: KvQuant, N: int, Hq: int) -> int:
@@ -444,23 +461,32 @@ def srt_tree_attn_quant(q, kv: KvQuant, k_new, v_new, tree_parent, n_nodes, scal
                         stream=None):
     """q [B,N,Hq,d] bf16; k_new, v_new [B,N,Hkv,d] bf16: the tree's own vectors."""
     N, ld = _new_rows(kv, k_new, v_new)
-    B, _, Hq, d = q.shape
-    if tuple(q.shape) != (kv.B, N, Hq, kv.d) or (out is not None and out.shape != q.shape):
+    B, dev = kv.B, kv.device
+    if q.dim() != 4 or q.shape[0] != B or q.shape[1] != N or q.shape[3] != kv.d or (out is not None and
+                                                                                     out.shape != q.shape):
         raise ValueError("q and out must be [B, N, Hq, d]")
-    if tuple(tree_parent.shape) != (B, N) or n_nodes.numel() != B:
+    if tree_parent.shape != (B, N) or n_nodes.numel() != B:
         raise ValueError("tree_parent must be [B, N], n_nodes [B]")
-    _same_device(kv.device, q=q, out=out, tree_parent=tree_parent, n_nodes=n_nodes, scratch=scratch)
-    with _device(kv.device):
-        if out is None:
-            with _on(stream):
-                out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        args = (kv._ref, B, N, Hq, _ptr(q, torch.bfloat16, "q"), _addr(k_new), _addr(v_new), ld,
-                _ptr(tree_parent, torch.int32, "tree_parent"), _ptr(n_nodes, torch.int32, "n_nodes"), float(scale),
-                _ptr(out, torch.bfloat16, "out"))
-        need = srt_tree_attn_quant_scratch_bytes(kv, N, Hq)
-        _scratch_call("srt_tree_attn_quant",
-                      lambda x: lib().srt_tree_attn_quant(*args, _ptr(x, name="scratch"), x.numel() * x.element_size(),
-                                                          _stream(stream)), scratch, need, kv.device, stream)
+    Hq = q.shape[2]
+    if out is None:
+        with _device(dev), _on(stream):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if scratch is None:
+        with _device(dev), _on(stream):
+            scratch = torch.empty(srt_tree_attn_quant_scratch_bytes(kv, N, Hq), dtype=torch.uint8, device=dev)
+    elif scratch.device != dev or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous tensor on {dev}")
+    args = (kv._ref, B, N, Hq, _arg(q, torch.bfloat16, dev, "q"), k_new.data_ptr(), v_new.data_ptr(), ld,
+            _arg(tree_parent, torch.int32, dev, "tree_parent"), _arg(n_nodes, torch.int32, dev, "n_nodes"), scale,
+            _arg(out, torch.bfloat16, dev, "out"))
+    call = lambda x: _on_device(dev, lib().srt_tree_attn_quant, *args, x.data_ptr(), x.numel() * x.element_size(),
+                                _stream_of(dev, stream))
+    st = call(scratch)
+    need = srt_tree_attn_quant_scratch_bytes(kv, N, Hq) if st == SRT_ERR_CAPACITY else 0
+    if need > scratch.numel() * scratch.element_size():
+        with _device(dev), _on(stream):
+            st = call(torch.empty(need, dtype=torch.uint8, device=dev))
+    _check("srt_tree_attn_quant", st)
     return out
 
 
@@ -469,10 +495,9 @@ def srt_kv_append(kv: KvQuant, k_new, v_new, counts, stream=None):
     T, ld = _new_rows(kv, k_new, v_new)
     if counts.numel() != kv.B:
         raise ValueError("counts must be [B]")
-    _same_device(kv.device, counts=counts)
-    with _device(kv.device):
-        _check("srt_kv_append", lib().srt_kv_append(kv._ref, kv.B, T, _addr(k_new), _addr(v_new), ld,
-                                                    _ptr(counts, torch.int32, "counts"), _stream(stream)))
+    _check("srt_kv_append", _on_device(
+        kv.device, lib().srt_kv_append, kv._ref, kv.B, T, k_new.data_ptr(), v_new.data_ptr(), ld,
+        _arg(counts, torch.int32, kv.device, "counts"), _stream_of(kv.device, stream)))
 
 
 def srt_commit_quant(kv: KvQuant, k_new, v_new, n_accepted, out_tokens, out_nodes, ctx_tail=None, draft_len=None,
@@ -481,21 +506,18 @@ def srt_commit_quant(kv: KvQuant, k_new, v_new, n_accepted, out_tokens, out_node
     k_new, v_new [B,N,Hkv,d]; advances ctx_len (and, if given, ctx_tail [B,Qmax]
     / draft_len [B]) in place."""
     N, ld = _new_rows(kv, k_new, v_new)
-    if out_tokens.dim() != 2 or out_tokens.shape[0] != kv.B or out_nodes.shape != out_tokens.shape:
+    B, dev, i32 = kv.B, kv.device, torch.int32
+    if out_tokens.dim() != 2 or out_tokens.shape[0] != B or out_nodes.shape != out_tokens.shape:
         raise ValueError("out_tokens and out_nodes must be [B, Dmax + 1]")
-    if n_accepted.numel() != kv.B or (draft_len is not None and draft_len.numel() != kv.B):
+    if n_accepted.numel() != B or (draft_len is not None and draft_len.numel() != B):
         raise ValueError("n_accepted and draft_len must be [B]")
-    if ctx_tail is not None and (ctx_tail.dim() != 2 or ctx_tail.shape[0] != kv.B):
+    if ctx_tail is not None and (ctx_tail.dim() != 2 or ctx_tail.shape[0] != B):
         raise ValueError("ctx_tail must be [B, Qmax]")
-    _same_device(kv.device, n_accepted=n_accepted, out_tokens=out_tokens, out_nodes=out_nodes, ctx_tail=ctx_tail,
-                 draft_len=draft_len)
-    qmax = int(ctx_tail.shape[1]) if ctx_tail is not None else 0
-    with _device(kv.device):
-        _check("srt_commit_quant", lib().srt_commit_quant(
-            kv._ref, kv.B, N, _addr(k_new), _addr(v_new), ld, int(out_tokens.shape[1]) - 1,
-            _ptr(n_accepted, torch.int32, "n_accepted"), _ptr(out_tokens, torch.int32, "out_tokens"),
-            _ptr(out_nodes, torch.int32, "out_nodes"), qmax, _ptr(ctx_tail, torch.int32, "ctx_tail"),
-            _ptr(draft_len, torch.int32, "draft_len"), _stream(stream)))
+    _check("srt_commit_quant", _on_device(
+        dev, lib().srt_commit_quant, kv._ref, B, N, k_new.data_ptr(), v_new.data_ptr(), ld, out_tokens.shape[1] - 1,
+        _arg(n_accepted, i32, dev, "n_accepted"), _arg(out_tokens, i32, dev, "out_tokens"),
+        _arg(out_nodes, i32, dev, "out_nodes"), ctx_tail.shape[1] if ctx_tail is not None else 0,
+        _maybe(ctx_tail, i32, dev, "ctx_tail"), _maybe(draft_len, i32, dev, "draft_len"), _stream_of(dev, stream)))
 
 
 def srt_kv_read(kv: KvQuant, start, T: int, out=None, stream=None):
@@ -503,17 +525,15 @@ def srt_kv_read(kv: KvQuant, start, T: int, out=None, stream=None):
     outside the context are left as they are (zero if ``out`` is not given)."""
     if start.numel() != kv.B or T < 1:
         raise ValueError("start must be [B], T >= 1")
-    shape = (kv.B, T, kv.Hkv, kv.d)
-    with _device(kv.device):
-        if out is None:
-            with _on(stream):
-                out = [torch.zeros(shape, dtype=torch.bfloat16, device=kv.device) for _ in range(2)]
-        if any(tuple(x.shape) != shape for x in out):
-            raise ValueError("out must be two tensors [B, T, Hkv, d]")
-        _same_device(kv.device, start=start, k_out=out[0], v_out=out[1])
-        _check("srt_kv_read", lib().srt_kv_read(kv._ref, kv.B, T, _ptr(start, torch.int32, "start"),
-                                                _ptr(out[0], torch.bfloat16, "k_out"),
-                                                _ptr(out[1], torch.bfloat16, "v_out"), _stream(stream)))
+    shape, dev = (kv.B, T, kv.Hkv, kv.d), kv.device
+    if out is None:
+        with _device(dev), _on(stream):
+            out = [torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    if len(out) != 2 or out[0].shape != shape or out[1].shape != shape:
+        raise ValueError("out must be two tensors [B, T, Hkv, d]")
+    _check("srt_kv_read", _on_device(
+        dev, lib().srt_kv_read, kv._ref, kv.B, T, _arg(start, torch.int32, dev, "start"),
+        _arg(out[0], torch.bfloat16, dev, "k_out"), _arg(out[1], torch.bfloat16, dev, "v_out"), _stream_of(dev, stream)))
     return out
 
 
@@ -523,7 +543,8 @@ class Rules:
     """Sampling rules of a batch (srt_rules of include/srt.h), each optional:
     seen [B,V] int16 (the bits of the count words), repetition, frequency,
     presence [B] fp32, bias lists (bias_offsets [B+1] int32, bias_tokens int32,
-    bias_values fp32), mask [B,N,ceil(V/32)] int32 (bits of allowed tokens)."""
+    bias_values fp32), mask [B,N,ceil(V/32)] int32 (bits of allowed tokens).  It
+    keeps the tensors it is made of; their contents may change between calls."""
 
     _TYPES = {"seen": torch.int16, "repetition": torch.float32, "frequency": torch.float32, "presence": torch.float32,
               "bias_offsets": torch.int32, "bias_tokens": torch.int32, "bias_values": torch.float32,
@@ -541,16 +562,20 @@ class Rules:
         if all(has) and t["bias_tokens"].numel() != t["bias_values"].numel():
             raise ValueError("bias_tokens and bias_values differ in length")
         n_bias = int(t["bias_tokens"].numel()) if all(has) else 0
-        self._args = RulesArgs(*[_ptr(t[k], x, k) for k, x in self._TYPES.items()], n_bias, 0)
+        given = [x for x in t.values() if x is not None]
+        self.device = given[0].device if given else None
+        self._args = RulesArgs(*[_maybe(t[k], x, self.device, k) for k, x in self._TYPES.items()], n_bias, 0)
         self._ref = ctypes.byref(self._args)
 
     def check(self, B: int, N: int, V: int, device):
+        if self.device is not None and self.device != device:
+            raise ValueError(f"the rules are on {self.device}, not on {device}")
         want = {"seen": (B, V), "repetition": (B,), "frequency": (B,), "presence": (B,), "bias_offsets": (B + 1,),
                 "mask": (B, N, (V + 31) // 32)}
         for name, shape in want.items():
-            if self.tensors[name] is not None and tuple(self.tensors[name].shape) != shape:
+            t = self.tensors[name]
+            if t is not None and t.shape != shape:
                 raise ValueError(f"{name} must be {list(shape)}")
-        _same_device(device, **self.tensors)
 
 
 def srt_accept_rules(logits, gumbel, inv_temperature: float, rules: Rules, tree_tokens, tree_parent, n_nodes,
@@ -558,27 +583,26 @@ def srt_accept_rules(logits, gumbel, inv_temperature: float, rules: Rules, tree_
     """srt_accept under sampling rules; a walk that finds every token forbidden
     ends with -1 and n_emitted = n_accepted."""
     B, N, V = logits.shape
-    if gumbel is not None and tuple(gumbel.shape) != (B, max_depth + 1, V):
+    if gumbel is not None and gumbel.shape != (B, max_depth + 1, V):
         raise ValueError("gumbel must be [B, max_depth+1, V]")
-    if tuple(tree_tokens.shape) != (B, N) or tuple(tree_parent.shape) != (B, N) or n_nodes.numel() != B:
+    if tree_tokens.shape != (B, N) or tree_parent.shape != (B, N) or n_nodes.numel() != B:
         raise ValueError("tree arrays must be [B, N], n_nodes [B]")
-    dev = logits.device
+    dev, f32, i32 = logits.device, torch.float32, torch.int32
     rules.check(B, N, V, dev)
-    _same_device(dev, gumbel=gumbel, tree_tokens=tree_tokens, tree_parent=tree_parent, n_nodes=n_nodes)
-    need = srt_accept_scratch_bytes(B)
-    with _device(dev):
-        with _on(stream):
+    if out is None or scratch is None or scratch.numel() * scratch.element_size() < srt_accept_scratch_bytes(B):
+        with _device(dev), _on(stream):
             if out is None:
                 out = _walk_outputs(B, max_depth, dev)
-            if scratch is None or scratch.numel() < need:
-                scratch = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-        _check("srt_accept_rules", lib().srt_accept_rules(
-            B, N, V, max_depth, _ptr(logits, torch.float32, "logits"), _ptr(gumbel, torch.float32, "gumbel"),
-            float(inv_temperature), rules._ref, _ptr(tree_tokens, torch.int32, "tree_tokens"),
-            _ptr(tree_parent, torch.int32, "tree_parent"), _ptr(n_nodes, torch.int32, "n_nodes"),
-            _ptr(out["n_accepted"], torch.int32), _ptr(out["out_tokens"], torch.int32),
-            _ptr(out["out_nodes"], torch.int32), _ptr(out.get("n_emitted"), torch.int32), _ptr(scratch, name="scratch"),
-            scratch.numel() * scratch.element_size(), _stream(stream)))
+            scratch = torch.empty(max(srt_accept_scratch_bytes(B), 1), dtype=torch.uint8, device=dev)
+    if scratch.device != dev or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous tensor on {dev}")
+    _check("srt_accept_rules", _on_device(
+        dev, lib().srt_accept_rules, B, N, V, max_depth, _arg(logits, f32, dev, "logits"),
+        _maybe(gumbel, f32, dev, "gumbel"), inv_temperature, rules._ref, _arg(tree_tokens, i32, dev, "tree_tokens"),
+        _arg(tree_parent, i32, dev, "tree_parent"), _arg(n_nodes, i32, dev, "n_nodes"),
+        _arg(out["n_accepted"], i32, dev, "n_accepted"), _arg(out["out_tokens"], i32, dev, "out_tokens"),
+        _arg(out["out_nodes"], i32, dev, "out_nodes"), _maybe(out.get("n_emitted"), i32, dev, "n_emitted"),
+        scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream_of(dev, stream)))
     return out
 
 
@@ -587,13 +611,11 @@ def srt_seen_add(seen, tokens, lengths, prompt: bool = False, reset: bool = Fals
     seen [B,V] int16, in place."""
     if seen.dim() != 2 or tokens.dim() != 2 or tokens.shape[0] != seen.shape[0] or lengths.numel() != seen.shape[0]:
         raise ValueError("seen must be [B, V], tokens [B, T], lengths [B]")
-    B, V = seen.shape
-    _same_device(seen.device, tokens=tokens, lengths=lengths)
-    with _device(seen.device):
-        _check("srt_seen_add", lib().srt_seen_add(
-            _ptr(seen, torch.int16, "seen"), B, V, _ptr(tokens, torch.int32, "tokens"),
-            _ptr(lengths, torch.int32, "lengths"), int(tokens.shape[1]), int(bool(prompt)), int(bool(reset)),
-            _stream(stream)))
+    dev = seen.device
+    _check("srt_seen_add", _on_device(
+        dev, lib().srt_seen_add, _arg(seen, torch.int16, dev, "seen"), seen.shape[0], seen.shape[1],
+        _arg(tokens, torch.int32, dev, "tokens"), _arg(lengths, torch.int32, dev, "lengths"), tokens.shape[1],
+        int(bool(prompt)), int(bool(reset)), _stream_of(dev, stream)))
 
 
 def srt_version() -> str:
