@@ -316,10 +316,19 @@ __global__ __launch_bounds__(kCombineRows * D / 4) void tree_attn_combine_kernel
 // 18 us in a table for 8192 keys, 26 before these rules; 1 of 300: 14 us in one for
 // 32768, 17 before, as only the plan kernel goes).  small = false: without
 // these, for a scratch that has no room for their partials.
-int chunk_for(int32_t B, int32_t Hkv, int64_t RB, int64_t cap, bool small) {
+// fine: for the 8-bit cache's kernel, whose items take half the time and less where trees
+// are narrow, so that a few long items decide more often when the call ends.
+// Fewer than 512 (sequence, KV head) pairs with trees of up to two row blocks
+// then take 4096-key splits where they would take 8192: 64 sequences of
+// 4k to 16k, 28 heads, 4 KV heads, trees of up to 8 / 16 / 32 / 64 nodes: 114 ->
+// 90, 227 -> 137, 242 -> 144, 248 -> 215 us, single tokens 85 -> 78; not from
+// 512 pairs (128 such sequences: 355 and 386 us, single tokens 123 and 128), nor
+// for wider trees, whose partial results cost more (8 of 256 nodes: 530 and 558).
+int chunk_for(int32_t B, int32_t Hkv, int64_t RB, int64_t cap, bool small, bool fine) {
   int chunk = kChunk;
   auto items = [&](int c) { return static_cast<int64_t>(B) * Hkv * RB * ((cap + c - 1) / c); };
   while (chunk > kMinChunk && items(chunk) < 512) chunk /= 2;
+  if (fine && chunk == kChunk && RB <= 2 && static_cast<int64_t>(B) * Hkv < 512) chunk /= 2;
   if (small && chunk == kMinChunk)
     for (int c = kSmallChunk; c < kMinChunk; c *= 2)
       if (cap > c + 512 && cap <= kSmallSplits * c && items(c) <= kSmallItems) return c;
@@ -376,11 +385,12 @@ int64_t combine_grid(const AttnBase& a, int cus) {
 
 // Checks a call's sizes and scratch and fills in everything of `a` that they
 // decide (B, N, Hq, Hkv and cap are set; cap beyond int32 is refused here).
-int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_bytes) {
+int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_bytes, bool fine) {
   const int32_t G = a.Hq / a.Hkv;
   const int64_t RB = (a.N * G + kRowsPerBlock - 1) / kRowsPerBlock;
-  int chunk = chunk_for(a.B, a.Hkv, RB, cap, true);
-  if (scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk)) chunk = chunk_for(a.B, a.Hkv, RB, cap, false);
+  int chunk = chunk_for(a.B, a.Hkv, RB, cap, true, fine);
+  if (scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk))
+    chunk = chunk_for(a.B, a.Hkv, RB, cap, false, false);
   if (!scratch || scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk)) return SRT_ERR_CAPACITY;
   if (reinterpret_cast<uintptr_t>(scratch) % 256) return SRT_ERR_INVALID;
   a.G = G;
@@ -402,9 +412,9 @@ int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_b
 
 // Work-list packing: sequence < 65536, KV head < 256, split < 4096, row block
 // < 2048, combine units < 2^31.
-bool packs(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap) {
+bool packs(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap, bool fine) {
   const int64_t RB = (N * (Hq / Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
-  return B <= 65535 && Hkv <= 255 && splits_for(cap, chunk_for(B, Hkv, RB, cap, true)) <= 4095 &&
+  return B <= 65535 && Hkv <= 255 && splits_for(cap, chunk_for(B, Hkv, RB, cap, true, fine)) <= 4095 &&
          (N * (Hq / Hkv)) / kRowsPerBlock <= 2046 && max_combine_units(B, N, Hq / Hkv, Hkv) <= (int64_t(1) << 30);
 }
 

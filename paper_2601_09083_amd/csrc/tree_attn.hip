@@ -490,7 +490,7 @@ extern "C" size_t srt_tree_attn_scratch_bytes(int32_t B, int32_t N, int32_t Hq, 
   if (B < 0 || N < 1 || N > kMaxN || Hq < 1 || Hkv < 1 || Hq % Hkv || page < 1 || max_pages < 1) return 0;
   const int64_t RB = (N * (Hq / Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
   const int64_t cap = static_cast<int64_t>(page) * max_pages;
-  return scratch_for(B, N, Hq, Hkv, d, cap, chunk_for(B, Hkv, RB, cap, true));
+  return scratch_for(B, N, Hq, Hkv, d, cap, chunk_for(B, Hkv, RB, cap, true, false));
 }
 
 extern "C" int srt_tree_attn(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int32_t page,
@@ -504,7 +504,7 @@ extern "C" int srt_tree_attn(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int3
   if (d != 64 && d != 128) return SRT_ERR_UNSUPPORTED;
   if (page < 16 || (page & (page - 1))) return SRT_ERR_UNSUPPORTED;
   const int64_t cap = static_cast<int64_t>(page) * max_pages;
-  if (!packs(B, N, Hq, Hkv, cap)) return SRT_ERR_UNSUPPORTED;
+  if (!packs(B, N, Hq, Hkv, cap, false)) return SRT_ERR_UNSUPPORTED;
   if (B == 0) return SRT_OK;
   if (!q || !k_cache || !v_cache || !block_table || !ctx_len || !tree_parent || !n_nodes || !out)
     return SRT_ERR_INVALID;
@@ -527,7 +527,7 @@ extern "C" int srt_tree_attn(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int3
   a.max_pages = max_pages;
   a.num_pages = num_pages;
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
-  const int st = lay_out(a, cap, d, scratch, scratch_bytes);
+  const int st = lay_out(a, cap, d, scratch, scratch_bytes, false);
   if (st != SRT_OK) return st;
   a.ctx_cap = a.cap;
 

@@ -96,7 +96,7 @@ template <int D, int KV, int WR>
 __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const SeqInfo si, int b, int g, int s, int rb) {
   using Sh = Shape<D>;
   constexpr int WK = kWaves / WR;             // groups of waves along the keys
-  constexpr int T = WR >= 4 ? 64 : 32;        // keys per tile
+  constexpr int T = WR == 8 ? 64 : 32;        // keys per tile
   constexpr int KB = T / 32;                  // MFMA key blocks per tile
   constexpr int NB = WR == 1 ? 1 : 2;         // tile buffers per key group
   constexpr int KPW = T / WR;                 // keys that a wave stages of each tile
@@ -307,8 +307,15 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
         sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][kb], qf[ks], sacc[kb], 0, 0, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, KB * Sh::KS, 0);  // DS reads
-    __builtin_amdgcn_sched_group_barrier(0x008, KB * Sh::KS, 0);  // then MFMAs
+    // Half of the fragments are read ahead of the products, the other half as
+    // those free their registers (all of them at once spill).
+    __builtin_amdgcn_sched_group_barrier(0x100, KB * Sh::KS / 2, 0);
+#pragma unroll
+    for (int i = 0; i < Sh::KS / 2; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, KB * Sh::KS / 2, 0);
   };
   typedef short i16x4v __attribute__((ext_vector_type(4)));
   auto v_read = [&](const uint8_t* tile, int ks0, i16x4v (&vf)[2][Sh::DB][2]) {
@@ -648,7 +655,7 @@ extern "C" size_t srt_tree_attn_quant_scratch_bytes(const srt_kv_quant* kv, int3
   if (!kv || check_kv_sizes(*kv) != SRT_OK || B < 0 || N < 1 || N > kMaxN || Hq < 1 || Hq % kv->Hkv) return 0;
   const int64_t RB = (N * (Hq / kv->Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
   const int64_t cap = key_cap(*kv, N);
-  return scratch_for(B, N, Hq, kv->Hkv, kv->d, cap, chunk_for(B, kv->Hkv, RB, cap, true));
+  return scratch_for(B, N, Hq, kv->Hkv, kv->d, cap, chunk_for(B, kv->Hkv, RB, cap, true, true));
 }
 
 extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq, const uint16_t* q,
@@ -660,7 +667,7 @@ extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N,
   if (st != SRT_OK) return st;
   if (Hq % kv->Hkv) return SRT_ERR_INVALID;
   const int64_t cap = key_cap(*kv, N);
-  if (!packs(B, N, Hq, kv->Hkv, cap)) return SRT_ERR_UNSUPPORTED;
+  if (!packs(B, N, Hq, kv->Hkv, cap, true)) return SRT_ERR_UNSUPPORTED;
   if (B == 0) return SRT_OK;
   st = check_kv_pointers(*kv);
   if (st == SRT_OK) st = check_new(*kv, k_new, v_new, ld);
@@ -693,7 +700,7 @@ extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N,
   a.num_pages = kv->num_pages;
   a.ld = ld;
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
-  st = lay_out(a, cap, kv->d, scratch, scratch_bytes);
+  st = lay_out(a, cap, kv->d, scratch, scratch_bytes, true);
   if (st != SRT_OK) return st;
   a.ctx_cap = a.cap - N;
 
