@@ -4,7 +4,10 @@
 paged KV cache, queries, logits, noise) and runs the calls of a step:
 ``srt_draft`` -> ``srt_tree_attn`` -> ``srt_accept`` -> ``srt_trie_insert``
 -> ``srt_commit`` (the accepted path becomes context, so the next step drafts
-and attends from the grown sequence).
+and attends from the grown sequence).  With ``kv="e4m3"`` or ``"int8"`` the KV
+cache is held in 8 bits (``srt_tree_attn_quant``, ``srt_commit_quant``); with
+``use_rules`` the policy decodes under sampling rules (``srt_accept_rules``,
+``srt_seen_add``).
 Only buffer management and argument passing happen here; every step of the
 path runs in the HIP kernels of libsrt.
 """
@@ -96,6 +99,27 @@ def node_capacity_for(total_tokens: int, depth: int, headroom_tokens: int = 0) -
     return int((total_tokens + headroom_tokens) * depth) + 1024
 
 
+KV_DTYPES = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def make_kv_quant(B: int, num_pages: int, hkv: int, page: int, d: int, block_table, kv: str = "e4m3",
+                  device="cuda") -> srt.KvQuant:
+    """An empty 8-bit cache for B sequences on the given block table [B, max_pages]."""
+    pages = [torch.zeros((num_pages, hkv, page, d), dtype=torch.uint8, device=device).view(KV_DTYPES[kv])
+             for _ in range(2)]
+    scales = [torch.ones((num_pages, hkv), device=device) for _ in range(2)]
+    tails = [torch.zeros((B, hkv, page, d), dtype=torch.bfloat16, device=device) for _ in range(2)]
+    return srt.KvQuant(*pages, *scales, *tails, block_table, torch.zeros(B, dtype=torch.int32, device=device))
+
+
+def bias_lists(biases: List[Dict[int, float]], device="cuda") -> dict:
+    """Per-sequence {token: bias} as the bias arguments of ``srt.Rules``."""
+    rows = [sorted(x.items()) for x in biases]
+    return dict(bias_offsets=_dev(np.cumsum([0] + [len(x) for x in rows]), device),
+                bias_tokens=_dev(np.array([t for x in rows for t, _ in x], dtype=np.int32), device),
+                bias_values=_dev(np.array([v for x in rows for _, v in x], dtype=np.float32), device, torch.float32))
+
+
 @dataclass
 class VerifyState:
     cfg: W.Config
@@ -121,11 +145,16 @@ class VerifyState:
     acc: dict = field(default_factory=dict)
     accept_scratch: Optional[torch.Tensor] = None
     extra_streams: int = 0
+    kv: Optional[srt.KvQuant] = None       # the 8-bit cache, in place of k_cache and v_cache
+    k_new: Optional[torch.Tensor] = None   # and the tree's own vectors [B, N, Hkv, d]
+    v_new: Optional[torch.Tensor] = None
+    rules: Optional[srt.Rules] = None
+    seen: Optional[torch.Tensor] = None    # count rows [B, V] that the penalties read
 
     # ---- set-up ---------------------------------------------------------
     @classmethod
     def build(cls, cfg: W.Config, device="cuda", tokens: Optional[W.TokenWorkload] = None,
-              steps_headroom: int = 64, with_seqs: bool = True, kv_headroom: int = 0):
+              steps_headroom: int = 64, with_seqs: bool = True, kv_headroom: int = 0, kv: str = "bf16"):
         tw = W.make_tokens(cfg) if tokens is None else tokens
         B = tw.batch
         streams, sp = [], []
@@ -156,8 +185,44 @@ class VerifyState:
         st.attn_out = torch.empty_like(q)
         need = srt.srt_tree_attn_scratch_bytes(B, cfg.n_nodes, cfg.hq, cfg.hkv, cfg.head_dim, cfg.page,
                                                int(bt.shape[1]))
+        if kv != "bf16":
+            st._quantise(kv)
+            need = srt.srt_tree_attn_quant_scratch_bytes(st.kv, cfg.n_nodes, cfg.hq)
         st.scratch = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
         return st
+
+    def _quantise(self, kv: str, piece: int = 1024):
+        """Moves the contexts into an 8-bit cache, a piece of them at a time; the
+        vectors at the tree's places become the tree's own."""
+        c, B = self.cfg, self.tokens.batch
+        self.kv = make_kv_quant(B, self.num_pages, c.hkv, c.page, c.head_dim, self.block_table, kv, self.device)
+        lens = self.attn_len.long()
+
+        def rows(cache, p):  # positions p [B, T] of every sequence
+            pg = self.block_table.gather(1, (p // c.page).clamp(max=self.block_table.shape[1] - 1)).long().clamp(min=0)
+            return cache[pg, :, p % c.page].contiguous()
+
+        for t0 in range(0, int(lens.max()), piece):
+            p = (t0 + torch.arange(piece, device=self.device)).expand(B, -1)
+            srt.srt_kv_append(self.kv, rows(self.k_cache, p), rows(self.v_cache, p),
+                              (lens - t0).clamp(0, piece).to(torch.int32))
+        p = lens[:, None] + torch.arange(c.n_nodes, device=self.device)
+        self.k_new, self.v_new = rows(self.k_cache, p), rows(self.v_cache, p)
+        self.k_cache = self.v_cache = None
+        self.attn_len = self.kv.ctx_len
+
+    def use_rules(self, repetition=None, frequency=None, presence=None, biases=None, mask=None):
+        """Sampling rules for the steps that follow: per-sequence penalties (lists
+        or arrays [B]) over the tokens of the running sequences so far, biases (a
+        {token: bias} per sequence), mask [B, N, ceil(V / 32)] int32."""
+        tw, dev = self.tokens, self.device
+        mat, lens = W.pack_streams(list(tw.seqs))
+        self.seen = torch.zeros((tw.batch, self.cfg.vocab), dtype=torch.int16, device=dev)
+        srt.srt_seen_add(self.seen, _dev(mat, dev), _dev(lens, dev), reset=True)
+        f = lambda x: None if x is None else _dev(np.asarray(x, dtype=np.float32), dev, torch.float32)
+        self.rules = srt.Rules(seen=self.seen, repetition=f(repetition), frequency=f(frequency), presence=f(presence),
+                               mask=mask, **(bias_lists(biases, dev) if biases is not None else {}))
+        return self.rules
 
     def make_logits(self, boost: Optional[str] = None, sampled: bool = True, sigma: Optional[float] = None):
         """Per-node logits (boosting each node's first drafted child) and
@@ -177,6 +242,9 @@ class VerifyState:
         return self.tree
 
     def attention(self):
+        if self.kv is not None:
+            return srt.srt_tree_attn_quant(self.q, self.kv, self.k_new, self.v_new, self.tree["tree_parent"],
+                                           self.tree["n_nodes"], self.scale, out=self.attn_out, scratch=self.scratch)
         return srt.srt_tree_attn(self.q, self.k_cache, self.v_cache, self.block_table, self.attn_len,
                                  self.tree["tree_parent"], self.tree["n_nodes"], self.scale, out=self.attn_out,
                                  scratch=self.scratch)
@@ -185,6 +253,11 @@ class VerifyState:
         if self.accept_scratch is None:
             self.accept_scratch = torch.empty(max(srt.srt_accept_scratch_bytes(self.tokens.batch), 1),
                                               dtype=torch.uint8, device=self.device)
+        if self.rules is not None:
+            self.acc = srt.srt_accept_rules(self.logits, self.gumbel, inv_temperature, self.rules,
+                                            self.tree["tree_tokens"], self.tree["tree_parent"], self.tree["n_nodes"],
+                                            self.cfg.max_depth, out=self.acc or None, scratch=self.accept_scratch)
+            return self.acc
         self.acc = srt.srt_accept(self.logits, self.gumbel, inv_temperature, self.tree["tree_tokens"],
                                   self.tree["tree_parent"], self.tree["n_nodes"], self.cfg.max_depth,
                                   out=self.acc or None, scratch=self.accept_scratch)
@@ -193,8 +266,14 @@ class VerifyState:
     def insert(self):
         srt.srt_trie_insert(self.caches.ws, self.prompt_ids, self.seq_stream_dev, self.acc["out_tokens"],
                             self.acc["n_emitted"])
+        if self.seen is not None:
+            srt.srt_seen_add(self.seen, self.acc["out_tokens"], self.acc["n_emitted"])
 
     def commit(self):
+        if self.kv is not None:
+            srt.srt_commit_quant(self.kv, self.k_new, self.v_new, self.acc["n_accepted"], self.acc["out_tokens"],
+                                 self.acc["out_nodes"], ctx_tail=self.ctx_tail, draft_len=self.draft_len)
+            return
         srt.srt_commit(self.k_cache, self.v_cache, self.block_table, self.attn_len, self.acc["n_accepted"],
                        self.acc["out_tokens"], self.acc["out_nodes"], self.cfg.n_nodes, ctx_tail=self.ctx_tail,
                        draft_len=self.draft_len)
