@@ -464,7 +464,12 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
     i16x4v vf0[2][Sh::DB][2];
     v_read(tile, 0, vf0);
     bf16x8 pb[2 * KB];
+    // Of the two waves on a SIMD the one in its softmax issues first: the other's
+    // MFMAs wait little for it, its own for the softmax (8 sequences with trees of
+    // 64 to 256 nodes: 530 -> 512 us; of no use where waves wait for HBM).
+    if constexpr (WR >= 4) __builtin_amdgcn_s_setprio(1);
     softmax(open_c, t0, sacc, pb);
+    if constexpr (WR >= 4) __builtin_amdgcn_s_setprio(0);
     if constexpr (KB == 2) {
       i16x4v vf1[2][Sh::DB][2];
       v_read(tile, 2, vf1);
