@@ -371,3 +371,31 @@ def test_offsets_beyond_32_bits():
     near = new_cache(1, hkv, page, d, "int8", 3, "cuda")
     srt.srt_kv_append(near, bf16(k).cuda(), bf16(v).cuda(), i32([700]))
     assert torch.equal(a, srt.srt_tree_attn_quant(q, near, kn, kn, i32([[-1]]), i32([1]), d ** -0.5))
+
+
+@pytest.mark.parametrize("kv,d,page", [("e4m3", 128, 16), ("int8", 128, 32), ("e4m3", 64, 64), ("int8", 64, 128)])
+def test_calls_that_stream_equal_small_ones(kv, d, page):
+    """128 MiB of rows and more are written and read non-temporally: the same bits
+    as in pieces, and a sample of them as the oracle's."""
+    B, T, hkv = 4, 8192 + 40, 1024 // d
+    g = torch.Generator(device="cuda").manual_seed(d + page)
+    k, v = (torch.randn((B, T, hkv, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    counts = [T, T - 7, 0, 5000]
+    big, small = (new_cache(B, hkv, page, d, kv, T // page + 1, "cuda", seed=3) for _ in range(2))
+    srt.srt_kv_append(big, k, v, i32(counts))
+    for t0 in range(0, T, 2000):
+        part = [x[:, t0:t0 + 2000].contiguous() for x in (k, v)]
+        srt.srt_kv_append(small, *part, i32(np.clip(np.array(counts) - t0, 0, part[0].shape[1])))
+    for x, y in zip(big.tensors[:4] + (big.ctx_len,), small.tensors[:4] + (small.ctx_len,)):
+        same = (lambda z: z.view(torch.uint8)) if x.element_size() == 1 else (lambda z: z)
+        assert torch.equal(same(x), same(y))
+    zero = i32([0] * B)
+    whole = srt.srt_kv_read(big, zero, T)  # (tails among them; their rows behind the context hold anything)
+    for x, y in zip(whole, srt.srt_kv_read(small, zero, T)):
+        assert torch.equal(x, y)
+    for t0 in range(0, T, 2000):
+        part = srt.srt_kv_read(big, i32([t0] * B), min(2000, T - t0))
+        for x, y in zip(whole, part):
+            assert torch.equal(x[:, t0:t0 + 2000], y)
+    want, _, _ = KQ.context(k[1, :3 * page + 1].float().cpu().numpy(), kv, page)
+    assert torch.equal(whole[0][1, :3 * page].cpu(), bf16(want[:3 * page]))
