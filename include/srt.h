@@ -359,7 +359,7 @@ int srt_commit(int32_t B, int32_t N, int32_t Hkv, int32_t d, int32_t page, int32
  *   - in a page, if its page is full (p < F = L - L % page): the code at slot
  *     p % page of page block_table[b, p / page], whose value is code * scale
  *     with the scale of that page, KV head and tensor;
- *   - else in the sequence's tail, row p % page, in bf16.
+ *   - else in the sequence's tail, row p % page, in bf16 (rows L % page .. hold anything).
  * A page is quantised once, when it is full, from the bf16 vectors in the
  * tail: with amp = max(max |x| over the page's page x d values of a KV head,
  * 2^-60) and top = 448 (SRT_KV_E4M3) or 127 (SRT_KV_INT8),
@@ -419,7 +419,11 @@ typedef struct {
  * v_scale is taken as at least 2^-70 and at most 2^100.
  * q, out [B, N, Hq, d] bf16; tree_parent [B, N], n_nodes [B], scale, scratch,
  * limits and errors as srt_tree_attn, with max_pages * page + page + N - 1
- * in the place of max_pages * page. */
+ * in the place of max_pages * page; q and out 16-byte aligned (else
+ * SRT_ERR_INVALID); srt_tree_attn_quant_scratch_bytes is 0 for arguments that
+ * the call refuses.  The vectors of live nodes must be finite; rows of k_new and
+ * v_new from n_nodes[b] on, tail rows from L % page on and pages and scales of
+ * no live position are not read. */
 size_t srt_tree_attn_quant_scratch_bytes(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq);
 
 int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq, const uint16_t* q,

@@ -413,9 +413,10 @@ int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_b
 // Work-list packing: sequence < 65536, KV head < 256, split < 4096, row block
 // < 2048, combine units < 2^31.
 bool packs(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap, bool fine) {
+  if (static_cast<int64_t>(N) * (Hq / Hkv) / kRowsPerBlock > 2046) return false;
   const int64_t RB = (N * (Hq / Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
   return B <= 65535 && Hkv <= 255 && splits_for(cap, chunk_for(B, Hkv, RB, cap, true, fine)) <= 4095 &&
-         (N * (Hq / Hkv)) / kRowsPerBlock <= 2046 && max_combine_units(B, N, Hq / Hkv, Hkv) <= (int64_t(1) << 30);
+         max_combine_units(B, N, Hq / Hkv, Hkv) <= (int64_t(1) << 30);
 }
 
 }  // namespace

@@ -492,7 +492,7 @@ extern "C" int srt_seen_add(uint16_t* seen, int32_t B, int32_t V, const int32_t*
   if (reset) {
     seen_rows_kernel<true><<<static_cast<unsigned>(chunks * B), 1024, 0, s>>>(a, static_cast<int>(chunks));
   } else if (stride <= kSeenStep) {
-    seen_step_kernel<<<static_cast<unsigned>((B + 3) / 4), 256, 0, s>>>(a);
+    seen_step_kernel<<<static_cast<unsigned>((static_cast<int64_t>(B) + 3) / 4), 256, 0, s>>>(a);
   } else {
     seen_rows_kernel<false><<<static_cast<unsigned>(chunks * B), 1024, 0, s>>>(a, static_cast<int>(chunks));
   }

@@ -658,8 +658,9 @@ int64_t key_cap(const srt_kv_quant& kv, int32_t N) {
 
 extern "C" size_t srt_tree_attn_quant_scratch_bytes(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq) {
   if (!kv || check_kv_sizes(*kv) != SRT_OK || B < 0 || N < 1 || N > kMaxN || Hq < 1 || Hq % kv->Hkv) return 0;
-  const int64_t RB = (N * (Hq / kv->Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
   const int64_t cap = key_cap(*kv, N);
+  if (!packs(B, N, Hq, kv->Hkv, cap, true)) return 0;
+  const int64_t RB = (N * (Hq / kv->Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
   return scratch_for(B, N, Hq, kv->Hkv, kv->d, cap, chunk_for(B, kv->Hkv, RB, cap, true, true));
 }
 

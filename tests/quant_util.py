@@ -132,7 +132,7 @@ class AttnCase:
         return ref, 1.02 * tol  # (second order terms)
 
     def check(self, out, seqs=None, what=""):
-        o = out.float().cpu().numpy().astype(np.float64)
+        o = out.double().cpu().numpy()
         worst = 0.0
         for b in range(self.B) if seqs is None else seqs:
             n = int(self.n_nodes[b])

@@ -81,6 +81,8 @@ def test_attention_arguments():
     assert need > 0 and need % 4 == 0
     assert attn(c, size=16) == S.SRT_ERR_CAPACITY and attn(c, scratch=None) == S.SRT_ERR_CAPACITY
     assert attn(c, B=65536) == S.SRT_ERR_UNSUPPORTED
+    assert attn(c, N=256, Hq=1 << 30) == S.SRT_ERR_UNSUPPORTED
+    assert S.lib().srt_tree_attn_quant_scratch_bytes(ctypes.byref(c), 4, 256, 1 << 30) == 0
     assert attn(kv(page=256, max_pages=1 << 21)) == S.SRT_ERR_UNSUPPORTED  # more than 4095 splits
     assert S.lib().srt_tree_attn_quant_scratch_bytes(None, 4, 8, 4) == 0
     assert S.lib().srt_tree_attn_quant(None, 4, 8, 4, P, P, P, 256, P, P, 0.1, P, P, 1 << 30, None) == S.SRT_ERR_INVALID

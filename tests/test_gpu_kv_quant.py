@@ -216,6 +216,23 @@ def test_attention_wide_trees_and_long_contexts():
     print(f"tolerance used: {c.check(c.run()):.3f}", flush=True)
 
 
+@pytest.mark.parametrize("kv", ["e4m3", "int8"])
+def test_attention_splits_that_end_inside_a_tree(kv):
+    """Rows that see nothing of the last split: 256-, 1024- and 2048-key splits
+    that end among the tree's keys, in its tail, or just before either."""
+    for B, ctx in ((3, [1014, 1023, 1008]), (2, [250, 1270]), (24, [2040 - i for i in range(24)])):
+        c = AttnCase(14 + B, B, 64, 14, 2, 64, ctx, kv, n_nodes=[64] * B, max_pages=max(ctx) // 16 + 4)
+        c.check(c.run(), what=f"{B} sequences")
+
+
+def test_attention_takes_a_smaller_scratch():
+    """A scratch for larger splits only serves; one that is too small is replaced."""
+    c = AttnCase(15, 2, 4, 7, 1, 128, [900, 300])
+    need = srt.srt_tree_attn_quant_scratch_bytes(c.cache, c.N, c.hq)
+    for size in (need, need - 256, need // 2, 256):
+        c.check(c.run(scratch=torch.empty(size, dtype=torch.uint8, device="cuda")), what=f"scratch of {size}")
+
+
 def test_attention_large_splits():
     # 8192-key splits: 256 sequence-head pairs with 16k of room
     base = [8192 - 64 - 7, 8192, 9000, 12345, 16354, 100, 5000, 8193]
