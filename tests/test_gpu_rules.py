@@ -201,8 +201,8 @@ def test_walk_on_a_side_stream_and_replayed_from_graphs():
 
 # --------------------------------------------------------------------------- counts
 
-@pytest.mark.parametrize("V", [1, 7, 1001, 16384, 16385, 70000])
-@pytest.mark.parametrize("T", [1, 13, 64, 65, 3000])
+@pytest.mark.parametrize("V", [1, 7, 1001, 16384, 16385, 32767, 32769, 70000])
+@pytest.mark.parametrize("T", [1, 13, 64, 65, 3000, 66000])
 def test_seen_add(V, T):
     rng = np.random.default_rng(V + T)
     B = 5
