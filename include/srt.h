@@ -13,6 +13,10 @@
  *    nodes only)
  *   srt_trie_insert-> emitted tokens appended to the sequence's stream
  *   srt_commit     -> accepted nodes' K/V moved into place, context advanced
+ * Beside these, the same step over a KV cache of 8-bit pages
+ *   srt_kv_append, srt_tree_attn_quant, srt_commit_quant, srt_kv_read
+ * and the acceptance walk under penalties, biases and masks
+ *   srt_accept_rules, srt_seen_add
  *
  * Conventions shared by every entry point
  *   - Pointers are device pointers unless the comment says "host".  All

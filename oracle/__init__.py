@@ -30,8 +30,12 @@ method computes, written from the paper (SRT, arXiv 2601.09083):
                    state (Section 3's single verification pass), in fp64
                    rounded once to fp32, with the bound for other fp32
                    summation orders.
+* ``kv_quant``  -- the 8-bit KV cache: a page's codes and scales, its values,
+                   what a sequence's context holds.
+* ``rules``     -- the acceptance walk under penalties, biases and masks, and
+                   the token counts they read.
 
 Pins (tests marked ``not gpu``) tie each function to closed forms, brute
 force, library routines and invariants; see ``tests/test_oracle_*.py``.
 """
-from . import accept, attention, commit, draft, lmhead, trie  # noqa: F401
+from . import accept, attention, commit, draft, kv_quant, lmhead, rules, trie  # noqa: F401
