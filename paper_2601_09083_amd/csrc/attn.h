@@ -45,8 +45,11 @@ struct AttnBase {
   int32_t cap;      // positions that context and tree may take together
   int32_t ctx_cap;  // positions that the context may take
   int32_t S, RB, total;
+  int32_t part_rows;  // rows of a partial result
   int32_t chunk;  // keys per split: a power of two in [kSmallChunk, kChunk]
 };
+
+constexpr int kNarrowRows = 32;  // of the trees that the 8-bit cache's kernel takes with half the waves
 
 // Work list: plan[0] = number of items, plan[1] = next item to hand out,
 // then item i at plan[kPlanHeader + 2 i] = sequence, [.. + 1] = KV head |
@@ -253,7 +256,7 @@ __global__ __launch_bounds__(kCombineRows * D / 4) void tree_attn_combine_kernel
   constexpr int Q = D / 4;
   const int per_head = kDirect ? (a.N * a.G + kCombineRows - 1) / kCombineRows : a.plan[3] | 1;
   const int n_units = (kDirect ? a.B : a.plan[2]) * a.Hkv * per_head;
-  const int RBR = a.RB * kRowsPerBlock;
+  const int RBR = a.part_rows;
   const int q = threadIdx.x % Q;
   for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
     const int e = u / (a.Hkv * per_head), rest = u - e * a.Hkv * per_head;
@@ -316,19 +319,22 @@ __global__ __launch_bounds__(kCombineRows * D / 4) void tree_attn_combine_kernel
 // 18 us in a table for 8192 keys, 26 before these rules; 1 of 300: 14 us in one for
 // 32768, 17 before, as only the plan kernel goes).  small = false: without
 // these, for a scratch that has no room for their partials.
-// fine: for the 8-bit cache's kernel, whose items take half the time and less where trees
-// are narrow, so that a few long items decide more often when the call ends.
-// Fewer than 512 (sequence, KV head) pairs with trees of up to two row blocks
-// then take 4096-key splits where they would take 8192: 64 sequences of
-// 4k to 16k, 28 heads, 4 KV heads, trees of up to 8 / 16 / 32 / 64 nodes: 114 ->
-// 90, 227 -> 137, 242 -> 144, 248 -> 215 us, single tokens 85 -> 78; not from
-// 512 pairs (128 such sequences: 355 and 386 us, single tokens 123 and 128), nor
-// for wider trees, whose partial results cost more (8 of 256 nodes: 530 and 558).
-int chunk_for(int32_t B, int32_t Hkv, int64_t RB, int64_t cap, bool small, bool fine) {
-  int chunk = kChunk;
+// rows: query rows of the widest tree for the 8-bit cache's kernel, whose items take
+// half the time and less where trees are narrow, so that a few long items decide more
+// often when the call ends; 0 for the bf16 cache's.  Fewer than 512 (sequence, KV head)
+// pairs with trees of up to two row blocks then take 4096-key splits where they would
+// take 8192: 64 sequences of 4k to 16k, 28 heads, 4 KV heads, trees of up to 8 / 16 /
+// 32 / 64 nodes: 114 -> 90, 227 -> 137, 242 -> 144, 248 -> 215 us; not from 512 pairs
+// (128 such sequences: 355 and 386 us), nor for wider trees, whose partial results cost
+// more (8 of 256 nodes: 530 and 558).  Trees of up to kNarrowRows rows always do, as two
+// of their workgroups share a CU's rate (28 heads, 4 KV heads, single tokens or 4 nodes:
+// 300 sequences of 300 to 32k keys 109 -> 85 us, 256 of 2k to 8k 116 -> 114; at most 3%
+// the other way, 256 of 16k to 32k: 957 -> 988; with 2048 keys 93, 120 and 1061).
+int chunk_for(int32_t B, int32_t Hkv, int64_t RB, int64_t cap, bool small, int64_t rows) {
+  int chunk = rows > 0 && rows <= kNarrowRows ? kChunk / 2 : kChunk;
   auto items = [&](int c) { return static_cast<int64_t>(B) * Hkv * RB * ((cap + c - 1) / c); };
   while (chunk > kMinChunk && items(chunk) < 512) chunk /= 2;
-  if (fine && chunk == kChunk && RB <= 2 && static_cast<int64_t>(B) * Hkv < 512) chunk /= 2;
+  if (rows > 0 && chunk == kChunk && RB <= 2 && static_cast<int64_t>(B) * Hkv < 512) chunk /= 2;
   if (small && chunk == kMinChunk)
     for (int c = kSmallChunk; c < kMinChunk; c *= 2)
       if (cap > c + 512 && cap <= kSmallSplits * c && items(c) <= kSmallItems) return c;
@@ -349,13 +355,21 @@ size_t plan_bytes(int64_t items, int64_t units) {
   return ((kPlanHeader + 2 * items + 2 * units) * sizeof(int32_t) + 255) / 256 * 256;
 }
 
-size_t scratch_for(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int64_t cap, int chunk) {
+// Rows of a (sequence, KV head, split) that the partial results hold room for: whole
+// row blocks for the bf16 cache's kernel, the widest tree's rows for the 8-bit one's
+// (single tokens of 256 sequences of up to 32k, 28 heads, 4 KV heads: 30 MB for 1.1 GB).
+int64_t part_rows(int32_t N, int32_t G, bool quant) {
+  const int64_t rows = static_cast<int64_t>(N) * G;
+  return quant ? rows : (rows + kRowsPerBlock - 1) / kRowsPerBlock * kRowsPerBlock;
+}
+
+size_t scratch_for(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int64_t cap, int chunk, bool quant) {
   const int G = Hq / Hkv;
   const int64_t RB = (N * G + kRowsPerBlock - 1) / kRowsPerBlock;
   const int S = splits_for(cap, chunk);
   const size_t plan = plan_bytes(static_cast<int64_t>(B) * Hkv * S * RB, max_combine_units(B, N, G, Hkv));
   if (S <= 1) return plan;
-  return plan + static_cast<size_t>(B) * Hkv * S * RB * kRowsPerBlock * (d + 2) * sizeof(float);
+  return plan + static_cast<size_t>(B) * Hkv * S * part_rows(N, G, quant) * (d + 2) * sizeof(float);
 }
 
 int cu_count() {
@@ -385,19 +399,20 @@ int64_t combine_grid(const AttnBase& a, int cus) {
 
 // Checks a call's sizes and scratch and fills in everything of `a` that they
 // decide (B, N, Hq, Hkv and cap are set; cap beyond int32 is refused here).
-int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_bytes, bool fine) {
+int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_bytes, bool quant) {
   const int32_t G = a.Hq / a.Hkv;
   const int64_t RB = (a.N * G + kRowsPerBlock - 1) / kRowsPerBlock;
-  int chunk = chunk_for(a.B, a.Hkv, RB, cap, true, fine);
-  if (scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk))
-    chunk = chunk_for(a.B, a.Hkv, RB, cap, false, false);
-  if (!scratch || scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk)) return SRT_ERR_CAPACITY;
+  int chunk = chunk_for(a.B, a.Hkv, RB, cap, true, quant ? a.N * G : 0);
+  if (scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk, quant))
+    chunk = chunk_for(a.B, a.Hkv, RB, cap, false, 0);
+  if (!scratch || scratch_bytes < scratch_for(a.B, a.N, a.Hq, a.Hkv, d, cap, chunk, quant)) return SRT_ERR_CAPACITY;
   if (reinterpret_cast<uintptr_t>(scratch) % 256) return SRT_ERR_INVALID;
   a.G = G;
   a.cap = static_cast<int32_t>(cap);
   a.chunk = chunk;
   a.S = splits_for(cap, chunk);
   a.RB = static_cast<int32_t>(RB);
+  a.part_rows = static_cast<int32_t>(part_rows(a.N, G, quant));
   const int64_t total = static_cast<int64_t>(a.B) * a.Hkv * a.S * a.RB;
   if (total > (int64_t(1) << 30)) return SRT_ERR_INVALID;
   a.total = static_cast<int32_t>(total);
@@ -406,16 +421,16 @@ int lay_out(AttnBase& a, int64_t cap, int32_t d, void* scratch, size_t scratch_b
   a.combine_at = kPlanHeader + 2 * total;
   a.part_o = a.S > 1 ? reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + pbytes) : nullptr;
   a.part_ml =
-      a.S > 1 ? a.part_o + static_cast<int64_t>(a.B) * a.Hkv * a.S * a.RB * kRowsPerBlock * d : nullptr;
+      a.S > 1 ? a.part_o + static_cast<int64_t>(a.B) * a.Hkv * a.S * a.part_rows * d : nullptr;
   return SRT_OK;
 }
 
 // Work-list packing: sequence < 65536, KV head < 256, split < 4096, row block
 // < 2048, combine units < 2^31.
-bool packs(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap, bool fine) {
+bool packs(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap, bool quant) {
   if (static_cast<int64_t>(N) * (Hq / Hkv) / kRowsPerBlock > 2046) return false;
   const int64_t RB = (N * (Hq / Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
-  return B <= 65535 && Hkv <= 255 && splits_for(cap, chunk_for(B, Hkv, RB, cap, true, fine)) <= 4095 &&
+  return B <= 65535 && Hkv <= 255 && splits_for(cap, chunk_for(B, Hkv, RB, cap, true, quant ? N * (Hq / Hkv) : 0)) <= 4095 &&
          max_combine_units(B, N, Hq / Hkv, Hkv) <= (int64_t(1) << 30);
 }
 

@@ -490,7 +490,7 @@ extern "C" size_t srt_tree_attn_scratch_bytes(int32_t B, int32_t N, int32_t Hq, 
   if (B < 0 || N < 1 || N > kMaxN || Hq < 1 || Hkv < 1 || Hq % Hkv || page < 1 || max_pages < 1) return 0;
   const int64_t RB = (N * (Hq / Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
   const int64_t cap = static_cast<int64_t>(page) * max_pages;
-  return scratch_for(B, N, Hq, Hkv, d, cap, chunk_for(B, Hkv, RB, cap, true, false));
+  return scratch_for(B, N, Hq, Hkv, d, cap, chunk_for(B, Hkv, RB, cap, true, 0), false);
 }
 
 extern "C" int srt_tree_attn(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int32_t page,

@@ -23,7 +23,7 @@
 //     head would be bound by one wave's chain per tile (1.3 us for 64 keys in
 //     tree_attn.hip, whatever the rows).  A workgroup's 8 waves are therefore
 //     WR waves along the rows times 8 / WR along the keys, by the rows that the
-//     item has: up to 32 rows every wave streams 32-key tiles of its own,
+//     item has (4 waves, two workgroups to a CU, in batches of narrow trees): up to 32 rows every wave streams 32-key tiles of its own,
 //     with no barrier at all, up to 64 and 128 pairs and fours of waves share
 //     a tile, and the key groups' partial results are merged in LDS at the end.
 #include "attn.h"
@@ -50,19 +50,34 @@ struct QuantArgs : AttnBase {
 };
 
 constexpr int kGroup = 16;  // keys that share their scales (a page has at least as many)
+// Trees of up to kNarrowRows rows: workgroups of this many waves, two to a CU, so that
+// one streams while the other claims, fills, drains and merges (28 heads, 4 KV heads,
+// single tokens: 256 sequences of 200 to 2000 keys 52 -> 36 us, 512 of 2k to 10k 237 ->
+// 217; with workgroups of two waves, four to a CU, 50 and 234).  A batch that has an
+// item for every CU at most keeps 8 waves (4 sequences: 10.2 and 11.1), and so would one
+// whose keys lie in few long sequences, which the host does not see (16 sequences of
+// 4000 to 30000 keys, 32 heads, 8 KV heads: 54 -> 62).
+constexpr int kNarrowWaves = 4;
+// Bytes of a bf16 row times keys of the table, up to which a narrow batch has a
+// workgroup launched for every item: no list, no claims (185 sequences of 60 keys, 8 KV
+// heads of 64, 27 nodes: 37 -> 18.6 us; 28 heads, 4 KV heads of 128, 512 sequences of up
+// to 1500 keys, one node: 50.7 -> 42.3; 256 of up to 2000: 35.9 -> 37.1, the longest no
+// longer come first).
+constexpr int64_t kUnlisted = 1536 * 2 * 128;
 constexpr float kLeastScale = 0x1p-70f, kMostScale = 0x1p100f;
 
-template <int D>
+template <int D, int W>
 struct Smem {
   using Sh = Shape<D>;
   static constexpr int kRow = Sh::KSTRIDE + Sh::VSTRIDE;
-  __attribute__((aligned(16))) uint8_t pool[256 * kRow];  // tiles, then the key groups' partial results
-  uint64_t anc[kMaxN][4];
-  int32_t spar[kMaxN];
+  static constexpr int kNodes = W == kWaves ? kMaxN : kNarrowRows;
+  __attribute__((aligned(16))) uint8_t pool[32 * W * kRow];  // tiles, then the key groups' partial results
+  uint64_t anc[kNodes][4];
+  int32_t spar[kNodes];
   __attribute__((aligned(16))) float kc[kChunk / kGroup];  // scale * log2(e) * sk of the split's key groups
   __attribute__((aligned(16))) float lv[kChunk / kGroup];  // log2(sv)
   __attribute__((aligned(16))) float rv[kChunk / kGroup];  // 1 / sv
-  float m[kWaves][kRowsPerWave], l[kWaves][kRowsPerWave];
+  float m[W][kRowsPerWave], l[W][kRowsPerWave];
 };
 
 // The place in a row of K or V of 16-byte chunk c of its LDS row.  A lane holds
@@ -91,11 +106,11 @@ __device__ inline uint2 widen(uint32_t w) {
 }
 
 // One work item: rows rb * 256 .. of (sequence b, KV head g) against the keys of
-// split s, WR waves along the rows.
-template <int D, int KV, int WR>
-__device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const SeqInfo si, int b, int g, int s, int rb) {
+// split s, with W waves, WR of them along the rows.
+template <int D, int KV, int WR, int W>
+__device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W>& sm, const SeqInfo si, int b, int g, int s, int rb) {
   using Sh = Shape<D>;
-  constexpr int WK = kWaves / WR;             // groups of waves along the keys
+  constexpr int WK = W / WR;                  // groups of waves along the keys
   constexpr int T = WR == 8 ? 64 : 32;        // keys per tile
   constexpr int KB = T / 32;                  // MFMA key blocks per tile
   constexpr int NB = WR == 1 ? 1 : 2;         // tile buffers per key group
@@ -104,15 +119,15 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
   constexpr int UPT = KPW / U;
   constexpr int LPU = U / 8;                  // loads per unit: 8 rows each, 8 lanes a row
   constexpr int EPL = D / 8;                  // codes per lane and load
-  constexpr int NPG = kChunk / kWaves / U / SRT_WAVE;  // registers of page ids
+  constexpr int NPG = kChunk / W / U / SRT_WAVE;  // registers of page ids
   constexpr int kTileBytes = T * (Sh::KSTRIDE + Sh::VSTRIDE);
   // Few rows: the pages are read once, by this workgroup alone, and need no
   // place in the caches (256 sequences of one node, 28 heads: 260 us with
   // ordinary loads, 225 with non-temporal ones; other row blocks read wide
   // trees' pages again: 531 and 543).
   constexpr int kAux = WR == 8 ? 0 : 2;
-  static_assert(NB * WK * T <= 256, "tiles fit the pool");
-  static_assert(NPG * SRT_WAVE * U * kWaves == kChunk && NPG >= 1, "page ids of a split");
+  static_assert(NB * WK * T <= 32 * W, "tiles fit the pool");
+  static_assert(NPG * SRT_WAVE * U * W == kChunk && NPG >= 1, "page ids of a split");
 
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE);
@@ -134,7 +149,7 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
   // Scales of the split's key groups.
   const int64_t bt_row = static_cast<int64_t>(b) * a.max_pages;
   const int pshift = a.page_shift, pmask = a.page - 1;
-  for (int i = tid; i < n1 * (T / kGroup); i += kThreads) {
+  for (int i = tid; i < n1 * (T / kGroup); i += W * SRT_WAVE) {
     const int p = k_begin + i * kGroup;
     float ks = 1.f, vs = 1.f;
     if (p < lim) {
@@ -151,9 +166,9 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
   }
   // Ancestor-or-self bitsets, where the split reaches the tree.
   if (k_end > si.L) {
-    for (int i = tid; i < si.n; i += kThreads) sm.spar[i] = a.parent[static_cast<int64_t>(b) * a.N + i];
+    for (int i = tid; i < si.n; i += W * SRT_WAVE) sm.spar[i] = a.parent[static_cast<int64_t>(b) * a.N + i];
     __syncthreads();
-    for (int i = tid; i < si.n; i += kThreads) {
+    for (int i = tid; i < si.n; i += W * SRT_WAVE) {
       uint64_t bits[4] = {0, 0, 0, 0};
       int j = i;
       while (j >= 0) {
@@ -529,8 +544,7 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
 
   // ---- results --------------------------------------------------------------
   const float lt = sum_halves(l);
-  const int RBR = a.RB * kRowsPerBlock;
-  const int64_t part0 = ((static_cast<int64_t>(b) * a.Hkv + g) * a.S + s) * RBR;
+  const int64_t part0 = ((static_cast<int64_t>(b) * a.Hkv + g) * a.S + s) * a.part_rows;
   if constexpr (WK == 1) {
     if (!row_ok) return;
     const int hq = g * a.G + row % a.G;
@@ -560,7 +574,7 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
   } else {
     // Merge of the key groups: out = sum 2^(m_k - M) O_k over the groups.
     constexpr int PS = D + 4;  // floats per partial row (conflict-free 16-byte stores)
-    static_assert(kWaves * kRowsPerWave * PS * 4 <= static_cast<int>(sizeof(sm.pool)), "partial results fit the pool");
+    static_assert(W * kRowsPerWave * PS * 4 <= static_cast<int>(sizeof(sm.pool)), "partial results fit the pool");
     float* part = reinterpret_cast<float*>(sm.pool);
     __syncthreads();  // every wave has read its last tile
     if (wave_active) {
@@ -578,7 +592,7 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
     __syncthreads();
     constexpr int Q = D / 4;
     const int here = min(WR * kRowsPerWave, rows - rb * kRowsPerBlock);
-    for (int i = tid; i < here * Q; i += kThreads) {
+    for (int i = tid; i < here * Q; i += W * SRT_WAVE) {
       const int r = i / Q, q = i % Q;
       const int rw = r / kRowsPerWave, rl = r % kRowsPerWave;
       float M = -INFINITY;
@@ -612,17 +626,21 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D>& sm, const Se
   }
 }
 
-template <int D, int KV, bool kDirect>
-__global__ __launch_bounds__(kThreads, 1) void tree_attn_quant_kernel(QuantArgs a) {
-  __shared__ Smem<D> sm;
+template <int D, int KV, int W, bool kDirect>
+__global__ __launch_bounds__(W * SRT_WAVE, 2) void tree_attn_quant_kernel(QuantArgs a) {
+  __shared__ Smem<D, W> sm;
   auto run_item = [&](int b, int g, int s, int rb) {
     const SeqInfo si = seq_info(a, b);
     const int here = si.n * a.G - rb * kRowsPerBlock;
     if (here <= 0 || s * a.chunk >= si.total) return;
-    if (here <= 32) attend<D, KV, 1>(a, sm, si, b, g, s, rb);
-    else if (here <= 64) attend<D, KV, 2>(a, sm, si, b, g, s, rb);
-    else if (here <= 128) attend<D, KV, 4>(a, sm, si, b, g, s, rb);
-    else attend<D, KV, 8>(a, sm, si, b, g, s, rb);
+    if constexpr (W < kWaves) {
+      attend<D, KV, 1, W>(a, sm, si, b, g, s, rb);
+    } else {
+      if (here <= 32) attend<D, KV, 1, W>(a, sm, si, b, g, s, rb);
+      else if (here <= 64) attend<D, KV, 2, W>(a, sm, si, b, g, s, rb);
+      else if (here <= 128) attend<D, KV, 4, W>(a, sm, si, b, g, s, rb);
+      else attend<D, KV, 8, W>(a, sm, si, b, g, s, rb);
+    }
   };
   if constexpr (kDirect) {  // a workgroup for every item there can be
     const int x = blockIdx.x / a.RB, y = x / a.S;
@@ -644,9 +662,12 @@ __global__ __launch_bounds__(kThreads, 1) void tree_attn_quant_kernel(QuantArgs 
 }
 
 template <int D, int KV>
-void launch_quant(const QuantArgs& a, bool direct, unsigned grid, hipStream_t s) {
-  if (direct) tree_attn_quant_kernel<D, KV, true><<<grid, kThreads, 0, s>>>(a);
-  else tree_attn_quant_kernel<D, KV, false><<<grid, kThreads, 0, s>>>(a);
+void launch_quant(const QuantArgs& a, bool narrow, bool direct, unsigned grid, hipStream_t s) {
+  constexpr int N = kNarrowWaves;
+  if (narrow && direct) tree_attn_quant_kernel<D, KV, N, true><<<grid, N * SRT_WAVE, 0, s>>>(a);
+  else if (narrow) tree_attn_quant_kernel<D, KV, N, false><<<grid, N * SRT_WAVE, 0, s>>>(a);
+  else if (direct) tree_attn_quant_kernel<D, KV, kWaves, true><<<grid, kThreads, 0, s>>>(a);
+  else tree_attn_quant_kernel<D, KV, kWaves, false><<<grid, kThreads, 0, s>>>(a);
 }
 
 // Positions that the context and a tree of N nodes may take.
@@ -661,7 +682,7 @@ extern "C" size_t srt_tree_attn_quant_scratch_bytes(const srt_kv_quant* kv, int3
   const int64_t cap = key_cap(*kv, N);
   if (!packs(B, N, Hq, kv->Hkv, cap, true)) return 0;
   const int64_t RB = (N * (Hq / kv->Hkv) + kRowsPerBlock - 1) / kRowsPerBlock;
-  return scratch_for(B, N, Hq, kv->Hkv, kv->d, cap, chunk_for(B, kv->Hkv, RB, cap, true, true));
+  return scratch_for(B, N, Hq, kv->Hkv, kv->d, cap, chunk_for(B, kv->Hkv, RB, cap, true, N * (Hq / kv->Hkv)), true);
 }
 
 extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N, int32_t Hq, const uint16_t* q,
@@ -712,17 +733,20 @@ extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N,
 
   const int cus = cu_count();
   if (cus <= 0) return SRT_ERR_HIP;
-  const unsigned grid = static_cast<unsigned>(std::min<int64_t>(a.total, cus));
+  const bool narrow = a.total > cus && static_cast<int64_t>(N) * a.G <= kNarrowRows;
+  const int places = narrow ? cus * (kWaves / kNarrowWaves) : cus;  // workgroups that run at once
   hipStream_t s = as_stream(stream);
-  const bool direct = a.total <= cus;  // every item has a CU: nothing to order or hand out
+  // Every item runs at once, or all are short: nothing to order or hand out.
+  const bool direct = a.total <= places || (narrow && a.S == 1 && cap * 2 * kv->d <= kUnlisted);
+  const unsigned grid = static_cast<unsigned>(direct ? a.total : std::min<int64_t>(a.total, places));
   if (!direct) tree_attn_plan_kernel<<<1, 1024, 0, s>>>(a);
   const bool e4m3 = kv->kv_type == SRT_KV_E4M3;
   if (kv->d == 128) {
-    if (e4m3) launch_quant<128, SRT_KV_E4M3>(a, direct, grid, s);
-    else launch_quant<128, SRT_KV_INT8>(a, direct, grid, s);
+    if (e4m3) launch_quant<128, SRT_KV_E4M3>(a, narrow, direct, grid, s);
+    else launch_quant<128, SRT_KV_INT8>(a, narrow, direct, grid, s);
   } else {
-    if (e4m3) launch_quant<64, SRT_KV_E4M3>(a, direct, grid, s);
-    else launch_quant<64, SRT_KV_INT8>(a, direct, grid, s);
+    if (e4m3) launch_quant<64, SRT_KV_E4M3>(a, narrow, direct, grid, s);
+    else launch_quant<64, SRT_KV_INT8>(a, narrow, direct, grid, s);
   }
   if (a.S > 1) launch_combine(a, kv->d, direct, static_cast<unsigned>(combine_grid(a, cus)), s);
   return launch_status();

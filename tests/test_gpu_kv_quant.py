@@ -241,6 +241,32 @@ def test_attention_large_splits():
 
 
 @pytest.mark.parametrize("kv", ["e4m3", "int8"])
+@pytest.mark.parametrize("B,N,hq,hkv,d,page,longest", [
+    (70, 4, 28, 4, 128, 16, 300),   # 28 rows, short table
+    (40, 32, 8, 8, 64, 32, 700),    # 32 rows, as many nodes
+    (261, 1, 32, 1, 64, 128, 900),  # 32 heads of one node
+    (300, 2, 10, 2, 128, 16, 2400),  # a longer table
+    (290, 3, 8, 8, 64, 64, 40),     # 2320 (sequence, KV head) pairs, few keys
+])
+def test_attention_large_batches_of_narrow_trees(kv, B, N, hq, hkv, d, page, longest):
+    """Up to 32 query rows per KV head in more items than the GPU has CUs."""
+    rng = np.random.default_rng(16)
+    ctx = np.where(np.arange(B) % 7 == 0, np.arange(B) % 40, rng.integers(0, longest, B))
+    c = AttnCase(16, B, N, hq, hkv, d, ctx, kv, page)
+    print(f"tolerance used: {c.check(c.run()):.3f}", flush=True)
+
+
+def test_attention_of_narrow_trees_takes_a_smaller_scratch():
+    """8192-key splits where the scratch has no room for the partial results of 4096-key ones."""
+    base = [8192 - 64 - 7, 8192, 9000, 12345, 16354, 100, 5000, 8193, 4096, 0]
+    c = AttnCase(17, 40, 4, 8, 8, 128, [base[i % 10] for i in range(40)])
+    need = srt.srt_tree_attn_quant_scratch_bytes(c.cache, c.N, c.hq)
+    for size in (need, need * 6 // 10):
+        out = c.run(scratch=torch.empty(size, dtype=torch.uint8, device="cuda"))
+        c.check(out, seqs=range(0, 40, 3), what=f"scratch of {size}")
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "int8"])
 def test_attention_peaked(kv):
     """Scores of large magnitude: the reference is raised again and again."""
     c = AttnCase(6, 4, 16, 7, 1, 128, [300, 1500, 40, 2100], kv, qk=3.0)
