@@ -49,8 +49,6 @@ struct AttnBase {
   int32_t chunk;  // keys per split: a power of two in [kSmallChunk, kChunk]
 };
 
-constexpr int kNarrowRows = 32;  // of the trees that the 8-bit cache's kernel takes with half the waves
-
 // Work list: plan[0] = number of items, plan[1] = next item to hand out,
 // then item i at plan[kPlanHeader + 2 i] = sequence, [.. + 1] = KV head |
 // split << 8 | row block << 20.  Items are ordered by decreasing cost
@@ -299,6 +297,19 @@ __global__ __launch_bounds__(kCombineRows * D / 4) void tree_attn_combine_kernel
   }
 }
 
+// Whether the 8-bit cache's kernel takes a batch with half the waves a workgroup, two
+// workgroups to a CU: up to 32 rows (one wave's) always, up to kNarrowRows where there are
+// many (sequence, KV head) pairs, as an item takes twice as long then.  28 heads, 4 KV
+// heads unless said: 512 sequences of 1000 to 8000 keys, 16 nodes: 215 -> 182 us, 256 of
+// 100 to 500: 58 -> 37, of 200 to 2000: 65 -> 69; 1024 of 500 to 4000, 12 heads, 2 KV
+// heads: 151 -> 112; 64 of 4k to 16k: 101 -> 138, with 8 nodes 90 -> 101.  Up to 32 rows
+// it loses only where a few long contexts of many decide (32 sequences, median 1000, up
+// to 8000, 4 nodes: 32 -> 35; 256 of 2 KV heads of 64: 40 -> 47), which the host cannot see.
+constexpr int kNarrowRows = 128;
+inline bool half_waves(int64_t pairs, int64_t rows) {
+  return rows > 0 && (rows <= 32 || (rows <= kNarrowRows && pairs >= 1024));
+}
+
 // Keys per split: the largest power of two in [kMinChunk, kChunk] that still
 // gives B * Hkv * RB * (capacity / chunk) >= 512 work items (two per CU of
 // the 256; RB row blocks per sequence and KV head), so that small batches
@@ -326,12 +337,12 @@ __global__ __launch_bounds__(kCombineRows * D / 4) void tree_attn_combine_kernel
 // take 8192: 64 sequences of 4k to 16k, 28 heads, 4 KV heads, trees of up to 8 / 16 /
 // 32 / 64 nodes: 114 -> 90, 227 -> 137, 242 -> 144, 248 -> 215 us; not from 512 pairs
 // (128 such sequences: 355 and 386 us), nor for wider trees, whose partial results cost
-// more (8 of 256 nodes: 530 and 558).  Trees of up to kNarrowRows rows always do, as two
+// more (8 of 256 nodes: 530 and 558).  With half the waves a workgroup they always do, as two
 // of their workgroups share a CU's rate (28 heads, 4 KV heads, single tokens or 4 nodes:
 // 300 sequences of 300 to 32k keys 109 -> 85 us, 256 of 2k to 8k 116 -> 114; at most 3%
 // the other way, 256 of 16k to 32k: 957 -> 988; with 2048 keys 93, 120 and 1061).
 int chunk_for(int32_t B, int32_t Hkv, int64_t RB, int64_t cap, bool small, int64_t rows) {
-  int chunk = rows > 0 && rows <= kNarrowRows ? kChunk / 2 : kChunk;
+  int chunk = half_waves(static_cast<int64_t>(B) * Hkv, rows) ? kChunk / 2 : kChunk;
   auto items = [&](int c) { return static_cast<int64_t>(B) * Hkv * RB * ((cap + c - 1) / c); };
   while (chunk > kMinChunk && items(chunk) < 512) chunk /= 2;
   if (rows > 0 && chunk == kChunk && RB <= 2 && static_cast<int64_t>(B) * Hkv < 512) chunk /= 2;

@@ -50,13 +50,11 @@ struct QuantArgs : AttnBase {
 };
 
 constexpr int kGroup = 16;  // keys that share their scales (a page has at least as many)
-// Trees of up to kNarrowRows rows: workgroups of this many waves, two to a CU, so that
-// one streams while the other claims, fills, drains and merges (28 heads, 4 KV heads,
-// single tokens: 256 sequences of 200 to 2000 keys 52 -> 36 us, 512 of 2k to 10k 237 ->
-// 217; with workgroups of two waves, four to a CU, 50 and 234).  A batch that has an
-// item for every CU at most keeps 8 waves (4 sequences: 10.2 and 11.1), and so would one
-// whose keys lie in few long sequences, which the host does not see (16 sequences of
-// 4000 to 30000 keys, 32 heads, 8 KV heads: 54 -> 62).
+// Narrow trees (half_waves): workgroups of this many waves, two to a CU, so that one
+// streams while the other claims, fills, drains and merges (28 heads, 4 KV heads, single
+// tokens: 256 sequences of 200 to 2000 keys 52 -> 36 us, 512 of 2k to 10k 237 -> 217;
+// with workgroups of two waves, four to a CU, 50 and 234).  A batch that has an item for
+// every CU at most keeps 8 waves (4 sequences: 10.2 and 11.1).
 constexpr int kNarrowWaves = 4;
 // Bytes of a bf16 row times keys of the table, up to which a narrow batch has a
 // workgroup launched for every item: no list, no claims (185 sequences of 60 keys, 8 KV
@@ -66,17 +64,19 @@ constexpr int kNarrowWaves = 4;
 constexpr int64_t kUnlisted = 1536 * 2 * 128;
 constexpr float kLeastScale = 0x1p-70f, kMostScale = 0x1p100f;
 
-template <int D, int W>
+// Of a workgroup of W waves for trees of up to R rows (of a block, where W is 8).
+template <int D, int W, int R>
 struct Smem {
   using Sh = Shape<D>;
   static constexpr int kRow = Sh::KSTRIDE + Sh::VSTRIDE;
-  static constexpr int kNodes = W == kWaves ? kMaxN : kNarrowRows;
+  static constexpr int kNodes = W == kWaves ? kMaxN : R;
+  static constexpr int kKeys = W == kWaves || R <= 32 ? kChunk : kChunk / 2;  // of a split
   __attribute__((aligned(16))) uint8_t pool[32 * W * kRow];  // tiles, then the key groups' partial results
   uint64_t anc[kNodes][4];
   int32_t spar[kNodes];
-  __attribute__((aligned(16))) float kc[kChunk / kGroup];  // scale * log2(e) * sk of the split's key groups
-  __attribute__((aligned(16))) float lv[kChunk / kGroup];  // log2(sv)
-  __attribute__((aligned(16))) float rv[kChunk / kGroup];  // 1 / sv
+  __attribute__((aligned(16))) float kc[kKeys / kGroup];  // scale * log2(e) * sk of the split's key groups
+  __attribute__((aligned(16))) float lv[kKeys / kGroup];  // log2(sv)
+  __attribute__((aligned(16))) float rv[kKeys / kGroup];  // 1 / sv
   float m[W][kRowsPerWave], l[W][kRowsPerWave];
 };
 
@@ -107,8 +107,9 @@ __device__ inline uint2 widen(uint32_t w) {
 
 // One work item: rows rb * 256 .. of (sequence b, KV head g) against the keys of
 // split s, with W waves, WR of them along the rows.
-template <int D, int KV, int WR, int W>
-__device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W>& sm, const SeqInfo si, int b, int g, int s, int rb) {
+template <int D, int KV, int WR, int W, int R>
+__device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W, R>& sm, const SeqInfo si, int b, int g, int s,
+                                       int rb) {
   using Sh = Shape<D>;
   constexpr int WK = W / WR;                  // groups of waves along the keys
   constexpr int T = WR == 8 ? 64 : 32;        // keys per tile
@@ -119,7 +120,8 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W>& sm, const
   constexpr int UPT = KPW / U;
   constexpr int LPU = U / 8;                  // loads per unit: 8 rows each, 8 lanes a row
   constexpr int EPL = D / 8;                  // codes per lane and load
-  constexpr int NPG = kChunk / W / U / SRT_WAVE;  // registers of page ids
+  constexpr int kKeys = Smem<D, W, R>::kKeys;
+  constexpr int NPG = kKeys / W / U / SRT_WAVE;  // registers of page ids
   constexpr int kTileBytes = T * (Sh::KSTRIDE + Sh::VSTRIDE);
   // Few rows: the pages are read once, by this workgroup alone, and need no
   // place in the caches (256 sequences of one node, 28 heads: 260 us with
@@ -127,7 +129,7 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W>& sm, const
   // trees' pages again: 531 and 543).
   constexpr int kAux = WR == 8 ? 0 : 2;
   static_assert(NB * WK * T <= 32 * W, "tiles fit the pool");
-  static_assert(NPG * SRT_WAVE * U * W == kChunk && NPG >= 1, "page ids of a split");
+  static_assert(NPG * SRT_WAVE * U * W == kKeys && NPG >= 1 && NPG <= 2, "page ids of a split");
 
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE);
@@ -626,20 +628,20 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W>& sm, const
   }
 }
 
-template <int D, int KV, int W, bool kDirect>
+template <int D, int KV, int W, int R, bool kDirect>
 __global__ __launch_bounds__(W * SRT_WAVE, 2) void tree_attn_quant_kernel(QuantArgs a) {
-  __shared__ Smem<D, W> sm;
+  __shared__ Smem<D, W, R> sm;
   auto run_item = [&](int b, int g, int s, int rb) {
     const SeqInfo si = seq_info(a, b);
     const int here = si.n * a.G - rb * kRowsPerBlock;
     if (here <= 0 || s * a.chunk >= si.total) return;
-    if constexpr (W < kWaves) {
+    if constexpr (R == 32) {
       attend<D, KV, 1, W>(a, sm, si, b, g, s, rb);
     } else {
       if (here <= 32) attend<D, KV, 1, W>(a, sm, si, b, g, s, rb);
       else if (here <= 64) attend<D, KV, 2, W>(a, sm, si, b, g, s, rb);
-      else if (here <= 128) attend<D, KV, 4, W>(a, sm, si, b, g, s, rb);
-      else attend<D, KV, 8, W>(a, sm, si, b, g, s, rb);
+      else if (R == 128 || here <= 128) attend<D, KV, 4, W>(a, sm, si, b, g, s, rb);
+      else if constexpr (R > 128) attend<D, KV, 8, W>(a, sm, si, b, g, s, rb);
     }
   };
   if constexpr (kDirect) {  // a workgroup for every item there can be
@@ -661,13 +663,17 @@ __global__ __launch_bounds__(W * SRT_WAVE, 2) void tree_attn_quant_kernel(QuantA
   }
 }
 
+template <int D, int KV, int W, int R>
+void launch_waves(const QuantArgs& a, bool direct, unsigned grid, hipStream_t s) {
+  if (direct) tree_attn_quant_kernel<D, KV, W, R, true><<<grid, W * SRT_WAVE, 0, s>>>(a);
+  else tree_attn_quant_kernel<D, KV, W, R, false><<<grid, W * SRT_WAVE, 0, s>>>(a);
+}
+
 template <int D, int KV>
 void launch_quant(const QuantArgs& a, bool narrow, bool direct, unsigned grid, hipStream_t s) {
-  constexpr int N = kNarrowWaves;
-  if (narrow && direct) tree_attn_quant_kernel<D, KV, N, true><<<grid, N * SRT_WAVE, 0, s>>>(a);
-  else if (narrow) tree_attn_quant_kernel<D, KV, N, false><<<grid, N * SRT_WAVE, 0, s>>>(a);
-  else if (direct) tree_attn_quant_kernel<D, KV, kWaves, true><<<grid, kThreads, 0, s>>>(a);
-  else tree_attn_quant_kernel<D, KV, kWaves, false><<<grid, kThreads, 0, s>>>(a);
+  if (!narrow) launch_waves<D, KV, kWaves, kRowsPerBlock>(a, direct, grid, s);
+  else if (a.part_rows <= 32) launch_waves<D, KV, kNarrowWaves, 32>(a, direct, grid, s);
+  else launch_waves<D, KV, kNarrowWaves, kNarrowRows>(a, direct, grid, s);
 }
 
 // Positions that the context and a tree of N nodes may take.
@@ -733,7 +739,9 @@ extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N,
 
   const int cus = cu_count();
   if (cus <= 0) return SRT_ERR_HIP;
-  const bool narrow = a.total > cus && static_cast<int64_t>(N) * a.G <= kNarrowRows;
+  const int64_t rows = a.part_rows;
+  const bool narrow = a.total > cus && half_waves(static_cast<int64_t>(B) * kv->Hkv, rows) &&
+                      (rows <= 32 || a.chunk <= kChunk / 2);
   const int places = narrow ? cus * (kWaves / kNarrowWaves) : cus;  // workgroups that run at once
   hipStream_t s = as_stream(stream);
   // Every item runs at once, or all are short: nothing to order or hand out.

@@ -267,6 +267,24 @@ def test_attention_of_narrow_trees_takes_a_smaller_scratch():
 
 
 @pytest.mark.parametrize("kv", ["e4m3", "int8"])
+@pytest.mark.parametrize("B,N,hq,hkv,d,page,longest", [
+    (260, 16, 28, 4, 128, 16, 300),   # up to 112 rows, short table
+    (132, 128, 8, 8, 64, 32, 200),    # up to 128, as many nodes
+    (520, 9, 10, 2, 128, 64, 2000),   # up to 45, a longer table
+    (130, 8, 64, 8, 64, 16, 4500),    # up to 64, two splits
+])
+def test_attention_many_pairs_of_medium_trees(kv, B, N, hq, hkv, d, page, longest):
+    """33 to 128 query rows per KV head, 1024 (sequence, KV head) pairs and more."""
+    rng = np.random.default_rng(18)
+    ctx = np.where(np.arange(B) % 7 == 0, np.arange(B) % 40, rng.integers(0, longest, B))
+    c = AttnCase(18, B, N, hq, hkv, d, ctx, kv, page)
+    print(f"tolerance used: {c.check(c.run(), seqs=range(0, B, 5)):.3f}", flush=True)
+    need = srt.srt_tree_attn_quant_scratch_bytes(c.cache, c.N, c.hq)
+    out = c.run(scratch=torch.empty(need * 6 // 10, dtype=torch.uint8, device="cuda"))  # larger splits, where it serves
+    c.check(out, seqs=range(0, B, 11), what="smaller scratch")
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "int8"])
 def test_attention_peaked(kv):
     """Scores of large magnitude: the reference is raised again and again."""
     c = AttnCase(6, 4, 16, 7, 1, 128, [300, 1500, 40, 2100], kv, qk=3.0)
