@@ -202,6 +202,22 @@ __device__ inline void advance_draft(int32_t* row, int Qmax, int32_t* draft_len,
 }
 
 // ---------------------------------------------------------------------------
+// fp32 operations that are rounded one by one
+// ---------------------------------------------------------------------------
+// A product is not contracted with the sum that takes it.  (The device headers'
+// __fmul_rn, __fadd_rn and __fsub_rn are the plain operators, which the compiler
+// makes one fused operation of by default; the result then lacks a rounding.)
+__device__ inline float mul_rounded(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
+__device__ inline float add_rounded(float a, float b) {
+#pragma clang fp contract(off)
+  return a + b;
+}
+
+// ---------------------------------------------------------------------------
 // Wave helpers
 // ---------------------------------------------------------------------------
 __device__ inline int lane_id() { return __lane_id(); }

@@ -72,14 +72,14 @@ __device__ inline void stand_on(const RulesArgs& a, Row& w, int b, int u) {
 
 // The penalised logit; every operation rounded by itself.
 __device__ inline float penalised(const Row& w, float y, bool prompt, int count) {
-  if (prompt || count > 0) y = y > 0.f ? __fdiv_rn(y, w.r) : __fmul_rn(y, w.r);
-  y = __fsub_rn(y, __fmul_rn(w.f, static_cast<float>(count)));
-  return count > 0 ? __fsub_rn(y, w.p) : y;
+  if (prompt || count > 0) y = y > 0.f ? __fdiv_rn(y, w.r) : mul_rounded(y, w.r);
+  y = add_rounded(y, -mul_rounded(w.f, static_cast<float>(count)));
+  return count > 0 ? add_rounded(y, -w.p) : y;
 }
 
 template <bool kNoise>
 __device__ inline float noisy(const Row& w, float y, float g) {
-  return kNoise ? __fadd_rn(__fmul_rn(y, w.invT), g) : y;
+  return kNoise ? add_rounded(mul_rounded(y, w.invT), g) : y;
 }
 
 // The best so far in ascending order of the index: a NaN or -inf is never taken.
@@ -141,7 +141,7 @@ __device__ inline void special(const RulesArgs& a, const Row& w, const Path& pat
   for (int i = 0; i < n; ++i) count += path.tok[i] == t;
   float y = penalised(w, l, word & kPrompt, count);
   if (from >= 0)
-    for (int i = from; i < w.bias1 && a.bias_tokens[i] == t; ++i) y = __fadd_rn(y, a.bias_values[i]);
+    for (int i = from; i < w.bias1 && a.bias_tokens[i] == t; ++i) y = add_rounded(y, a.bias_values[i]);
   const float x = noisy<kNoise>(w, y, g);
   if ((allowed & 1u) && x > -INFINITY) key = max(key, pack_key(x, t));
 }
