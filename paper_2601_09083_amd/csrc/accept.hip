@@ -54,7 +54,7 @@ __device__ inline void take(Best& b, float v, int i) {
 }
 
 __device__ inline float score(float l, float g, float invT, bool noisy) {
-  return noisy ? __fadd_rn(__fmul_rn(l, invT), g) : l;
+  return noisy ? add_rounded(mul_rounded(l, invT), g) : l;
 }
 
 // This thread's share of the arg-max of x_j over j in [lo, hi) of one row (lo a

@@ -25,3 +25,10 @@ def test_walk_under_rules(V, sampled):
                       **bias_lists([dict(x) for x in c.bias]))
     c.check(srt.srt_accept_rules(dev(c.logits), dev(c.gumbel), float(c.invT), rules, dev(c.tok), dev(c.par),
                                  dev(c.n, torch.int32), c.dmax))
+
+
+@pytest.mark.parametrize("V", ROWS)
+def test_plain_walk(V):
+    c = Planted(V + 2, 48, V, ("noise",), True)
+    c.check(srt.srt_accept(dev(c.logits), dev(c.gumbel), float(c.invT), dev(c.tok), dev(c.par), dev(c.n, torch.int32),
+                           c.dmax))
