@@ -611,7 +611,7 @@ __device__ inline void head_tile(const HeadArgs& a, Shared& s, int v0, int v_end
           for (int e = 0; e < 4; ++e) {
             if (vb + e < v_end) {
               float sc = acc[x][y][4 * q + e];
-              if (kNoise) sc = __fadd_rn(__fmul_rn(sc, a.invT), gv[e]);
+              if (kNoise) sc = add_rounded(mul_rounded(sc, a.invT), gv[e]);
               take(bv, bi, sc, vb + e);
             }
           }

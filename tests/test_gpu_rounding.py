@@ -32,3 +32,16 @@ def test_plain_walk(V):
     c = Planted(V + 2, 48, V, ("noise",), True)
     c.check(srt.srt_accept(dev(c.logits), dev(c.gumbel), float(c.invT), dev(c.tok), dev(c.par), dev(c.n, torch.int32),
                            c.dmax))
+
+
+@pytest.mark.parametrize("B", [48, 160])
+@pytest.mark.parametrize("V", [1003, 70003])
+def test_walk_with_the_head(V, B):
+    """One hidden value that is not zero: a node's logits are a column of the head, exactly."""
+    c = Planted(V + B, B, V, ("noise",), True, bf16=True)
+    hidden = torch.eye(2 * B, device="cuda").to(torch.bfloat16).view(B, 2, 2 * B)
+    head = dev(c.logits.reshape(2 * B, V)).t().to(torch.bfloat16)
+    d = (2 * B + 63) // 64 * 64
+    pad = lambda x: torch.nn.functional.pad(x, (0, d - 2 * B)).contiguous()
+    c.check(srt.srt_accept_lmhead(pad(hidden), pad(head), dev(c.gumbel), float(c.invT), dev(c.tok), dev(c.par),
+                                  dev(c.n, torch.int32), c.dmax))
