@@ -265,6 +265,15 @@ def _walk_outputs(B: int, max_depth: int, dev) -> dict:
             "n_emitted": torch.empty(B, dtype=torch.int32, device=dev)}
 
 
+def _check_walk_outputs(out, B: int, max_depth: int):
+    """The outputs of a walk are of its sizes (the kernels write all of them)."""
+    for name in ("n_accepted", "out_tokens", "out_nodes", "n_emitted"):
+        shape = (B, max_depth + 1) if name.startswith("out") else (B,)
+        t = out.get(name) if name == "n_emitted" else out[name]  # (that one is optional)
+        if t is not None and t.shape != shape:
+            raise ValueError(f"out: {name} must be {list(shape)}")
+
+
 def srt_accept_scratch_bytes(B: int) -> int:
     return int(lib().srt_accept_scratch_bytes(B))
 
@@ -589,11 +598,14 @@ def srt_accept_rules(logits, gumbel, inv_temperature: float, rules: Rules, tree_
         raise ValueError("tree arrays must be [B, N], n_nodes [B]")
     dev, f32, i32 = logits.device, torch.float32, torch.int32
     rules.check(B, N, V, dev)
+    if out is not None:
+        _check_walk_outputs(out, B, max_depth)
     if out is None or scratch is None or scratch.numel() * scratch.element_size() < srt_accept_scratch_bytes(B):
         with _device(dev), _on(stream):
             if out is None:
                 out = _walk_outputs(B, max_depth, dev)
-            scratch = torch.empty(max(srt_accept_scratch_bytes(B), 1), dtype=torch.uint8, device=dev)
+            if scratch is None or scratch.numel() * scratch.element_size() < srt_accept_scratch_bytes(B):
+                scratch = torch.empty(max(srt_accept_scratch_bytes(B), 1), dtype=torch.uint8, device=dev)
     if scratch.device != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be a contiguous tensor on {dev}")
     _check("srt_accept_rules", _on_device(
