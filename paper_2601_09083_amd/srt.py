@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 from typing import Optional
 
@@ -267,11 +268,24 @@ def _walk_outputs(B: int, max_depth: int, dev) -> dict:
 
 def _check_walk_outputs(out, B: int, max_depth: int):
     """The outputs of a walk are of its sizes (the kernels write all of them)."""
-    for name in ("n_accepted", "out_tokens", "out_nodes", "n_emitted"):
-        shape = (B, max_depth + 1) if name.startswith("out") else (B,)
-        t = out.get(name) if name == "n_emitted" else out[name]  # (that one is optional)
-        if t is not None and t.shape != shape:
+    for name, t, shape in _outputs_with_shapes(out, B, max_depth):
+        if t.shape != shape:
             raise ValueError(f"out: {name} must be {list(shape)}")
+
+
+def _check_walk_room(out, B: int, max_depth: int):
+    """The outputs of a walk have room for what the kernels write."""
+    for name, t, shape in _outputs_with_shapes(out, B, max_depth):
+        if t.numel() < math.prod(shape):
+            raise ValueError(f"out: {name} must be {list(shape)}")
+
+
+def _outputs_with_shapes(out, B: int, max_depth: int):
+    rows, table = (B,), (B, max_depth + 1)
+    for name, shape in (("n_accepted", rows), ("out_tokens", table), ("out_nodes", table), ("n_emitted", rows)):
+        t = out.get(name) if name == "n_emitted" else out[name]  # (that one is optional)
+        if t is not None:
+            yield name, t, shape
 
 
 def srt_accept_scratch_bytes(B: int) -> int:
@@ -285,6 +299,8 @@ def srt_accept(logits, gumbel, inv_temperature: float, tree_tokens, tree_parent,
     if gumbel is not None and tuple(gumbel.shape) != (B, max_depth + 1, V):
         raise ValueError("gumbel must be [B, max_depth+1, V]")
     dev = logits.device
+    if out is not None:
+        _check_walk_room(out, B, max_depth)
     need = srt_accept_scratch_bytes(B)
     with _on(stream):
         if out is None:
@@ -309,6 +325,7 @@ def srt_accept_noalloc(logits, gumbel, inv_temperature: float, tree_tokens, tree
     B, N, V = logits.shape
     if gumbel is not None and tuple(gumbel.shape) != (B, max_depth + 1, V):
         raise ValueError("gumbel must be [B, max_depth+1, V]")
+    _check_walk_room(out, B, max_depth)
     _check("srt_accept_noalloc", lib().srt_accept_noalloc(
         B, N, V, max_depth, _ptr(logits, torch.float32, "logits"), _ptr(gumbel, torch.float32, "gumbel"),
         float(inv_temperature), _ptr(tree_tokens, torch.int32, "tree_tokens"),
@@ -336,7 +353,9 @@ def srt_accept_lmhead(hidden, w_head, gumbel, inv_temperature: float, tree_token
         raise ValueError("tree arrays must be [B, N]")
     dev = hidden.device
     need = srt_accept_lmhead_scratch_bytes(B, N, V)
-    if out is None:
+    if out is not None:
+        _check_walk_room(out, B, max_depth)
+    else:
         with _on(stream):
             out = _walk_outputs(B, max_depth, dev)
     args = (B, N, dm, V, max_depth, _ptr(hidden, torch.bfloat16, "hidden"), _ptr(w_head, torch.bfloat16, "w_head"),

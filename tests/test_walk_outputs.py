@@ -29,6 +29,24 @@ def test_rules_walk_refuses_outputs_of_other_sizes(bad):
         S.srt_accept_rules(logits, None, 1.0, S.Rules(), tok, par, n, D, out=outputs(**bad))
 
 
+SMALL = [dict(out_tokens=(B, D)), dict(out_nodes=(B - 1, D + 1)), dict(n_accepted=(B - 1,)), dict(n_emitted=(1,))]
+
+
+@pytest.mark.parametrize("small", SMALL)
+@pytest.mark.parametrize("walk", ["accept", "noalloc", "lmhead"])
+def test_walks_refuse_outputs_without_room(walk, small):
+    logits, tok, par, n = arguments()
+    out = outputs(**small)
+    with pytest.raises(ValueError, match=f"out: {list(small)[0]}"):
+        if walk == "accept":
+            S.srt_accept(logits, None, 1.0, tok, par, n, D, out=out)
+        elif walk == "noalloc":
+            S.srt_accept_noalloc(logits, None, 1.0, tok, par, n, D, out)
+        else:
+            bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+            S.srt_accept_lmhead(bf(B, N, 64), bf(V, 64), None, 1.0, tok, par, n, D, out=out)
+
+
 @pytest.mark.gpu
 def test_rules_walk_keeps_the_scratch_it_is_given():
     """Without ``out`` too: a walk by levels leaves its lists in it."""
