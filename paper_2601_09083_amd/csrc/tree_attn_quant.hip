@@ -89,6 +89,12 @@ __device__ constexpr int chunk_at(int c) {
   return D == 128 ? (c < 8 ? 2 * c : 2 * (c - 8) + 1) : c;
 }
 
+// LDS accesses of a wave's lanes before this come before those after it.
+__device__ inline void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Four codes as two words of two bf16 (exact: e4m3 has 4 significant bits, int8 7).
 template <int KV>
 __device__ inline uint2 widen(uint32_t w) {
@@ -502,18 +508,24 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W, R>& sm, co
   constexpr int kBuffer = WK * kTileBytes;
   if constexpr (WR == 1) {
     // A wave's tiles are its own: the LDS keeps a wave's stores and loads in
-    // order, so one buffer serves and no wave waits for another.
+    // order, so one buffer serves and no wave waits for another.  The compiler
+    // knows of one lane's addresses only: its fences keep the order of stores and
+    // reads between the lanes (no instruction comes of them).
     const int iters = n1 > kg ? (n1 - kg + WK - 1) / WK : 0;
     if (iters > 0) load_pages(0);
     __syncthreads();  // the scales (and the bitsets)
     for (int it = 0; it < iters; ++it) {
       store_pages(mine);
+      wave_lds_fence();
       if (it + 1 < iters) load_pages(it + 1);
       compute(std::false_type(), k_begin + (it * WK + kg) * T, mine);
+      wave_lds_fence();
     }
     for (int it = kg; it < n2; it += WK) {
       stage_open(o_begin + it * T, mine);
+      wave_lds_fence();
       compute(std::true_type(), o_begin + it * T, mine);
+      wave_lds_fence();
     }
   } else {
     // One barrier a tile: tile t + 1 is stored into the buffers that tile t - 1 left.
