@@ -340,7 +340,9 @@ int srt_accept_lmhead(int32_t B, int32_t N, int32_t d_model, int32_t V, int32_t 
  * token): ctx_tail[b] (right-aligned last max_match committed tokens, -1
  * padded, as srt_draft reads it) becomes the last max_match tokens of the
  * grown sequence and draft_len[b] += k + 1.  The bonus token is the next
- * pass's root; its vectors are the caller's to write at the new L.
+ * pass's root; its vectors are the caller's to write at the new L.  A walk that
+ * ended without a bonus token (out_tokens[b, k] < 0, srt_accept_rules) has
+ * emitted k tokens, and the draft inputs advance by those.
  * Layouts: k_cache, v_cache [num_pages, Hkv, page, d] bf16 bits, 16-byte
  * aligned, updated in place; block_table [B, max_pages] int32; ctx_len,
  * n_accepted, draft_len [B] int32; out_tokens, out_nodes [B, Dmax+1]

@@ -9,7 +9,8 @@
 // c_1 < ... < c_k, position L + j receives the vectors of L + c_j, the
 // cached length becomes L + k + 1 and the bonus token (whose vectors the
 // next pass computes, as its root) ends the committed sequence.  The draft
-// tail and committed count advance by the k + 1 emitted tokens.
+// tail and committed count advance by the emitted tokens: the k accepted ones
+// and the bonus token, if the walk has one.
 //
 // GPU design: one workgroup per sequence.  The rows to move (accepted node
 // j's K and V vectors of every KV head, d * 2 bytes each) are split into
@@ -99,12 +100,11 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
     __syncthreads();
   }
 
-  const int e = k + 1;
   if (a.ctx_tail && tid < SRT_WAVE)
     advance_draft(a.ctx_tail + static_cast<int64_t>(b) * a.Qmax, a.Qmax, a.draft_len + b,
-                  a.out_tokens + static_cast<int64_t>(b) * (a.Dmax + 1), e);
+                  a.out_tokens + static_cast<int64_t>(b) * (a.Dmax + 1), k);
   __syncthreads();  // every thread has read ctx_len[b]
-  if (tid == 0) a.ctx_len[b] = static_cast<int32_t>(L + e);
+  if (tid == 0) a.ctx_len[b] = static_cast<int32_t>(L + k + 1);
 }
 
 }  // namespace

@@ -184,10 +184,12 @@ __device__ inline uint32_t trie_find_or_create(const TrieView& t, uint64_t key, 
 // ---------------------------------------------------------------------------
 // Draft inputs
 // ---------------------------------------------------------------------------
-// Draft tail of one sequence, at most 64 tokens: shift left by the e emitted
-// tokens and append them.  One wave, whose lanes all read before any writes.
-__device__ inline void advance_draft(int32_t* row, int Qmax, int32_t* draft_len, const int32_t* emitted, int e) {
+// Draft tail of one sequence, at most 64 tokens: shift left by the emitted
+// tokens, k accepted ones and the bonus token (none where the walk ended without
+// one, -1), and append them.  One wave, whose lanes all read before any writes.
+__device__ inline void advance_draft(int32_t* row, int Qmax, int32_t* draft_len, const int32_t* emitted, int k) {
   const int64_t t = *draft_len;
+  const int e = k + (emitted[k] >= 0);
   int32_t nv = -1;
   const int i = threadIdx.x % SRT_WAVE;
   if (i < Qmax) {

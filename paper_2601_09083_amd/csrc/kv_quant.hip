@@ -208,9 +208,9 @@ __global__ __launch_bounds__(kThreads + SRT_WAVE) void write_short_kernel(WriteA
       head.rest();
     }
   } else {
-    const int e = min(max(a.counts[b], 0), min(a.Dmax, a.T - 1)) + 1;
+    const int k = min(max(a.counts[b], 0), min(a.Dmax, a.T - 1));
     advance_draft(a.ctx_tail + static_cast<int64_t>(b) * a.Qmax, a.Qmax, a.draft_len + b,
-                  a.emitted + static_cast<int64_t>(b) * (a.Dmax + 1), e);
+                  a.emitted + static_cast<int64_t>(b) * (a.Dmax + 1), k);
   }
   __syncthreads();  // every thread has read ctx_len[b]
   if (threadIdx.x == 0) a.ctx_len[b] = end;
