@@ -150,6 +150,7 @@ class VerifyState:
     v_new: Optional[torch.Tensor] = None
     rules: Optional[srt.Rules] = None
     seen: Optional[torch.Tensor] = None    # count rows [B, V] that the penalties read
+    ended: Optional[torch.Tensor] = None   # [B] bool: under rules, sequences whose walk found every token forbidden
 
     # ---- set-up ---------------------------------------------------------
     @classmethod
@@ -214,11 +215,14 @@ class VerifyState:
     def use_rules(self, repetition=None, frequency=None, presence=None, biases=None, mask=None):
         """Sampling rules for the steps that follow: per-sequence penalties (lists
         or arrays [B]) over the tokens of the running sequences so far, biases (a
-        {token: bias} per sequence), mask [B, N, ceil(V / 32)] int32."""
+        {token: bias} per sequence), mask [B, N, ceil(V / 32)] int32.  A sequence
+        whose walk finds every token forbidden ends with that step (``ended``): it
+        emits nothing from then on, and its context, counts and draft inputs stay."""
         tw, dev = self.tokens, self.device
         mat, lens = W.pack_streams(list(tw.seqs))
         self.seen = torch.zeros((tw.batch, self.cfg.vocab), dtype=torch.int16, device=dev)
         srt.srt_seen_add(self.seen, _dev(mat, dev), _dev(lens, dev), reset=True)
+        self.ended = torch.zeros(tw.batch, dtype=torch.bool, device=dev)
         f = lambda x: None if x is None else _dev(np.asarray(x, dtype=np.float32), dev, torch.float32)
         self.rules = srt.Rules(seen=self.seen, repetition=f(repetition), frequency=f(frequency), presence=f(presence),
                                mask=mask, **(bias_lists(biases, dev) if biases is not None else {}))
@@ -257,10 +261,15 @@ class VerifyState:
             self.acc = srt.srt_accept_rules(self.logits, self.gumbel, inv_temperature, self.rules,
                                             self.tree["tree_tokens"], self.tree["tree_parent"], self.tree["n_nodes"],
                                             self.cfg.max_depth, out=self.acc or None, scratch=self.accept_scratch)
-            return self.acc
-        self.acc = srt.srt_accept(self.logits, self.gumbel, inv_temperature, self.tree["tree_tokens"],
-                                  self.tree["tree_parent"], self.tree["n_nodes"], self.cfg.max_depth,
-                                  out=self.acc or None, scratch=self.accept_scratch)
+        else:
+            self.acc = srt.srt_accept(self.logits, self.gumbel, inv_temperature, self.tree["tree_tokens"],
+                                      self.tree["tree_parent"], self.tree["n_nodes"], self.cfg.max_depth,
+                                      out=self.acc or None, scratch=self.accept_scratch)
+        if self.ended is not None:
+            for k in ("n_accepted", "n_emitted"):
+                self.acc[k].masked_fill_(self.ended, 0)
+            for k in ("out_tokens", "out_nodes"):
+                self.acc[k].masked_fill_(self.ended[:, None], -1)
         return self.acc
 
     def insert(self):
@@ -270,6 +279,16 @@ class VerifyState:
             srt.srt_seen_add(self.seen, self.acc["out_tokens"], self.acc["n_emitted"])
 
     def commit(self):
+        if self.ended is None:
+            self._commit()
+            return
+        before = self.attn_len.clone()
+        self._commit()
+        # (the root's vectors that a commit appends lie behind the context of a sequence that had ended)
+        torch.where(self.ended, before, self.attn_len, out=self.attn_len)
+        self.ended |= self.acc["n_emitted"] == self.acc["n_accepted"]
+
+    def _commit(self):
         if self.kv is not None:
             srt.srt_commit_quant(self.kv, self.k_new, self.v_new, self.acc["n_accepted"], self.acc["out_tokens"],
                                  self.acc["out_nodes"], ctx_tail=self.ctx_tail, draft_len=self.draft_len)
