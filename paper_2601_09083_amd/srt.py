@@ -12,6 +12,7 @@ import contextlib
 import ctypes
 import math
 import os
+import types
 from typing import Optional
 
 import torch
@@ -434,7 +435,12 @@ class KvQuant:
     [P,Hkv,page,d] of torch.float8_e4m3fn or torch.int8, a scale for each page
     and KV head [P,Hkv] fp32, the open page of every sequence [B,Hkv,page,d]
     bf16, block_table [B,max_pages] and ctx_len [B] int32.  It keeps the tensors
-    it is made of; they are updated in place."""
+    it is made of; they are updated in place, and are not to be replaced (another
+    set of tensors is another cache)."""
+
+    k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len = (
+        property(lambda self, i=i: self._tensors[i]) for i in range(8))
+    tensors = property(lambda self: self._tensors)
 
     def __init__(self, k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len):
         if k_pages.dim() != 4 or k_pages.dtype not in KV_TYPES:
@@ -451,13 +457,11 @@ class KvQuant:
         self.max_pages, self.device = int(block_table.shape[1]), k_pages.device
         if self.device.type != "cuda":
             raise ValueError("k_pages must be a CUDA (HIP) tensor")
-        self.tensors = (k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len)
-        self.k_pages, self.v_pages, self.k_scale, self.v_scale = self.tensors[:4]
-        self.k_tail, self.v_tail, self.block_table, self.ctx_len = self.tensors[4:]
-        types = (k_pages.dtype,) * 2 + (torch.float32,) * 2 + (torch.bfloat16,) * 2 + (torch.int32,) * 2
+        self._tensors = (k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len)
+        dtypes = (k_pages.dtype,) * 2 + (torch.float32,) * 2 + (torch.bfloat16,) * 2 + (torch.int32,) * 2
         names = [k for k, _ in KvQuantArgs._fields_[7:]]
         self._args = KvQuantArgs(KV_TYPES[k_pages.dtype], Hkv, d, page, self.max_pages, 0, P,
-                                 *[_arg(t, x, self.device, n) for t, x, n in zip(self.tensors, types, names)])
+                                 *[_arg(t, x, self.device, n) for t, x, n in zip(self._tensors, dtypes, names)])
         self._ref = ctypes.byref(self._args)
 
 
@@ -572,7 +576,8 @@ class Rules:
     seen [B,V] int16 (the bits of the count words), repetition, frequency,
     presence [B] fp32, bias lists (bias_offsets [B+1] int32, bias_tokens int32,
     bias_values fp32), mask [B,N,ceil(V/32)] int32 (bits of allowed tokens).  It
-    keeps the tensors it is made of; their contents may change between calls."""
+    keeps the tensors it is made of; their contents may change between calls, the
+    tensors themselves are not to be replaced."""
 
     _TYPES = {"seen": torch.int16, "repetition": torch.float32, "frequency": torch.float32, "presence": torch.float32,
               "bias_offsets": torch.int32, "bias_tokens": torch.int32, "bias_values": torch.float32,
@@ -582,7 +587,7 @@ class Rules:
         for name in tensors:
             if name not in self._TYPES:
                 raise ValueError(f"no such rule: {name}")
-        self.tensors = {k: tensors.get(k) for k in self._TYPES}
+        self.tensors = types.MappingProxyType({k: tensors.get(k) for k in self._TYPES})
         t = self.tensors
         has = [t[k] is not None for k in ("bias_offsets", "bias_tokens", "bias_values")]
         if any(has) != all(has):
