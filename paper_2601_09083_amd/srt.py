@@ -430,6 +430,14 @@ def _on_device(device, call, *args):
         return call(*args)
 
 
+def _kept_tensor(i):
+    """Tensor i of a handle; only itself can be assigned to it (as in ctx_len += 1)."""
+    def assign(self, t):
+        if t is not self._tensors[i]:
+            raise AttributeError("the handle keeps the tensors that it is made of: make another one")
+    return property(lambda self: self._tensors[i], assign)
+
+
 class KvQuant:
     """A KV cache held in 8 bits (srt_kv_quant of include/srt.h): pages
     [P,Hkv,page,d] of torch.float8_e4m3fn or torch.int8, a scale for each page
@@ -438,8 +446,7 @@ class KvQuant:
     it is made of; they are updated in place, and are not to be replaced (another
     set of tensors is another cache)."""
 
-    k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len = (
-        property(lambda self, i=i: self._tensors[i]) for i in range(8))
+    k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len = (_kept_tensor(i) for i in range(8))
     tensors = property(lambda self: self._tensors)
 
     def __init__(self, k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, block_table, ctx_len):

@@ -11,8 +11,16 @@ NAMES = ("k_pages", "v_pages", "k_scale", "v_scale", "k_tail", "v_tail", "block_
 @pytest.mark.parametrize("name", NAMES)
 def test_a_cache_does_not_take_another_tensor(name):
     kv = S.KvQuant.__new__(S.KvQuant)  # (a whole one needs a GPU)
+    kv._tensors = tuple(torch.zeros(1) for _ in range(8))
     with pytest.raises(AttributeError):
         setattr(kv, name, torch.zeros(1))
+
+
+def test_a_cache_is_updated_in_place():
+    kv = S.KvQuant.__new__(S.KvQuant)
+    kv._tensors = tuple(torch.zeros(1) for _ in range(8))
+    kv.ctx_len += 1
+    assert kv._tensors[7].tolist() == [1.0] and kv.ctx_len is kv._tensors[7]
 
 
 def test_rules_do_not_take_another_tensor():
