@@ -32,7 +32,9 @@
  *     stream (or by the caller).
  *   - Return value: SRT_OK, or a negative srt_status.  Argument errors are
  *     found on the host before anything is enqueued (SRT_ERR_INVALID /
- *     SRT_ERR_UNSUPPORTED); launch failures give SRT_ERR_HIP.  Conditions
+ *     SRT_ERR_UNSUPPORTED, also of srt_kv_append, srt_commit_quant,
+ *     srt_accept_rules and srt_seen_add for sizes that would take a launch of
+ *     2^32 threads); launch failures give SRT_ERR_HIP.  Conditions
  *     only the device can see (cache full, a stream bound to another prompt,
  *     out-of-range ids) set sticky flags in the workspace, read with
  *     srt_trie_status; the kernels never access memory outside the

@@ -20,6 +20,9 @@ inline int launch_status() {
   return e == hipSuccess ? SRT_OK : SRT_ERR_HIP;
 }
 
+// A launch takes fewer than 2^32 threads in a dimension.
+inline bool launchable(int64_t workgroups, int64_t threads) { return workgroups <= 0xFFFFFFFFll / threads; }
+
 inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 // ---------------------------------------------------------------------------

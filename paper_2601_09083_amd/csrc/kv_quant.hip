@@ -383,7 +383,8 @@ extern "C" int srt_kv_append(const srt_kv_quant* kv, int32_t B, int32_t T, const
   if (st != SRT_OK) return st;
   const int64_t pages = (static_cast<int64_t>(T) + 2 * kv->page - 2) / kv->page;  // that L % page + T tokens touch
   const int64_t at_once = (2 * kv->Hkv + kWaves - 1) / kWaves;
-  if (pages * at_once * B > 0x7FFFFFFF) return SRT_ERR_UNSUPPORTED;
+  const int64_t per_seq = T <= kShort ? 1 : pages * at_once;  // workgroups
+  if (!launchable(per_seq, kThreads) || !launchable(per_seq * B, kThreads)) return SRT_ERR_UNSUPPORTED;
   if (B == 0) return SRT_OK;
   st = check_kv_pointers(*kv);
   if (st == SRT_OK) st = check_new(*kv, k_new, v_new, ld);
@@ -408,6 +409,7 @@ extern "C" int srt_commit_quant(const srt_kv_quant* kv, int32_t B, int32_t N, co
   if (st != SRT_OK) return st;
   if ((ctx_tail == nullptr) != (draft_len == nullptr)) return SRT_ERR_INVALID;
   if (ctx_tail && (max_match < 1 || max_match > 64)) return SRT_ERR_INVALID;
+  if (!launchable(B, kThreads + SRT_WAVE)) return SRT_ERR_UNSUPPORTED;
   if (B == 0) return SRT_OK;
   st = check_kv_pointers(*kv);
   if (st == SRT_OK) st = check_new(*kv, k_new, v_new, ld);

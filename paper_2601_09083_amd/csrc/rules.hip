@@ -463,6 +463,8 @@ extern "C" int srt_accept_rules(int32_t B, int32_t N, int32_t V, int32_t Dmax, c
                       out_tokens, out_nodes);
   if (st != SRT_OK || B == 0) return st;
   if (V > kMaxVocab) return SRT_ERR_UNSUPPORTED;
+  const bool short_rows = static_cast<int64_t>(V) * (gumbel ? 2 : 1) <= kShortRow;
+  const unsigned short_threads = V <= kNarrowRow ? 256 : 1024;
   if (!scratch || scratch_bytes < srt_accept_scratch_bytes(B)) return SRT_ERR_CAPACITY;
   if (reinterpret_cast<uintptr_t>(scratch) % 256) return SRT_ERR_INVALID;
 
@@ -481,13 +483,12 @@ extern "C" int srt_accept_rules(int32_t B, int32_t N, int32_t V, int32_t Dmax, c
   a.n_bias = rules->n_bias;
   a.mask_words = (V + 31) / 32;
   const int64_t grid = static_cast<int64_t>(B) * a.n_chunks;
-  if (grid > 0x7FFFFFFF) return SRT_ERR_UNSUPPORTED;
+  if (!(short_rows ? launchable(B, short_threads) : launchable(grid, kThreads))) return SRT_ERR_UNSUPPORTED;
 
   hipStream_t s = as_stream(stream);
-  if (static_cast<int64_t>(V) * (gumbel ? 2 : 1) <= kShortRow) {
-    const unsigned threads = V <= kNarrowRow ? 256 : 1024;
-    if (gumbel) rules_short_kernel<true><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
-    else rules_short_kernel<false><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
+  if (short_rows) {
+    if (gumbel) rules_short_kernel<true><<<static_cast<unsigned>(B), short_threads, 0, s>>>(a);
+    else rules_short_kernel<false><<<static_cast<unsigned>(B), short_threads, 0, s>>>(a);
     return launch_status();
   }
   for (int level = 0; level <= Dmax && st == SRT_OK; ++level) {
@@ -509,11 +510,13 @@ extern "C" int srt_seen_add(uint16_t* seen, int32_t B, int32_t V, const int32_t*
   if (B == 0) return SRT_OK;
   if (!seen || !tokens || !lengths) return SRT_ERR_INVALID;
   const int64_t chunks = (static_cast<int64_t>(V) + kSeenChunk - 1) / kSeenChunk;
-  if (chunks * B > 0x7FFFFFFF) return SRT_ERR_UNSUPPORTED;
+  const bool few = !reset && stride <= kSeenStep;
+  const int64_t step_grid = (static_cast<int64_t>(B) + 3) / 4;
+  if (!(few ? launchable(step_grid, 256) : launchable(chunks * B, kSeenThreads))) return SRT_ERR_UNSUPPORTED;
   const SeenArgs a = {seen, tokens, lengths, B, V, stride, prompt};
   hipStream_t s = as_stream(stream);
-  if (!reset && stride <= kSeenStep) {
-    seen_step_kernel<<<static_cast<unsigned>((static_cast<int64_t>(B) + 3) / 4), 256, 0, s>>>(a);
+  if (few) {
+    seen_step_kernel<<<static_cast<unsigned>(step_grid), 256, 0, s>>>(a);
     return launch_status();
   }
   // (longer rows of tokens than a counter holds enter in pieces)
