@@ -37,7 +37,8 @@ BF16_PEAK_TFLOPS = 2500.0
 def counters_path(config_name):
     """Committed rocprofv3 HBM-counter summary of srt_tree_attn on one workload."""
     return os.path.join(ROOT, "profiles", f"tree_attn_{config_name.replace('.', 'p')}_counters.json")
-ATTN_SRC = os.path.join(ROOT, "paper_2601_09083_amd", "csrc", "tree_attn.hip")
+# where the kernels of srt_tree_attn and the rules that launch them are
+ATTN_SRC = tuple(os.path.join(ROOT, "paper_2601_09083_amd", "csrc", f) for f in ("tree_attn.hip", "attn.h"))
 
 
 def attn_work(cfg, ctx_len, n_nodes, tree_depth):
@@ -55,8 +56,11 @@ def attn_work(cfg, ctx_len, n_nodes, tree_depth):
     return kv_bytes + qo_bytes, flops
 
 
-def source_sha(path):
-    return hashlib.sha256(open(path, "rb").read()).hexdigest()
+def source_sha(paths):
+    h = hashlib.sha256()
+    for path in paths:
+        h.update(open(path, "rb").read())
+    return h.hexdigest()
 
 
 def counter_traffic(config_name):
