@@ -529,7 +529,7 @@ extern "C" int srt_tree_attn(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int3
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   const int st = lay_out(a, cap, d, scratch, scratch_bytes, false);
   if (st != SRT_OK) return st;
-  a.ctx_cap = a.cap;
+  a.tree_room = 0;
 
   const int cus = cu_count();
   if (cus <= 0) return SRT_ERR_HIP;

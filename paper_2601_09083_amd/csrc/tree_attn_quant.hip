@@ -747,7 +747,7 @@ extern "C" int srt_tree_attn_quant(const srt_kv_quant* kv, int32_t B, int32_t N,
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   st = lay_out(a, cap, kv->d, scratch, scratch_bytes, true);
   if (st != SRT_OK) return st;
-  a.ctx_cap = a.cap - N;
+  a.tree_room = N;
 
   const int cus = cu_count();
   if (cus <= 0) return SRT_ERR_HIP;
