@@ -23,9 +23,10 @@
 //     head would be bound by one wave's chain per tile (1.3 us for 64 keys in
 //     tree_attn.hip, whatever the rows).  A workgroup's 8 waves are therefore
 //     WR waves along the rows times 8 / WR along the keys, by the rows that the
-//     item has (4 waves, two workgroups to a CU, in batches of narrow trees): up to 32 rows every wave streams 32-key tiles of its own,
-//     with no barrier at all, up to 64 and 128 pairs and fours of waves share
-//     a tile, and the key groups' partial results are merged in LDS at the end.
+//     item has (4 waves, two workgroups to a CU, in batches of narrow trees): up
+//     to 32 rows every wave streams 32-key tiles of its own, with no barrier at
+//     all, up to 64 and 128 pairs and fours of waves share a tile, and the key
+//     groups' partial results are merged in LDS at the end.
 #include "attn.h"
 #include "kv_quant.h"
 
@@ -429,7 +430,10 @@ __device__ __forceinline__ void attend(const QuantArgs& a, Smem<D, W, R>& sm, co
           }
       }
     }
-    // p * sv in bf16 and this lane's sum of p (of the rounded ones).
+    // p * sv in bf16, the type in which the second product's MFMAs take it (as
+    // tree_attn.hip's p; the same rounding of every term, at most 2^-8 of it, and
+    // the largest share of the result's error), and this lane's fp32 sum of p, of
+    // the rounded ones, so that the weights of a row add up to one.
     auto probs = [&](auto dm_c, float dm) {
       typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
       const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
