@@ -409,7 +409,7 @@ extern "C" int srt_commit_quant(const srt_kv_quant* kv, int32_t B, int32_t N, co
   if (st != SRT_OK) return st;
   if ((ctx_tail == nullptr) != (draft_len == nullptr)) return SRT_ERR_INVALID;
   if (ctx_tail && (max_match < 1 || max_match > 64)) return SRT_ERR_INVALID;
-  if (!launchable(B, kThreads + SRT_WAVE)) return SRT_ERR_UNSUPPORTED;
+  if (!launchable(B, kThreads + (ctx_tail ? SRT_WAVE : 0))) return SRT_ERR_UNSUPPORTED;
   if (B == 0) return SRT_OK;
   st = check_kv_pointers(*kv);
   if (st == SRT_OK) st = check_new(*kv, k_new, v_new, ld);

@@ -22,6 +22,9 @@ def test_batches_beyond_a_launch_are_refused():
     assert append(one, B=1 << 23, T=1) == S.SRT_ERR_UNSUPPORTED
     assert append(kv(Hkv=255), B=(1 << 31) - 1, T=(1 << 31) - 1, ld=1 << 20) == S.SRT_ERR_UNSUPPORTED
     assert commit(one, B=1 << 23) == S.SRT_ERR_UNSUPPORTED
+    between = 0xFFFFFFFF // 576 + 1  # too many with the wave of the draft inputs
+    assert commit(one, B=between, tail=P, length=P) == S.SRT_ERR_UNSUPPORTED
+    assert commit(one, B=between, acc=None) == S.SRT_ERR_INVALID  # (further on, without them)
     assert rules(1 << 24, 1000) == S.SRT_ERR_UNSUPPORTED
     assert rules(1 << 22, 4000) == S.SRT_ERR_UNSUPPORTED
     assert rules(1 << 19, 152064, sampled=True) == S.SRT_ERR_UNSUPPORTED
