@@ -17,6 +17,8 @@
  *   srt_kv_append, srt_tree_attn_quant, srt_commit_quant, srt_kv_read
  * and the acceptance walk under penalties, biases and masks
  *   srt_accept_rules, srt_seen_add
+ * The step's queries and keys turned by their positions, and its vectors written to the cache
+ *   srt_rope_append, srt_rope_rows
  *
  * Conventions shared by every entry point
  *   - Pointers are device pointers unless the comment says "host".  All
@@ -526,6 +528,59 @@ int srt_accept_rules(int32_t B, int32_t N, int32_t V, int32_t Dmax, const float*
 int srt_seen_add(uint16_t* seen, int32_t B, int32_t V, const int32_t* tokens,
                  const int32_t* lengths, int32_t stride, int32_t prompt, int32_t reset,
                  void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary position encoding of a step's queries and keys, and the append of its
+ * keys and values to the paged bf16 cache (Section 3: the pass that verifies the
+ * tree computes the vectors of every node).
+ *
+ * Row i < min(counts[b], T) of sequence b with L = ctx_len[b] committed positions
+ * is the token of position p = L + depth[b, i] (depth NULL: p = L + i).  With the
+ * angle a = p * inv_freq[m], formed in 64 bits, c = fl(cos a) * factor and
+ * s = fl(sin a) * factor, the pair (x0, x1) of a head's dims m and m + rot / 2
+ * (interleaved 0) or 2 m and 2 m + 1 (interleaved 1), m < rot / 2, becomes
+ *   (x0 * c - x1 * s, x1 * c + x0 * s)
+ * in fp32, rounded to bf16 once; dims from rot on stay.  Rows from counts[b] on
+ * are neither read nor written (a negative count is 0).
+ *
+ * srt_rope_append writes the turned queries to q_out and puts the turned keys and
+ * the values at slot L + i of the sequence (page block_table[b, (L + i) / page],
+ * slot (L + i) % page), where srt_tree_attn reads tree node i and srt_commit
+ * finds it; a slot outside the block table or the pool is skipped.  ctx_len is
+ * read only: after a prompt's piece the caller adds counts to it, once for all
+ * layers; after a tree srt_commit advances it.
+ * srt_rope_rows writes the turned keys as rows k_out, for the calls of the 8-bit
+ * cache (k_new of srt_kv_append, srt_tree_attn_quant and srt_commit_quant).
+ *
+ * Layouts (bf16 bits, all 16-byte aligned): q [B, T, Hq, d] with ldq elements from
+ * one token to the next (the sequences are T * ldq apart; so a fused projection's
+ * output is read where it lies), k and v [B, T, Hkv, d] alike with ldkv (ldk),
+ * k_out with ldo, q_out [B, T, Hq, d] packed; leading sizes are multiples of 8
+ * (else SRT_ERR_INVALID).  q_out and k_out may be q and k themselves (the same
+ * address and leading size), but not overlap them otherwise.  Caches, block_table
+ * and ctx_len as in srt_tree_attn, with pages of any size; depth [B, T],
+ * counts [B] int32; inv_freq [rot / 2] fp32 (device).  d a multiple of 8 up to
+ * 512, rot a multiple of 16 up to d, at most 65536 heads (else
+ * SRT_ERR_UNSUPPORTED).  No slot may belong to two sequences.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const float* inv_freq;  /* angle per position of each pair */
+  int32_t rot;            /* leading dims of a head that turn */
+  int32_t interleaved;    /* 0: dims m and m + rot / 2 are a pair; 1: 2 m and 2 m + 1 */
+  float factor;           /* of cos and sin: 1, or the attention scaling of a stretched context */
+  int32_t reserved;       /* must be 0 */
+} srt_rope;
+
+int srt_rope_append(const srt_rope* rope, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                    int32_t page, int32_t max_pages, int64_t num_pages, const uint16_t* q, int64_t ldq,
+                    const uint16_t* k, const uint16_t* v, int64_t ldkv, const int32_t* depth,
+                    const int32_t* counts, uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
+                    const int32_t* block_table, const int32_t* ctx_len, void* stream);
+
+int srt_rope_rows(const srt_rope* rope, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                  const uint16_t* q, int64_t ldq, const uint16_t* k, int64_t ldk, const int32_t* depth,
+                  const int32_t* counts, const int32_t* ctx_len, uint16_t* q_out, uint16_t* k_out,
+                  int64_t ldo, void* stream);
 
 /* Library version string (host only). */
 const char* srt_version(void);

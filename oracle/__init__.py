@@ -32,10 +32,12 @@ method computes, written from the paper (SRT, arXiv 2601.09083):
                    summation orders.
 * ``kv_quant``  -- the 8-bit KV cache: a page's codes and scales, its values,
                    what a sequence's context holds.
+* ``rope``      -- the rotary position encoding and a new vector's place in the
+                   cache.
 * ``rules``     -- the acceptance walk under penalties, biases and masks, and
                    the token counts they read.
 
 Pins (tests marked ``not gpu``) tie each function to closed forms, brute
 force, library routines and invariants; see ``tests/test_oracle_*.py``.
 """
-from . import accept, attention, commit, draft, kv_quant, lmhead, rules, trie  # noqa: F401
+from . import accept, attention, commit, draft, kv_quant, lmhead, rope, rules, trie  # noqa: F401

@@ -31,7 +31,7 @@ EXPORTS = ("srt_trie_workspace_bytes", "srt_trie_init", "srt_trie_insert", "srt_
            "srt_tree_attn", "srt_accept_scratch_bytes", "srt_accept", "srt_accept_lmhead_scratch_bytes",
            "srt_accept_lmhead", "srt_commit", "srt_version", "srt_accept_noalloc",
            "srt_tree_attn_quant_scratch_bytes", "srt_tree_attn_quant", "srt_kv_append", "srt_commit_quant",
-           "srt_kv_read", "srt_accept_rules", "srt_seen_add")
+           "srt_kv_read", "srt_accept_rules", "srt_seen_add", "srt_rope_append", "srt_rope_rows")
 SRT_ACCEPT_NOALLOC_MAX_BATCH = 4096  # include/srt.h
 
 
@@ -64,6 +64,11 @@ class RulesArgs(ctypes.Structure):
     _fields_ = ([(k, ctypes.c_void_p) for k in ("seen", "repetition", "frequency", "presence", "bias_offsets",
                                                 "bias_tokens", "bias_values", "mask")] +
                 [("n_bias", ctypes.c_int32), ("reserved", ctypes.c_int32)])
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("factor", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -103,6 +108,10 @@ def lib() -> ctypes.CDLL:
             "srt_accept_rules": (ctypes.c_int, [_I32] * 4 + [_P, _P, ctypes.c_float, ctypes.POINTER(RulesArgs)] +
                                  [_P] * 8 + [_SZ, _P]),
             "srt_seen_add": (ctypes.c_int, [_P, _I32, _I32, _P, _P, _I32, _I32, _I32, _P]),
+            "srt_rope_append": (ctypes.c_int, [ctypes.POINTER(RopeArgs)] + [_I32] * 7 + [_I64, _P, _I64, _P, _P, _I64] +
+                                [_P] * 8),
+            "srt_rope_rows": (ctypes.c_int, [ctypes.POINTER(RopeArgs)] + [_I32] * 5 + [_P, _I64, _P, _I64] + [_P] * 5 +
+                              [_I64, _P]),
             "srt_version": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -659,6 +668,95 @@ def srt_seen_add(seen, tokens, lengths, prompt: bool = False, reset: bool = Fals
         dev, lib().srt_seen_add, _arg(seen, torch.int16, dev, "seen"), seen.shape[0], seen.shape[1],
         _arg(tokens, torch.int32, dev, "tokens"), _arg(lengths, torch.int32, dev, "lengths"), tokens.shape[1],
         int(bool(prompt)), int(bool(reset)), _stream_of(dev, stream)))
+
+
+# --------------------------------------------------------------------------- position encoding
+
+class Rope:
+    """A rotary position encoding (srt_rope of include/srt.h): inv_freq [rot / 2]
+    fp32, the angle per position of each pair of a head's first rot dims, which
+    are m and m + rot / 2 or, interleaved, 2 m and 2 m + 1; factor multiplies
+    cos and sin.  It keeps inv_freq, whose contents may change between calls."""
+
+    inv_freq = property(lambda self: self._inv_freq)
+
+    def __init__(self, inv_freq, interleaved: bool = False, factor: float = 1.0):
+        if inv_freq.dim() != 1 or inv_freq.device.type != "cuda":
+            raise ValueError("inv_freq must be a CUDA (HIP) tensor [rot / 2]")
+        self._inv_freq, self.device, self.rot = inv_freq, inv_freq.device, 2 * int(inv_freq.numel())
+        self._args = RopeArgs(_arg(inv_freq, torch.float32, self.device, "inv_freq"), self.rot, int(bool(interleaved)),
+                              factor, 0)
+        self._ref = ctypes.byref(self._args)
+
+
+def _rope_rows(x, B, T, H, d, dev, name):
+    """Elements from one token to the next of rows [B,T,H,d]."""
+    if x.shape != (B, T, H, d) or x.dtype is not torch.bfloat16 or x.device != dev:
+        raise ValueError(f"{name} must be {[B, T, H, d]} of bfloat16 on {dev}")
+    ld = _lead(x.stride(), B, T, H, d)
+    if ld < 0:
+        raise ValueError(f"{name}: a token's heads must lie side by side, sequences T tokens apart")
+    return ld
+
+
+def _rope_sizes(rope, q, k, counts, ctx_len, depth):
+    if q.dim() != 4 or k.dim() != 4 or q.shape[1] < 1:
+        raise ValueError("q must be [B, T, Hq, d], k [B, T, Hkv, d]")
+    B, T, Hq, d = q.shape
+    if counts.numel() != B or ctx_len.numel() != B or (depth is not None and depth.shape != (B, T)):
+        raise ValueError("counts and ctx_len must be [B], depth [B, T]")
+    return B, T, Hq, k.shape[2], d, rope.device
+
+
+def _rope_out(out, like, heads, dev, stream, name):
+    """The packed output: the given one, or zeros (rows that no count covers are not written)."""
+    if out is None:
+        with _device(dev), _on(stream):
+            return torch.zeros(like.shape, dtype=torch.bfloat16, device=dev)
+    if out.shape != like.shape:
+        raise ValueError(f"{name} must be [B, T, {heads}, d]")
+    return out
+
+
+def srt_rope_append(rope: Rope, q, k, v, counts, k_cache, v_cache, block_table, ctx_len, depth=None, q_out=None,
+                    stream=None):
+    """Turns the queries q [B,T,Hq,d] and the keys k [B,T,Hkv,d] of the tokens at
+    positions ctx_len + depth (or ctx_len + i), writes the keys and the values v
+    to slots ctx_len + i of the caches [P,Hkv,page,d] and returns the queries
+    [B,T,Hq,d].  Rows from counts[b] on are left alone (zero in a new q_out)."""
+    B, T, Hq, Hkv, d, dev = _rope_sizes(rope, q, k, counts, ctx_len, depth)
+    ldq, ldk = _rope_rows(q, B, T, Hq, d, dev, "q"), _rope_rows(k, B, T, Hkv, d, dev, "k")
+    if _rope_rows(v, B, T, Hkv, d, dev, "v") != ldk:
+        raise ValueError("k and v must have the same strides")
+    if k_cache.dim() != 4 or k_cache.shape[1] != Hkv or k_cache.shape[3] != d or v_cache.shape != k_cache.shape:
+        raise ValueError("caches must be [P, Hkv, page, d]")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    q_out = _rope_out(q_out, q, Hq, dev, stream, "q_out")
+    bf16, i32 = torch.bfloat16, torch.int32
+    _check("srt_rope_append", _on_device(
+        dev, lib().srt_rope_append, rope._ref, B, T, Hq, Hkv, d, k_cache.shape[2], block_table.shape[1], k_cache.shape[0],
+        q.data_ptr(), ldq, k.data_ptr(), v.data_ptr(), ldk, _maybe(depth, i32, dev, "depth"),
+        _arg(counts, i32, dev, "counts"), _arg(q_out, bf16, dev, "q_out"), _arg(k_cache, bf16, dev, "k_cache"),
+        _arg(v_cache, bf16, dev, "v_cache"), _arg(block_table, i32, dev, "block_table"),
+        _arg(ctx_len, i32, dev, "ctx_len"), _stream_of(dev, stream)))
+    return q_out
+
+
+def srt_rope_rows(rope: Rope, q, k, counts, ctx_len, depth=None, q_out=None, k_out=None, stream=None):
+    """The turned queries [B,T,Hq,d] and keys [B,T,Hkv,d] as rows; k_out may have
+    rows of its own leading size and may be k itself (as where k and v are parts of
+    one projection, which the 8-bit cache's calls read)."""
+    B, T, Hq, Hkv, d, dev = _rope_sizes(rope, q, k, counts, ctx_len, depth)
+    ldq, ldk = _rope_rows(q, B, T, Hq, d, dev, "q"), _rope_rows(k, B, T, Hkv, d, dev, "k")
+    q_out, k_out = _rope_out(q_out, q, Hq, dev, stream, "q_out"), _rope_out(k_out, k, Hkv, dev, stream, "k_out")
+    ldo = _rope_rows(k_out, B, T, Hkv, d, dev, "k_out")
+    i32 = torch.int32
+    _check("srt_rope_rows", _on_device(
+        dev, lib().srt_rope_rows, rope._ref, B, T, Hq, Hkv, d, q.data_ptr(), ldq, k.data_ptr(), ldk,
+        _maybe(depth, i32, dev, "depth"), _arg(counts, i32, dev, "counts"), _arg(ctx_len, i32, dev, "ctx_len"),
+        _arg(q_out, torch.bfloat16, dev, "q_out"), k_out.data_ptr(), ldo, _stream_of(dev, stream)))
+    return q_out, k_out
 
 
 def srt_version() -> str:
