@@ -19,6 +19,8 @@
  *   srt_accept_rules, srt_seen_add
  * The step's queries and keys turned by their positions, and its vectors written to the cache
  *   srt_rope_append, srt_rope_rows
+ * the attention of groups of sequences that share a prompt's pages
+ *   srt_tree_attn_shared
  *
  * Conventions shared by every entry point
  *   - Pointers are device pointers unless the comment says "host".  All
@@ -581,6 +583,37 @@ int srt_rope_rows(const srt_rope* rope, int32_t B, int32_t T, int32_t Hq, int32_
                   const uint16_t* q, int64_t ldq, const uint16_t* k, int64_t ldk, const int32_t* depth,
                   const int32_t* counts, const int32_t* ctx_len, uint16_t* q_out, uint16_t* k_out,
                   int64_t ldo, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Tree-masked attention for batches of which groups of sequences share a long
+ * prefix (several answers to one prompt): srt_tree_attn's result, with the keys
+ * and values that a group shares read once for all of its sequences.
+ *
+ * Sequence b is of group group_ids[b]; one outside [0, n_groups) shares nothing.
+ * Group g's sequences agree in the block table entries of their first
+ * prefix_len[g] positions, as far as whole pages go: the pages are the same ones.
+ * What is taken as shared is prefix_len[g] or the shortest member's context, if
+ * that is shorter, rounded down to whole pages, and read through the block table
+ * of the group's first sequence; where the tables do not agree there, the others'
+ * results are those of the first one's pages.  Members need not be next to each
+ * other; groups of one member share nothing.  n_groups 0: no sequence shares
+ * (group_ids and prefix_len may be NULL).  Sharing changes where the splits of the
+ * keys lie, and so the results by rounding only.
+ * group_ids [B], prefix_len [n_groups] int32; everything else as srt_tree_attn.
+ * scratch: srt_tree_attn_shared_scratch_bytes(...) bytes (0 for arguments that the
+ * call refuses), 256-byte aligned, else SRT_ERR_CAPACITY / SRT_ERR_INVALID.
+ * Unsupported (SRT_ERR_UNSUPPORTED): B > 65535, n_groups > 4096, Hkv > 255,
+ * max_pages * page > 2^30, or B * N * Hq / Hkv beyond 2^23 rows.
+ * ---------------------------------------------------------------------- */
+size_t srt_tree_attn_shared_scratch_bytes(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d,
+                                          int32_t page, int32_t max_pages, int32_t n_groups);
+
+int srt_tree_attn_shared(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int32_t page,
+                         int32_t max_pages, int64_t num_pages, int32_t n_groups, const uint16_t* q,
+                         const uint16_t* k_cache, const uint16_t* v_cache, const int32_t* block_table,
+                         const int32_t* ctx_len, const int32_t* tree_parent, const int32_t* n_nodes,
+                         const int32_t* group_ids, const int32_t* prefix_len, float scale,
+                         uint16_t* out, void* scratch, size_t scratch_bytes, void* stream);
 
 /* Library version string (host only). */
 const char* srt_version(void);

@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libsrt.so")
 SOURCES = ["trie.hip", "draft.hip", "tree_attn.hip", "accept.hip", "lmhead.hip", "commit.hip", "tree_attn_quant.hip",
-           "kv_quant.hip", "rules.hip", "rope.hip"]
+           "kv_quant.hip", "rules.hip", "rope.hip",
+           "tree_attn_shared.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

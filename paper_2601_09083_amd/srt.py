@@ -31,7 +31,8 @@ EXPORTS = ("srt_trie_workspace_bytes", "srt_trie_init", "srt_trie_insert", "srt_
            "srt_tree_attn", "srt_accept_scratch_bytes", "srt_accept", "srt_accept_lmhead_scratch_bytes",
            "srt_accept_lmhead", "srt_commit", "srt_version", "srt_accept_noalloc",
            "srt_tree_attn_quant_scratch_bytes", "srt_tree_attn_quant", "srt_kv_append", "srt_commit_quant",
-           "srt_kv_read", "srt_accept_rules", "srt_seen_add", "srt_rope_append", "srt_rope_rows")
+           "srt_kv_read", "srt_accept_rules", "srt_seen_add", "srt_rope_append", "srt_rope_rows",
+           "srt_tree_attn_shared_scratch_bytes", "srt_tree_attn_shared")
 SRT_ACCEPT_NOALLOC_MAX_BATCH = 4096  # include/srt.h
 
 
@@ -112,6 +113,8 @@ def lib() -> ctypes.CDLL:
                                 [_P] * 8),
             "srt_rope_rows": (ctypes.c_int, [ctypes.POINTER(RopeArgs)] + [_I32] * 5 + [_P, _I64, _P, _I64] + [_P] * 5 +
                               [_I64, _P]),
+            "srt_tree_attn_shared_scratch_bytes": (_SZ, [_I32] * 8),
+            "srt_tree_attn_shared": (ctypes.c_int, [_I32] * 7 + [_I64, _I32] + [_P] * 9 + [ctypes.c_float, _P, _P, _SZ, _P]),
             "srt_version": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -757,6 +760,53 @@ def srt_rope_rows(rope: Rope, q, k, counts, ctx_len, depth=None, q_out=None, k_o
         _maybe(depth, i32, dev, "depth"), _arg(counts, i32, dev, "counts"), _arg(ctx_len, i32, dev, "ctx_len"),
         _arg(q_out, torch.bfloat16, dev, "q_out"), k_out.data_ptr(), ldo, _stream_of(dev, stream)))
     return q_out, k_out
+
+
+# --------------------------------------------------------------------------- attention over a shared prefix
+
+def srt_tree_attn_shared_scratch_bytes(B: int, N: int, Hq: int, Hkv: int, d: int, page: int, max_pages: int,
+                                       n_groups: int) -> int:
+    return int(lib().srt_tree_attn_shared_scratch_bytes(B, N, Hq, Hkv, d, page, max_pages, n_groups))
+
+
+def srt_tree_attn_shared(q, k_cache, v_cache, block_table, ctx_len, tree_parent, n_nodes, group_ids, prefix_len,
+                         scale: float, out=None, scratch=None, stream=None):
+    """srt_tree_attn where the sequences b of one group group_ids[b] ([B] int32,
+    outside [0, n_groups): none) share the pages of their first prefix_len[group]
+    ([n_groups] int32) positions, which are read once for all of them."""
+    if q.dim() != 4 or k_cache.dim() != 4 or block_table.dim() != 2 or prefix_len.dim() != 1:
+        raise ValueError("q must be [B, N, Hq, d], caches [P, Hkv, page, d], block_table [B, max_pages], prefix_len [n_groups]")
+    B, N, Hq, d = q.shape
+    P, Hkv, page, d2 = k_cache.shape
+    if d2 != d or v_cache.shape != k_cache.shape or block_table.shape[0] != B:
+        raise ValueError("cache or block_table: shape mismatch")
+    if tree_parent.shape != (B, N) or n_nodes.numel() != B or ctx_len.numel() != B or group_ids.numel() != B:
+        raise ValueError("tree_parent must be [B, N], n_nodes, ctx_len and group_ids [B]")
+    if out is not None and out.shape != q.shape:
+        raise ValueError("out must be [B, N, Hq, d]")
+    dev, bf16, i32, n_groups, mp = q.device, torch.bfloat16, torch.int32, prefix_len.shape[0], block_table.shape[1]
+    if out is None or scratch is None:
+        with _device(dev), _on(stream):
+            if out is None:
+                out = torch.empty_like(q)
+            if scratch is None:
+                scratch = torch.empty(max(1, srt_tree_attn_shared_scratch_bytes(B, N, Hq, Hkv, d, page, mp, n_groups)),
+                                      dtype=torch.uint8, device=dev)
+    if scratch.device != dev or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous tensor on {dev}")
+    args = (B, N, Hq, Hkv, d, page, mp, P, n_groups, _arg(q, bf16, dev, "q"), _arg(k_cache, bf16, dev, "k_cache"),
+            _arg(v_cache, bf16, dev, "v_cache"), _arg(block_table, i32, dev, "block_table"), _arg(ctx_len, i32, dev, "ctx_len"),
+            _arg(tree_parent, i32, dev, "tree_parent"), _arg(n_nodes, i32, dev, "n_nodes"),
+            _arg(group_ids, i32, dev, "group_ids"), _arg(prefix_len, i32, dev, "prefix_len"), scale, _arg(out, bf16, dev, "out"))
+    call = lambda x: _on_device(dev, lib().srt_tree_attn_shared, *args, x.data_ptr(), x.numel() * x.element_size(),
+                                _stream_of(dev, stream))
+    st = call(scratch)
+    if st == SRT_ERR_CAPACITY:
+        need = srt_tree_attn_shared_scratch_bytes(B, N, Hq, Hkv, d, page, mp, n_groups)
+        with _device(dev), _on(stream):
+            st = call(torch.empty(need, dtype=torch.uint8, device=dev))
+    _check("srt_tree_attn_shared", st)
+    return out
 
 
 def srt_version() -> str:
