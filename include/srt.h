@@ -21,6 +21,8 @@
  *   srt_rope_append, srt_rope_rows
  * the attention of groups of sequences that share a prompt's pages
  *   srt_tree_attn_shared
+ * and the acceptance walk of a policy that samples with top-k, top-p and min-p
+ *   srt_accept_sample
  *
  * Conventions shared by every entry point
  *   - Pointers are device pointers unless the comment says "host".  All
@@ -614,6 +616,45 @@ int srt_tree_attn_shared(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t 
                          const int32_t* ctx_len, const int32_t* tree_parent, const int32_t* n_nodes,
                          const int32_t* group_ids, const int32_t* prefix_len, float scale,
                          uint16_t* out, void* scratch, size_t scratch_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Acceptance walk where the policy samples with a temperature, top-k, top-p and
+ * min-p, each sequence with its own: srt_accept (srt_accept_rules, where rules are
+ * given) with this choice at a visited node u in step k:
+ *   y_j = the logit, under the rules if there are any (srt_accept_rules' y);
+ *   z_j = fl(y_j * inv_temperature[b]); a NaN or -inf (and what the mask forbids)
+ *         takes no part;
+ *   the tokens in the order of z descending, j ascending, are kept
+ *     as far as the first top_k[b] of them go (<= 0: all), and of these
+ *     as long as the mass exp(z - max z) of those before a token is below top_p[b]
+ *     times the mass of all of these (>= 1: all), and of these
+ *     as long as z_j - max z >= log(min_p[b]) (<= 0: all);
+ *   the first one is kept whatever the parameters are (top_k 1 is greedy; so is a
+ *   top_p of 0 or less, a min_p above 1, and a NaN in either);
+ *   tok = arg-max over the kept ones of fl(z_j + gumbel[b, k, j]), lowest j on ties.
+ * Masses are held in 64 bits, the weights they are sums of in 32 or more: the place
+ * of the top-p cut is that of exact sums to about 1e-7 of the mass.  Noise is read
+ * at kept tokens only (it must be finite there).  Where nothing takes part the walk
+ * ends without a bonus token, as srt_accept_rules' does.  Without noise (gumbel
+ * NULL) tok is the arg-max of y and the parameters are not used.
+ * Any pointer of the parameters may be NULL: 1, off, off, off.  inv_temperature,
+ * top_p, min_p [B] fp32, finite; top_k [B] int32.  rules may be NULL.  V up to 2^21,
+ * up to 2^18 under rules (else SRT_ERR_UNSUPPORTED).  Other arguments and outputs
+ * as srt_accept; one launch, no scratch.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const float* inv_temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int64_t reserved;  /* must be 0 */
+} srt_sampling;
+
+int srt_accept_sample(int32_t B, int32_t N, int32_t V, int32_t Dmax, const float* logits,
+                      const float* gumbel, const srt_sampling* sampling, const srt_rules* rules,
+                      const int32_t* tree_tokens, const int32_t* tree_parent, const int32_t* n_nodes,
+                      int32_t* n_accepted, int32_t* out_tokens, int32_t* out_nodes,
+                      int32_t* n_emitted, void* stream);
 
 /* Library version string (host only). */
 const char* srt_version(void);

@@ -34,10 +34,12 @@ method computes, written from the paper (SRT, arXiv 2601.09083):
                    what a sequence's context holds.
 * ``rope``      -- the rotary position encoding and a new vector's place in the
                    cache.
+* ``sampling``  -- the acceptance walk of a policy that samples with top-k, top-p and
+                   min-p.
 * ``rules``     -- the acceptance walk under penalties, biases and masks, and
                    the token counts they read.
 
 Pins (tests marked ``not gpu``) tie each function to closed forms, brute
 force, library routines and invariants; see ``tests/test_oracle_*.py``.
 """
-from . import accept, attention, commit, draft, kv_quant, lmhead, rope, rules, trie  # noqa: F401
+from . import accept, attention, commit, draft, kv_quant, lmhead, rope, rules, sampling, trie  # noqa: F401

@@ -12,7 +12,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libsrt.so")
 SOURCES = ["trie.hip", "draft.hip", "tree_attn.hip", "accept.hip", "lmhead.hip", "commit.hip", "tree_attn_quant.hip",
            "kv_quant.hip", "rules.hip", "rope.hip",
-           "tree_attn_shared.hip"]
+           "tree_attn_shared.hip", "sample.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -18,132 +18,21 @@
 // skips marked entries (a quartet of them is not read), and a thread per marked
 // token then scores it with its path count and bias.  Entries that were never
 // said (count word 0) take no arithmetic of the penalties.
-#include "accept.h"
+#include "rules.h"
 
 namespace {
 
 constexpr int kMaxChunk = 65536;                      // entries of a chunk, at most
 constexpr int64_t kMaxVocab = int64_t(kMaxChunk) * kMaxChunks;
-constexpr int kPrompt = 0x8000;                       // bit of a count word: in the prompt
-constexpr int kCount = 0x7fff;                        // its other bits: times in the output
 
-struct RulesArgs : AcceptArgs {
-  const uint16_t* seen;
-  const float* repetition;
-  const float* frequency;
-  const float* presence;
-  const int32_t* bias_offsets;
-  const int32_t* bias_tokens;
-  const float* bias_values;
-  const uint32_t* mask;
-  int32_t n_bias, mask_words;
-};
-
-// The rules of one sequence, then those of the node that it stands on.
-struct Row {
-  const float* logits;
-  const float* noise;    // nullptr: greedy
-  const uint16_t* seen;  // nullptr: no counts
-  const uint32_t* mask;  // nullptr: everything allowed
-  float r, f, p, invT;
-  int bias0, bias1;      // its entries of the bias list
-};
-
-__device__ inline Row rules_of(const RulesArgs& a, int b, int level) {
-  Row w;
-  w.noise = a.gumbel ? a.gumbel + (static_cast<int64_t>(b) * (a.Dmax + 1) + level) * a.V : nullptr;
-  w.seen = a.seen ? a.seen + static_cast<int64_t>(b) * a.V : nullptr;
-  w.r = a.repetition ? a.repetition[b] : 1.f;
-  w.f = a.frequency ? a.frequency[b] : 0.f;
-  w.p = a.presence ? a.presence[b] : 0.f;
-  w.invT = a.invT;
-  w.bias0 = w.bias1 = 0;
-  if (a.bias_offsets) {
-    w.bias0 = min(max(a.bias_offsets[b], 0), a.n_bias);
-    w.bias1 = min(max(a.bias_offsets[b + 1], w.bias0), a.n_bias);
-  }
-  return w;
-}
-
-__device__ inline void stand_on(const RulesArgs& a, Row& w, int b, int u) {
-  w.logits = a.logits + (static_cast<int64_t>(b) * a.N + u) * a.V;
-  w.mask = a.mask ? a.mask + (static_cast<int64_t>(b) * a.N + u) * a.mask_words : nullptr;
-}
-
-// The penalised logit; every operation rounded by itself.
-__device__ inline float penalised(const Row& w, float y, bool prompt, int count) {
-  if (prompt || count > 0) y = y > 0.f ? __fdiv_rn(y, w.r) : mul_rounded(y, w.r);
-  y = add_rounded(y, -mul_rounded(w.f, static_cast<float>(count)));
-  return count > 0 ? add_rounded(y, -w.p) : y;
-}
-
-template <bool kNoise>
-__device__ inline float noisy(const Row& w, float y, float g) {
-  return kNoise ? add_rounded(mul_rounded(y, w.invT), g) : y;
-}
-
-// The best so far in ascending order of the index: a NaN or -inf is never taken.
-struct Top {
-  float v = -INFINITY;
-  int i = 0;
-  __device__ void ascending(float x, int j) {
-    if (x > v) {
-      v = x;
-      i = j;
-    }
-  }
-  __device__ unsigned long long key() const { return v > -INFINITY ? pack_key(v, i) : 0ull; }
-};
-
-typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
-
-// Tokens emitted on this walk, and whether the bias list has an entry of them.
-struct Path {
-  int32_t tok[kMaxLevels];
-  int32_t biased[kMaxLevels];
-};
-
-// Marks of the chunk [lo, hi) (lo a multiple of 32) in `skip`: masked entries,
-// tokens of the path (n of them) and tokens with a bias.  All threads; synchronises.
-__device__ inline void mark(const RulesArgs& a, const Row& w, Path& path, int n, int lo, int hi, uint32_t* skip,
-                            int threads) {
-  const int words = (hi - lo + 31) / 32;
-  const int at = w.bias0 + static_cast<int>(threadIdx.x);
-  const int bias = at < w.bias1 ? a.bias_tokens[at] : -1;  // (under way together with the mask)
-  for (int i = threadIdx.x; i < words; i += threads) skip[i] = w.mask ? ~w.mask[lo / 32 + i] : 0u;
-  if (static_cast<int>(threadIdx.x) < n) path.biased[threadIdx.x] = 0;
-  __syncthreads();
-  auto set = [&](int t) { atomicOr(&skip[(t - lo) >> 5], 1u << ((t - lo) & 31)); };
-  auto set_bias = [&](int t) {
-    if (t < lo || t >= hi) return;
-    set(t);
-    for (int i = 0; i < n; ++i)
-      if (path.tok[i] == t) path.biased[i] = 1;
-  };
-  if (static_cast<int>(threadIdx.x) < n) {  // n < 64 <= threads
-    const int t = path.tok[threadIdx.x];
-    if (t >= lo && t < hi) set(t);
-  }
-  set_bias(bias);
-  for (int i = at + threads; i < w.bias1; i += threads) set_bias(a.bias_tokens[i]);
-  __syncthreads();
-}
-
-// Score of one marked token that is allowed, with its path count and, where
-// `from` >= 0, the run of its biases that starts at that entry of the list.
+// Score of one marked token that is allowed.
 template <bool kNoise>
 __device__ inline void special(const RulesArgs& a, const Row& w, const Path& path, int n, int t, int from,
                                unsigned long long& key) {
-  const uint32_t allowed = w.mask ? w.mask[t >> 5] >> (t & 31) : 1u;
-  const int word = w.seen ? w.seen[t] : 0;
+  const bool allowed = allowed_token(w, t);
   const float l = w.logits[t], g = kNoise ? w.noise[t] : 0.f;
-  int count = word & kCount;
-  for (int i = 0; i < n; ++i) count += path.tok[i] == t;
-  float y = penalised(w, l, word & kPrompt, count);
-  if (from >= 0)
-    for (int i = from; i < w.bias1 && a.bias_tokens[i] == t; ++i) y = add_rounded(y, a.bias_values[i]);
-  const float x = noisy<kNoise>(w, y, g);
-  if ((allowed & 1u) && x > -INFINITY) key = max(key, pack_key(x, t));
+  const float x = noisy<kNoise>(w, special_logit(a, w, path, n, t, from, l), g);
+  if (allowed && x > -INFINITY) key = max(key, pack_key(x, t));
 }
 
 // This thread's best entry of [lo, hi) of one row, packed (0: none).  kUnroll
@@ -202,23 +91,8 @@ __device__ inline unsigned long long part_best(const RulesArgs& a, const Row& w,
     const float x = noisy<kNoise>(w, y, kNoise ? w.noise[j] : 0.f);
     if (x > -INFINITY) key = max(key, pack_key(x, j));
   }
-  if (tid < n) {  // (one that the bias list has is scored there)
-    const int t = path.tok[tid];
-    if (t >= lo && t < hi && !path.biased[tid]) special<kNoise>(a, w, path, n, t, -1, key);
-  }
-  for (int k = w.bias0 + tid; k < w.bias1; k += threads) {
-    const int t = a.bias_tokens[k];
-    if (t >= lo && t < hi && (k == w.bias0 || a.bias_tokens[k - 1] != t)) special<kNoise>(a, w, path, n, t, k, key);
-  }
-  return key;
-}
-
-__device__ inline unsigned long long wave_max(unsigned long long key) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const unsigned long long o = shfl_xor_u64(key, off);
-    key = o > key ? o : key;
-  }
+  for_special(a, w, path, n, lo, hi, threads,
+              [&](int t, int from) { special<kNoise>(a, w, path, n, t, from, key); });
   return key;
 }
 
@@ -455,10 +329,7 @@ extern "C" int srt_accept_rules(int32_t B, int32_t N, int32_t V, int32_t Dmax, c
                                 const int32_t* tree_tokens, const int32_t* tree_parent, const int32_t* n_nodes,
                                 int32_t* n_accepted, int32_t* out_tokens, int32_t* out_nodes, int32_t* n_emitted,
                                 void* scratch, size_t scratch_bytes, void* stream) {
-  if (!rules || rules->reserved != 0 || rules->n_bias < 0) return SRT_ERR_INVALID;
-  const bool bias = rules->bias_offsets || rules->bias_tokens || rules->bias_values;
-  if (bias && (!rules->bias_offsets || (rules->n_bias > 0 && (!rules->bias_tokens || !rules->bias_values))))
-    return SRT_ERR_INVALID;
+  if (!rules || check_rules(*rules) != SRT_OK) return SRT_ERR_INVALID;
   int st = check_args(B, N, V, Dmax, logits, inv_temperature, tree_tokens, tree_parent, n_nodes, n_accepted,
                       out_tokens, out_nodes);
   if (st != SRT_OK || B == 0) return st;
@@ -472,16 +343,7 @@ extern "C" int srt_accept_rules(int32_t B, int32_t N, int32_t V, int32_t Dmax, c
   static_cast<AcceptArgs&>(a) =
       walk_args(B, N, V, Dmax, logits, gumbel, inv_temperature, tree_tokens, tree_parent, n_nodes, n_accepted,
                 out_tokens, out_nodes, n_emitted, static_cast<char*>(scratch), 32);
-  a.seen = rules->seen;
-  a.repetition = rules->repetition;
-  a.frequency = rules->frequency;
-  a.presence = rules->presence;
-  a.bias_offsets = rules->bias_offsets;
-  a.bias_tokens = rules->bias_tokens;
-  a.bias_values = rules->bias_values;
-  a.mask = rules->mask;
-  a.n_bias = rules->n_bias;
-  a.mask_words = (V + 31) / 32;
+  take_rules(a, *rules);
   const int64_t grid = static_cast<int64_t>(B) * a.n_chunks;
   if (!(short_rows ? launchable(B, short_threads) : launchable(grid, kThreads))) return SRT_ERR_UNSUPPORTED;
 

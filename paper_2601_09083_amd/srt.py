@@ -32,7 +32,7 @@ EXPORTS = ("srt_trie_workspace_bytes", "srt_trie_init", "srt_trie_insert", "srt_
            "srt_accept_lmhead", "srt_commit", "srt_version", "srt_accept_noalloc",
            "srt_tree_attn_quant_scratch_bytes", "srt_tree_attn_quant", "srt_kv_append", "srt_commit_quant",
            "srt_kv_read", "srt_accept_rules", "srt_seen_add", "srt_rope_append", "srt_rope_rows",
-           "srt_tree_attn_shared_scratch_bytes", "srt_tree_attn_shared")
+           "srt_tree_attn_shared_scratch_bytes", "srt_tree_attn_shared", "srt_accept_sample")
 SRT_ACCEPT_NOALLOC_MAX_BATCH = 4096  # include/srt.h
 
 
@@ -65,6 +65,10 @@ class RulesArgs(ctypes.Structure):
     _fields_ = ([(k, ctypes.c_void_p) for k in ("seen", "repetition", "frequency", "presence", "bias_offsets",
                                                 "bias_tokens", "bias_values", "mask")] +
                 [("n_bias", ctypes.c_int32), ("reserved", ctypes.c_int32)])
+
+
+class SamplingArgs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("inv_temperature", "top_k", "top_p", "min_p")] + [("reserved", ctypes.c_int64)]
 
 
 class RopeArgs(ctypes.Structure):
@@ -115,6 +119,8 @@ def lib() -> ctypes.CDLL:
                               [_I64, _P]),
             "srt_tree_attn_shared_scratch_bytes": (_SZ, [_I32] * 8),
             "srt_tree_attn_shared": (ctypes.c_int, [_I32] * 7 + [_I64, _I32] + [_P] * 9 + [ctypes.c_float, _P, _P, _SZ, _P]),
+            "srt_accept_sample": (ctypes.c_int, [_I32] * 4 + [_P, _P, ctypes.POINTER(SamplingArgs), ctypes.POINTER(RulesArgs)] +
+                                  [_P] * 8),
             "srt_version": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -671,6 +677,62 @@ def srt_seen_add(seen, tokens, lengths, prompt: bool = False, reset: bool = Fals
         dev, lib().srt_seen_add, _arg(seen, torch.int16, dev, "seen"), seen.shape[0], seen.shape[1],
         _arg(tokens, torch.int32, dev, "tokens"), _arg(lengths, torch.int32, dev, "lengths"), tokens.shape[1],
         int(bool(prompt)), int(bool(reset)), _stream_of(dev, stream)))
+
+
+# --------------------------------------------------------------------------- sampling
+
+class Sampling:
+    """How each sequence of a batch samples (srt_sampling of include/srt.h), each
+    optional: inv_temperature, top_p, min_p [B] fp32, top_k [B] int32.  It keeps the
+    tensors it is made of; their contents may change between calls, the tensors
+    themselves are not to be replaced."""
+
+    _TYPES = {"inv_temperature": torch.float32, "top_k": torch.int32, "top_p": torch.float32, "min_p": torch.float32}
+
+    def __init__(self, inv_temperature=None, top_k=None, top_p=None, min_p=None):
+        self.tensors = types.MappingProxyType(dict(inv_temperature=inv_temperature, top_k=top_k, top_p=top_p, min_p=min_p))
+        given = [x for x in self.tensors.values() if x is not None]
+        self.device = given[0].device if given else None
+        self._args = SamplingArgs(*[_maybe(self.tensors[k], x, self.device, k) for k, x in self._TYPES.items()], 0)
+        self._ref = ctypes.byref(self._args)
+
+    def check(self, B: int, device):
+        if self.device is not None and self.device != device:
+            raise ValueError(f"the sampling parameters are on {self.device}, not on {device}")
+        for name, t in self.tensors.items():
+            if t is not None and t.shape != (B,):
+                raise ValueError(f"{name} must be [{B}]")
+
+
+def srt_accept_sample(logits, gumbel, sampling: Sampling, tree_tokens, tree_parent, n_nodes, max_depth: int, rules=None,
+                      out=None, stream=None) -> dict:
+    """The acceptance walk of a policy that samples with each sequence's
+    temperature, top-k, top-p and min-p from the noise gumbel [B,max_depth+1,V] (None:
+    greedy), under sampling rules if given; outputs as srt_accept_rules."""
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, N, V]")
+    B, N, V = logits.shape
+    if gumbel is not None and gumbel.shape != (B, max_depth + 1, V):
+        raise ValueError("gumbel must be [B, max_depth+1, V]")
+    if tree_tokens.shape != (B, N) or tree_parent.shape != (B, N) or n_nodes.numel() != B:
+        raise ValueError("tree arrays must be [B, N], n_nodes [B]")
+    dev, f32, i32 = logits.device, torch.float32, torch.int32
+    sampling.check(B, dev)
+    if rules is not None:
+        rules.check(B, N, V, dev)
+    if out is None:
+        with _device(dev), _on(stream):
+            out = _walk_outputs(B, max_depth, dev)
+    else:
+        _check_walk_outputs(out, B, max_depth)
+    _check("srt_accept_sample", _on_device(
+        dev, lib().srt_accept_sample, B, N, V, max_depth, _arg(logits, f32, dev, "logits"),
+        _maybe(gumbel, f32, dev, "gumbel"), sampling._ref, rules._ref if rules is not None else None,
+        _arg(tree_tokens, i32, dev, "tree_tokens"), _arg(tree_parent, i32, dev, "tree_parent"),
+        _arg(n_nodes, i32, dev, "n_nodes"), _arg(out["n_accepted"], i32, dev, "n_accepted"),
+        _arg(out["out_tokens"], i32, dev, "out_tokens"), _arg(out["out_nodes"], i32, dev, "out_nodes"),
+        _maybe(out.get("n_emitted"), i32, dev, "n_emitted"), _stream_of(dev, stream)))
+    return out
 
 
 # --------------------------------------------------------------------------- position encoding
