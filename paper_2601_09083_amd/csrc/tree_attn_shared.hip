@@ -7,16 +7,459 @@
 // in parts, the shared prefix and its own keys, which their running maximum m and
 // sum l join exactly: out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.
 //
-// GPU design.  The tile kernel (attn_bf16.h) takes items of two kinds: the rows of
-// one sequence against a split of its own keys, and the rows of a whole group,
-// 256 at a time, against a split of the prefix, where no key is masked.  Read by
+// GPU design.  The tile kernel is that of tree_attn.hip, whose comments describe it;
+// its items are of two kinds: the rows of one sequence against a split of its own
+// keys, and the rows of a whole group, 256 at a time, against a split of the prefix,
+// where no key is masked.  Read by
 // every sequence, the prefixes of a batch of single tokens are most of its bytes.
 // A plan kernel (one workgroup) finds the groups' members, the keys that they can
 // share -- whole pages, no further than the shortest member's context -- and the
 // items, longest first; the combine kernel of attn.h joins the parts.
-#include "attn_bf16.h"
+#include "attn.h"
 
 namespace {
+
+struct SharedArgs : AttnBase {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* bt;
+  const int32_t* parent;
+  int32_t page, page_shift, max_pages;
+  int64_t num_pages;
+  float scale_log2;
+  // what the plan kernel works out
+  int4* group;           // [n_groups] first sequence, shared keys, first entry of its nodes, nodes
+  int32_t* seq_prefix;   // [B] keys that the sequence's group takes for it
+  int32_t* node_of;      // live nodes of the sharing sequences, group by group: sequence << 8 | node
+};
+constexpr uint32_t kPrefixItem = 1u << 31;  // of an item's first word: sequence or group | row block << 16
+
+// Buffer descriptor over `nbytes` bytes at `base` (loads past nbytes read 0).
+__device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const uint16_t* base, int nbytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, nbytes, 0x00020000);
+}
+
+// kLoads 16-byte loads through one descriptor: lane byte offset voff plus
+// j * step for load j.
+template <int kLoads, int kStep>
+__device__ inline void buffer_load16(const uint16_t* base, int nbytes, int voff, uint4 (&r)[kLoads]) {
+  const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(base, nbytes);
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const i32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff + j * kStep, 0, 0);
+    r[j] = __builtin_bit_cast(uint4, x);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) {
+  using Sh = Shape<D>;
+  constexpr int CPR = Sh::CPR;
+  __shared__ __attribute__((aligned(16))) uint8_t Ks[2 * Sh::KTILE];
+  __shared__ __attribute__((aligned(16))) uint8_t Vs[2 * Sh::VTILE];
+  __shared__ uint64_t anc[kMaxN][4];
+  __shared__ int32_t spar[kMaxN];
+
+  const int tid = threadIdx.x;
+  const int w = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE);  // wave-uniform, in an SGPR
+  const int lane = tid % SRT_WAVE;
+  const int l32 = lane % 32;  // query row of this lane inside the wave's 32
+  const int h = lane / 32;    // lane half
+
+  // `b`: a sequence, or a group whose rows take a split of their shared prefix.
+  auto run_item = [&](const int b, const int g, const int s, const int rb, const bool prefix) {
+  SeqInfo si;
+  int4 group;
+  int k0 = 0, part = s, nsplit, b_table = b;  // first key, partial result, partial results, block table's row
+  if (prefix) {
+    group = a.group[b];
+    si = {group.w, group.y, group.y};  // (no key of theirs is masked)
+    nsplit = 2;
+    b_table = group.x;
+  } else {
+    si = seq_info(a, b);
+    k0 = a.seq_prefix[b];
+    part += (k0 + a.chunk - 1) / a.chunk;
+    nsplit = part - s + (si.total - k0 + a.chunk - 1) / a.chunk;
+  }
+  const int rows = si.n * a.G;
+  if (rb * kRowsPerBlock >= rows) return;
+  const int k_begin = k0 + s * a.chunk;
+  if (k_begin >= si.total) return;
+  const int k_end = min(k_begin + a.chunk, si.total);
+  const int ntiles = (k_end - k_begin + kTile - 1) / kTile;
+  const int row0 = rb * kRowsPerBlock + w * kRowsPerWave;
+  const bool wave_active = row0 < rows;  // wave-uniform
+
+  // Ancestor-or-self bitsets, needed only when this split reaches the tree.
+  if (k_end > si.L) {
+    for (int i = tid; i < si.n; i += kThreads) spar[i] = a.parent[static_cast<int64_t>(b) * a.N + i];
+    __syncthreads();
+    for (int i = tid; i < si.n; i += kThreads) {
+      uint64_t bits[4] = {0, 0, 0, 0};
+      int j = i;
+      while (j >= 0) {
+        bits[j >> 6] |= 1ull << (j & 63);
+        const int pj = spar[j];
+        if (pj >= j) break;  // malformed parent: stop (parents precede children)
+        j = pj;
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) anc[i][x] = bits[x];
+    }
+  }
+
+  // Query fragment: B operand of S^T = K Q^T; lane holds row l32 and head
+  // dims 16 ks + 8 h .. +7 for k-step ks.
+  const int row = row0 + l32;
+  const bool row_ok = row < rows;
+  int node = row_ok ? row / a.G : 0, b_row = b;  // of the sequence's tree, and the sequence
+  if (prefix) {
+    const int e = a.node_of[group.z + node];
+    node = e & 255;
+    b_row = e >> 8;
+  }
+  bf16x8 qf[Sh::KS];
+  {
+    const int hq = g * a.G + (row_ok ? row % a.G : 0);
+    const bf16x8* qp =
+        reinterpret_cast<const bf16x8*>(a.q + ((static_cast<int64_t>(b_row) * a.N + node) * a.Hq + hq) * D + 8 * h);
+#pragma unroll
+    for (int ks = 0; ks < Sh::KS; ++ks) qf[ks] = row_ok ? qp[2 * ks] : bf16x8{};
+    // Q is used exactly as given: the scale is applied to the fp32 scores
+    // (rounding a scaled Q back to bf16 would perturb every score by up to
+    // 2^-9 of its magnitude).
+  }
+  const float c_log2 = a.scale_log2;  // scale * log2(e)
+
+  f32x16 o[Sh::DB];
+#pragma unroll
+  for (int db = 0; db < Sh::DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+  // Reference maximum (log2 units) and lane-partial sum of the row.  The
+  // reference is raised only when the row maximum exceeds it by more than
+  // kLazy, so most tiles need no rescale of O.
+  constexpr float kLazy = 8.f;
+  float m = -INFINITY;
+  float l = 0.f;
+
+  // ---- staging ----------------------------------------------------------
+  // Wave w moves keys 8w .. 8w+7 of every K and V tile; they lie inside one
+  // page (pages are powers of two >= 16), so one scalar buffer descriptor
+  // covers exactly the valid keys and keys past the split end or on an
+  // invalid page read as zero.  Loads go to registers one tile ahead and are
+  // stored to LDS after the tile's compute.
+  const int pshift = a.page_shift;
+  const int pmask = (1 << pshift) - 1;
+  const int64_t bt_row = static_cast<int64_t>(b_table) * a.max_pages;
+  const int64_t head_stride = static_cast<int64_t>(a.page) * D;  // elements per (page, head)
+  constexpr int kRowsPerLoad = SRT_WAVE / CPR;                    // 4 (d=128) or 8 (d=64)
+  constexpr int kLoadsPerWave = kSubRows / kRowsPerLoad;          // per tile, per tensor
+  static_assert(kLoadsPerWave >= 1 && kSubRows % kRowsPerLoad == 0, "staging shape");
+  const int st_row = kSubRows * w + lane / CPR;  // tile row of this lane's first chunk
+  const int gl_off = ((lane / CPR) * D + (lane % CPR) * 8) * 2;
+  const int k_st = st_row * Sh::KSTRIDE + (lane % CPR) * 16;
+  const int v_st = st_row * Sh::VSTRIDE + (lane % CPR) * 16;
+
+  // Page ids of this wave's sub-block of every tile of the split, one tile
+  // per lane and register (a split has 128 tiles), fetched once; the loop
+  // reads them with v_readlane and touches no block-table memory.
+  static_assert(kChunk / kTile == 2 * SRT_WAVE, "two registers of page ids per split (of at most kChunk keys)");
+  int pg_lane[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int p0 = k_begin + kTile * (SRT_WAVE * j + lane) + kSubRows * w;
+    pg_lane[j] = p0 < k_end ? a.bt[bt_row + (p0 >> pshift)] : -1;
+  }
+  auto page_of = [&](int it) {
+    if (it >= ntiles) return -1;
+    return it < SRT_WAVE ? __builtin_amdgcn_readlane(pg_lane[0], it)
+                         : __builtin_amdgcn_readlane(pg_lane[1], it - SRT_WAVE);
+  };
+  uint4 kreg[kLoadsPerWave], vreg[kLoadsPerWave];
+  auto load_sub = [&](const uint16_t* base, int t0, int pg, uint4 (&r)[kLoadsPerWave]) {
+    const int p0 = t0 + kSubRows * w;
+    const bool ok = pg >= 0 && pg < a.num_pages && p0 < k_end;
+    const int nbytes = ok ? min(kSubRows, k_end - p0) * D * 2 : 0;
+    const int64_t off = ok ? (static_cast<int64_t>(pg) * a.Hkv + g) * head_stride + (p0 & pmask) * D : 0;
+    buffer_load16<kLoadsPerWave, kRowsPerLoad * D * 2>(base + off, nbytes, gl_off, r);
+  };
+  auto store_k = [&](uint8_t* Kb) {
+#pragma unroll
+    for (int j = 0; j < kLoadsPerWave; ++j) *reinterpret_cast<uint4*>(Kb + k_st + j * kRowsPerLoad * Sh::KSTRIDE) = kreg[j];
+  };
+  auto store_v = [&](uint8_t* Vb) {
+#pragma unroll
+    for (int j = 0; j < kLoadsPerWave; ++j) *reinterpret_cast<uint4*>(Vb + v_st + j * kRowsPerLoad * Sh::VSTRIDE) = vreg[j];
+  };
+
+  // ---- MFMA phases -------------------------------------------------------
+  // K operand (A of S^T): lane reads key l32 (+32 kb), head dims
+  // 16 ks + 8 h .. +7.
+  const int k_rd = l32 * Sh::KSTRIDE + 16 * h;
+  // V^T operand (A of O^T) by transposing reads: in each 16-lane group G,
+  // lane x addresses key 16 ks + 4 h + x/4 (+8 for the second half of the
+  // contraction) and head dims (D/2)(G%2) + 16 db + 4 (x%4) .. +3.
+  const int xg = lane % 16;
+  const int k_vd = (4 * h + xg / 4) * Sh::VSTRIDE + ((CPR / 2) * ((lane / 16) & 1) + (xg % 4) / 2) * 16 + 8 * (xg & 1);
+
+  // S^T[key][row] = q . k of one tile (raw fp32 dot products): two 32-key
+  // blocks.
+  auto qk = [&](const uint8_t* Kb, f32x16 (&sacc)[2]) {
+    // All fragment reads are issued before the first MFMA so that one LDS
+    // latency, not one per k-step, is exposed.
+    bf16x8 kf[Sh::KS][2];
+#pragma unroll
+    for (int ks = 0; ks < Sh::KS; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        kf[ks][kb] = *reinterpret_cast<const bf16x8*>(Kb + k_rd + kb * 32 * Sh::KSTRIDE + ks * 32);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[kb][r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < Sh::KS; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][kb], qf[ks], sacc[kb], 0, 0, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * Sh::KS, 0);  // DS reads
+    __builtin_amdgcn_sched_group_barrier(0x008, 2 * Sh::KS, 0);  // then MFMAs
+  };
+
+  // Mask, online softmax with lazy rescale; returns P in bf16.  Lane holds
+  // keys 32 kb + 8 (r/4) + 4 h + r%4 of its row in sacc[kb][r].
+  auto softmax = [&](int t0, f32x16 (&sacc)[2], bf16x8 (&pb)[4], float mref0) {
+    // Scores in log2 units relative to the reference: q.k * scale * log2(e)
+    // - mref0, one fp32 fused multiply-add per score (masked scores are set
+    // to -inf afterwards, so any finite scale is safe).
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[kb][r] = __builtin_fmaf(sacc[kb][r], c_log2, -mref0);
+    const bool need_mask = (t0 + kTile > si.L) || (t0 + kTile > k_end);
+    if (need_mask) {
+      // Visibility of keys t0 .. t0+63 for this lane's row as one 64-bit
+      // window: bit x is set iff key t0 + x < k_end and it is a context key
+      // or the tree position of an ancestor-or-self of the row's node.  (If
+      // the split ends before the tree, bits of tree positions are cleared
+      // by the k_end limit, so stale bitsets are never used.)
+      const int lim = k_end - t0;
+      uint64_t vis = lim >= 64 ? ~0ull : (lim <= 0 ? 0ull : (~0ull >> (64 - lim)));
+      const int j0 = t0 - si.L;  // tree index of key t0
+      if (j0 > -kTile) {
+        uint64_t win;
+        if (j0 >= 0) {
+          const int wd = j0 >> 6, sh = j0 & 63;
+          const uint64_t lo = wd < 4 ? anc[node][wd] : 0ull;
+          const uint64_t hi = wd + 1 < 4 ? anc[node][wd + 1] : 0ull;
+          win = sh ? (lo >> sh) | (hi << (64 - sh)) : lo;
+        } else {
+          const int sh = -j0;  // 1..63 context keys lead the window
+          win = (anc[node][0] << sh) | (~0ull >> (64 - sh));
+        }
+        vis &= win;
+      }
+      // lane half h holds keys 32 kb + 8 (r/4) + 4 h + r%4
+      const uint64_t vh = vis >> (4 * h);
+      const uint32_t v0 = static_cast<uint32_t>(vh), v1 = static_cast<uint32_t>(vh >> 32);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t vw = kb ? v1 : v0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int x = 8 * (r / 4) + r % 4;
+          sacc[kb][r] = ((vw >> x) & 1u) ? sacc[kb][r] : -INFINITY;
+        }
+      }
+    }
+    // Probabilities exp2(score - mref0 - dm), rounded to bf16 for the second
+    // product (sacc holds score - mref0); returns this lane's sum of them
+    // (its 32 keys of the row, two bf16 pairs per dot2, two accumulators).
+    // Contraction index 8 h + e of k-step ks <-> key 16 ks + 8 (e/4) + 4 h + e%4.
+    auto probs = [&](auto dm_c, float dm) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      const bf16x2 one2 = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+      float ps[2] = {0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          pb[ks][e] = static_cast<__bf16>(__builtin_amdgcn_exp2f(
+              decltype(dm_c)::value ? sacc[ks / 2][8 * (ks % 2) + e] - dm : sacc[ks / 2][8 * (ks % 2) + e]));
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const bf16x2 pr = {pb[ks][e], pb[ks][e + 1]};
+          ps[ks & 1] = __builtin_amdgcn_fdot2_f32_bf16(pr, one2, ps[ks & 1], false);
+        }
+      }
+      return ps[0] + ps[1];
+    };
+    // Fast path: exponentiate against the current reference without first
+    // taking the row maximum.  If every rounded probability of the row is
+    // below 2^kLazy (their sum is), no score exceeds the reference by kLazy,
+    // so the reference would not be raised and these are the final values.
+    // Otherwise (or while the reference is still -inf) the wave takes the
+    // row maximum, raises the reference as needed and exponentiates again.
+    float psum = probs(std::false_type(), 0.f);
+    const bool fast = m != -INFINITY && psum < 256.f;  // 256 = 2^kLazy
+    if (__ballot(!fast)) {
+      // (maximum, not fmaxf: no NaN-quieting of every operand; scores are
+      // finite or -inf)
+      float mloc = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; r += 2)
+          mloc = __builtin_elementwise_maximum(mloc, __builtin_elementwise_maximum(sacc[kb][r], sacc[kb][r + 1]));
+      mloc = max_halves(mloc);
+      const float ms = mloc + mref0;  // row max in log2 units
+      const bool raise = ms > m + kLazy;
+      if (__ballot(raise)) {
+        const float mnew = raise ? ms : m;
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < Sh::DB; ++db) o[db] *= alpha;
+        m = mnew;
+      }
+      psum = probs(std::true_type(), (m == -INFINITY ? 0.f : m) - mref0);
+    }
+    l += psum;
+  };
+
+  // O^T[d][row] += V^T P^T.
+  // V^T fragments of k-steps ks0, ks0+1 (two transposing reads per MFMA).
+  typedef short i16x4v __attribute__((ext_vector_type(4)));
+  auto v_read = [&](const uint8_t* Vb, int ks0, i16x4v (&vf)[2][Sh::DB][2]) {
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+      for (int db = 0; db < Sh::DB; ++db)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+          vf[k2][db][hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) i16x4v*)(Vb + k_vd + (ks0 + k2) * 16 * Sh::VSTRIDE +
+                                                          hh * 8 * Sh::VSTRIDE + db * 32));
+  };
+  auto pv = [&](const i16x4v (&vf)[2][Sh::DB][2], int ks0, const bf16x8 (&pb)[4]) {
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+      for (int db = 0; db < Sh::DB; ++db) {
+        const bf16x8 va =
+            __builtin_bit_cast(bf16x8, __builtin_shufflevector(vf[k2][db][0], vf[k2][db][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[ks0 + k2], o[db], 0, 0, 0);
+      }
+  };
+
+  // ---- tile loop ---------------------------------------------------------
+  // Iteration t: global loads of tile t+1 are issued to registers; the K
+  // fragments of tile t are read from LDS and S = K Q^T runs; the V^T
+  // fragments are read while softmax runs on the VALU; O += V^T P^T; then
+  // tile t+1 is stored into the buffers tile t-1 left.  One barrier per tile.
+  {
+    const int pg0 = page_of(0);
+    load_sub(a.k, k_begin, pg0, kreg);
+    load_sub(a.v, k_begin, pg0, vreg);
+    store_k(Ks);
+    store_v(Vs);
+  }
+  __syncthreads();
+
+  auto step = [&](int it, auto cur_c) {
+    constexpr int cur = decltype(cur_c)::value;
+    const int t0 = k_begin + it * kTile;
+    const bool next = it + 1 < ntiles;
+    if (next) {
+      const int pg = page_of(it + 1);
+      load_sub(a.k, t0 + kTile, pg, kreg);
+      load_sub(a.v, t0 + kTile, pg, vreg);
+    }
+    if (wave_active) {
+      f32x16 sacc[2];
+      const float mref0 = m == -INFINITY ? 0.f : m;
+      qk(Ks + cur * Sh::KTILE, sacc);
+      // First half of the V^T fragments is read while softmax runs, the
+      // second half while the first half's MFMAs run.
+      i16x4v vf0[2][Sh::DB][2], vf1[2][Sh::DB][2];
+      v_read(Vs + cur * Sh::VTILE, 0, vf0);
+      bf16x8 pb[4];
+      softmax(t0, sacc, pb, mref0);
+      v_read(Vs + cur * Sh::VTILE, 2, vf1);
+      pv(vf0, 0, pb);
+      pv(vf1, 2, pb);
+    }
+    if (next) {
+      store_k(Ks + (cur ^ 1) * Sh::KTILE);
+      store_v(Vs + (cur ^ 1) * Sh::VTILE);
+    }
+    __syncthreads();
+  };
+  for (int it = 0; it < ntiles; it += 2) {
+    step(it, std::integral_constant<int, 0>());
+    if (it + 1 < ntiles) step(it + 1, std::integral_constant<int, 1>());
+  }
+
+  // Epilogue: lane holds row l32 and, for block db and quad q = r/4, head
+  // dims (D/2)(q/2) + 16 db + 8 (q%2) + 4 h + 0..3.
+  const float lt = sum_halves(l);
+  if (!row_ok) return;
+  const int RBR = a.part_rows;
+  if (nsplit == 1) {
+    const int hq = g * a.G + row % a.G;
+    uint16_t* op = a.out + ((static_cast<int64_t>(b_row) * a.N + node) * a.Hq + hq) * D + 4 * h;
+    const float inv = lt > 0.f ? 1.f / lt : 0.f;
+#pragma unroll
+    for (int db = 0; db < Sh::DB; ++db) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int d0 = (D / 2) * (q / 2) + 16 * db + 8 * (q % 2);
+        const uint32_t x0 =
+            to_bf16_bits(o[db][4 * q] * inv) | (uint32_t(to_bf16_bits(o[db][4 * q + 1] * inv)) << 16);
+        const uint32_t x1 =
+            to_bf16_bits(o[db][4 * q + 2] * inv) | (uint32_t(to_bf16_bits(o[db][4 * q + 3] * inv)) << 16);
+        *reinterpret_cast<uint2*>(op + d0) = make_uint2(x0, x1);
+      }
+    }
+  } else {
+    const int64_t prow = ((static_cast<int64_t>(b_row) * a.Hkv + g) * a.S + part) * RBR +
+                         (prefix ? node * a.G + row % a.G : row);
+    float* po = a.part_o + prow * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < Sh::DB; ++db) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int d0 = (D / 2) * (q / 2) + 16 * db + 8 * (q % 2);
+        *reinterpret_cast<f32x4*>(po + d0) = f32x4{o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
+      }
+    }
+    if (h == 0) {
+      a.part_ml[2 * prow] = m;
+      a.part_ml[2 * prow + 1] = lt;
+    }
+  }
+  };
+
+  // Persistent workgroups: each takes the next item of the work list until
+  // the list is exhausted.
+  __shared__ int32_t s_item;
+  const int n_items = a.plan[0];
+  for (;;) {
+    if (tid == 0) s_item = atomicAdd(a.plan + 1, 1);
+    __syncthreads();
+    const int idx = s_item;
+    if (idx >= n_items) break;
+    const int b = a.plan[kPlanHeader + 2 * idx];
+    const int packed = a.plan[kPlanHeader + 2 * idx + 1];
+    run_item(b & 0xffff, packed & 0xff, packed >> 8, (b >> 16) & 0x7fff, static_cast<uint32_t>(b) & kPrefixItem);
+    __syncthreads();  // LDS and s_item are reused by the next item
+  }
+}
+
 
 constexpr int kMaxGroups = 4096;   // groups of a batch, whose counts are held in LDS
 constexpr int kPlanThreads = 1024;
@@ -291,8 +734,8 @@ extern "C" int srt_tree_attn_shared(int32_t B, int32_t N, int32_t Hq, int32_t Hk
   const unsigned grid = static_cast<unsigned>(std::min<int64_t>(z.items, cus));
   hipStream_t s = as_stream(stream);
   shared_plan_kernel<<<1, kPlanThreads, 0, s>>>(a, PlanArgs{group_ids, prefix_len, n_groups});
-  if (d == 128) tree_attn_kernel<128, false, SharedArgs><<<grid, kThreads, 0, s>>>(a);
-  else tree_attn_kernel<64, false, SharedArgs><<<grid, kThreads, 0, s>>>(a);
+  if (d == 128) shared_attn_kernel<128><<<grid, kThreads, 0, s>>>(a);
+  else shared_attn_kernel<64><<<grid, kThreads, 0, s>>>(a);
   launch_combine(a, d, false, static_cast<unsigned>(combine_grid(a, cus)), s);
   return launch_status();
 }
