@@ -30,16 +30,17 @@
 namespace {
 
 constexpr int kList = 4096;       // candidates that are sorted in LDS
-constexpr int kBins = 2048;       // of a histogram over a range of the score
+constexpr int kDraws = 12;        // of a long list's choice, before the last kept token is searched for
 constexpr int kSegs = 16;         // segments of a thread, at most
-constexpr int kUnroll = 5;        // quartets of a thread that are under way together
-constexpr int kMost = 1024;       // threads
-constexpr int kSegBins = 1024;    // of the segments' maxima, 1 / 16 of the score wide
+constexpr int kUnroll = 8;        // quartets of a thread in a batch
+constexpr int kAgain = 4;         // quartets of a thread that are read again together
+constexpr int kMost = 512;        // threads
+constexpr int kSegBins = 512;     // of the segments' maxima, 1 / 8 of the score wide
+constexpr int kMassBits = 44;     // of a bin's word: mass in units of 2^-24 below, count above
 constexpr int64_t kMaxVocab = int64_t(1) << 21;
 constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LDS
-constexpr int kShortVocab = 8192;  // rows up to which 256 threads walk
+constexpr int kShortVocab = 4096;  // rows up to which 256 threads walk
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr uint32_t kNothing = 0x007f;  // key16 of -inf
 
 struct SampleArgs : RulesArgs {
   const float* inv_temperature;
@@ -50,35 +51,48 @@ struct SampleArgs : RulesArgs {
 
 typedef unsigned long long u64;
 
-__device__ inline uint32_t key16(float x) { return static_cast<uint32_t>(pack_key(x, 0) >> 48); }
-// A float that is no larger than any that has this key16.
-__device__ inline float floor16(uint32_t k) {
-  const uint32_t u = k << 16;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+__device__ __forceinline__ double shfl_xor_f64(double v, int m) {
+  return __builtin_bit_cast(double, shfl_xor_u64(__builtin_bit_cast(u64, v), m));
+}
+
+// Inclusive prefix sum over the wave.
+__device__ __forceinline__ u64 wave_scan(u64 x, int lane) {
+#pragma unroll
+  for (int d = 1; d < SRT_WAVE; d <<= 1) {
+    const u64 y = __shfl_up(x, d, SRT_WAVE);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+__device__ __forceinline__ double wave_scan(double x, int lane) {
+#pragma unroll
+  for (int d = 1; d < SRT_WAVE; d <<= 1) {
+    const double y = __builtin_bit_cast(double, __shfl_up(__builtin_bit_cast(u64, x), d, SRT_WAVE));
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+__device__ __forceinline__ float score_of(u64 key) {
+  const uint32_t u = static_cast<uint32_t>(key >> 32);
   return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-
-__device__ inline double shfl_xor_f64(double v, int m) { return __builtin_bit_cast(double, shfl_xor_u64(__builtin_bit_cast(u64, v), m)); }
-
 // What the workgroup shares.
 struct Lds {
-  union {
-    u64 list[kList];               // packed candidates (score, token)
-    struct {
-      u64 mass[kBins];             // in units of 2^-40 of the row's largest weight
-      uint32_t count[kBins];
-    } hist;
-  };
-  uint16_t seg[kSegs * kMost];
+  u64 list[kList];  // packed candidates (score, token)
+  float seg[kSegs * kMost];
+  u64 segbin[kSegBins];
   Path path;
   int32_t par[kMaxN], tok[kMaxN];
-  u64 red[kMost / SRT_WAVE];
-  double redd[kMost / SRT_WAVE];
+  u64 red[2][kMost / SRT_WAVE];
+  double redd[2][kMost / SRT_WAVE];
+  float redm[kMost / SRT_WAVE];
   u64 found;
-  double before;
-  int32_t bin, n;
-  uint32_t lo, hi;
+  uint16_t work[kList];  // segments that are read again
+  int32_t n, m;
 };
 
 template <bool kRules>
@@ -89,7 +103,9 @@ struct Walker {
   Row w;
   int n;                 // tokens emitted on this walk
   int tid, threads, lane, wave, waves;
-  int e4, seg_batches;   // quartets of a row; batches of a segment
+  int e4, full;          // quartets of a row; batches that are whole
+  int seg_batches, batch_segs;  // batches of a segment, or segments of a batch
+  int parity;            // of the reductions' arrays: the next one's writes meet no reads of the last one's
   float M;               // largest score of the row
 
   // Score of a logit under the rules; a NaN counts as -inf.
@@ -99,42 +115,51 @@ struct Walker {
   }
   __device__ __forceinline__ bool marked(int j) const { return kRules && ((skip[j >> 5] >> (j & 31)) & 1u); }
 
-  // Scores of the batch of quartets i, i + threads, .. (-inf: none, or marked).
-  __device__ __forceinline__ void batch(int i, float (&z)[4 * kUnroll], float (*g)[4 * kUnroll]) const {
+  // A batch: quartets i, i + threads, .. of a row, i the thread's first.
+  struct Batch {
+    f32x4 x[kUnroll], g[kUnroll];
+    u16x4 c[kUnroll];
+  };
+  __device__ __forceinline__ int first_of(int b) const { return b * kUnroll * threads + tid; }
+  __device__ __forceinline__ int batches() const { return full + (full * kUnroll * threads < e4); }
+
+  // The batch's loads.  Quartets behind the row's end read the thread's first one's line.
+  template <bool kNoise>
+  __device__ __forceinline__ void load(int b, Batch& t) const {
     const f32x4u* r4 = reinterpret_cast<const f32x4u*>(w.logits);
     const f32x4u* g4 = reinterpret_cast<const f32x4u*>(w.noise);
     const u16x4* s4 = reinterpret_cast<const u16x4*>(w.seen);
-    f32x4 x[kUnroll];
-    u16x4 c[kUnroll];
-    uint32_t out[kUnroll];
+    const int i = first_of(b);
+    if (i >= e4) return;
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int at = i + k * threads < e4 ? i + k * threads : i;
+      t.x[k] = r4[at];
+      if (kNoise) t.g[k] = g4[at];
+      if (kRules && w.seen) t.c[k] = s4[at];
+    }
+  }
+  // Its scores (-inf: none, or marked).
+  __device__ __forceinline__ void scores(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
+    const int i = first_of(b);
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       const int at = i + k * threads;
-      out[k] = at < e4 ? (kRules ? (skip[at >> 3] >> ((4 * at) & 31)) & 15u : 0u) : 15u;
-    }
+      uint32_t out = b < full || at < e4 ? 0u : 15u;
+      if (kRules && out == 0) out = (skip[at >> 3] >> ((4 * at) & 31)) & 15u;
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      const int at = out[k] == 15u ? i : i + k * threads;  // (the first one's line is read)
-      x[k] = r4[at];
-      c[k] = u16x4{0, 0, 0, 0};
-      if (kRules && w.seen) c[k] = s4[at];
-      if (g) {
-        const f32x4 y = g4[at];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) (*g)[4 * k + e] = y[e];
+      for (int e = 0; e < 4; ++e) {
+        const float x = scored(t.x[k][e], kRules && w.seen ? t.c[k][e] : 0);
+        z[4 * k + e] = (out >> e) & 1u ? -INFINITY : x;
       }
     }
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[4 * k + e] = (out[k] >> e) & 1u ? -INFINITY : scored(x[k][e], c[k][e]);
   }
-  __device__ __forceinline__ int token(int i, int q) const { return 4 * (i + q / 4 * threads) + q % 4; }
+  __device__ __forceinline__ int token(int b, int q) const { return 4 * (first_of(b) + q / 4 * threads) + q % 4; }
 
   // f(score, token) for the entries outside the quartets: the row's last one to
   // three and, under rules, the marked ones that are allowed.
-  template <typename F>
-  __device__ __forceinline__ void extras(F f) const {
+  template <typename Fn>
+  __device__ __forceinline__ void extras(Fn f) const {
     const int j = 4 * e4 + tid;
     if (j < a.V && !marked(j)) f(scored(w.logits[j], w.seen ? w.seen[j] : 0), j);
     if constexpr (kRules)
@@ -144,444 +169,532 @@ struct Walker {
       });
   }
 
-  // f(score, token) for every entry whose score can be `least` or more.
-  template <typename F>
-  __device__ __forceinline__ void visit(float least, F f) const {
-    const uint32_t from = key16(least);
-    int b = 0;
-    for (int i = tid; i < e4; i += kUnroll * threads, ++b) {
-      if (s.seg[b / seg_batches * threads + tid] < from) continue;
+  // Whether the thread has an entry of score `least` or more in a batch.
+  __device__ __forceinline__ bool reaches(int b, float least) const {
+    if (first_of(b) >= e4) return false;
+    bool any = false;
+    for (int g = 0; g < batch_segs; ++g) any |= s.seg[(b / seg_batches * batch_segs + g) * threads + tid] >= least;
+    return any;
+  }
+
+  // f(score, token) for every entry of score `least` and more.
+  template <typename Fn>
+  __device__ __forceinline__ void visit(float least, Fn f) const {
+    const int n_b = batches();
+    for (int b = 0; b < n_b; ++b) {
+      if (!reaches(b, least)) continue;
+      Batch t;
       float z[4 * kUnroll];
-      batch(i, z, nullptr);
+      load<false>(b, t);
+      scores(b, t, z);
 #pragma unroll
       for (int q = 0; q < 4 * kUnroll; ++q)
-        if (z[q] >= least && z[q] > -INFINITY) f(z[q], token(i, q));
+        if (z[q] >= least && z[q] > -INFINITY) f(z[q], token(b, q));
     }
     extras([&](float z, int j) {
       if (z >= least && z > -INFINITY) f(z, j);
     });
   }
 
-  // The workgroup's largest.  Synchronises, before as well.
-  __device__ __forceinline__ u64 all_max(u64 key) const {
-    key = wave_max(key);
-    __syncthreads();
-    if (lane == 0) s.red[wave] = key;
-    __syncthreads();
-    return wave_max(lane < waves ? s.red[lane] : 0ull);
+  // Appends a token to the list where `in`; s.n counts all, also those that find no room.
+  __device__ __forceinline__ void append(bool in, float z, int j) const {
+    const u64 lanes = __ballot(in);
+    if (!lanes) return;
+    int at = 0;
+    if (lane == __ffsll(static_cast<long long>(lanes)) - 1) at = atomicAdd(&s.n, __popcll(lanes));
+    at = __shfl(at, __ffsll(static_cast<long long>(lanes)) - 1, SRT_WAVE) +
+         static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32),
+                                                    __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0)));
+    if (in && at < kList) s.list[at] = pack_key(z, j);
   }
-  __device__ __forceinline__ double all_sum(double x) const {
+
+  // The tokens of score `least` and more as the list, and how many there are (more
+  // than kList: at least that many).  The segments that reach it are listed first and
+  // their quartets dealt out to all threads: where a thread reads its own ones again,
+  // nearly every wave has one in each batch, and waits for each in turn (15 us of a
+  // 152k row's 27).  s.n and s.m have been cleared.
+  __device__ __forceinline__ int collect(float least) {
+    const int per = kUnroll * seg_batches / batch_segs;  // quartets of a segment
+    const int segs = (batches() + seg_batches - 1) / seg_batches * batch_segs;
+    for (int i = 0; i < segs; ++i) {
+      const int id = i * threads + tid;
+      const float top = s.seg[id];
+      const u64 lanes = __ballot(top >= least && top > -INFINITY);
+      if (!lanes) continue;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s.m, __popcll(lanes));
+      at = __builtin_amdgcn_readfirstlane(at) +
+           static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32),
+                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0)));
+      if (((lanes >> lane) & 1) && at < kList) s.work[at] = static_cast<uint16_t>(id);
+    }
+    __syncthreads();
+    const int m = s.m;
+    if (m > kList) return m;  // (each has a token)
+    const f32x4u* r4 = reinterpret_cast<const f32x4u*>(w.logits);
+    for (int i0 = 0; i0 < m * per; i0 += kAgain * threads) {
+      f32x4 x[kAgain];
+      int at[kAgain];
+#pragma unroll
+      for (int k = 0; k < kAgain; ++k) {
+        const int i = i0 + k * threads + tid;
+        at[k] = e4;
+        if (i < m * per) {
+          const int id = s.work[i / per], o = id / threads;
+          at[k] = (o * per + i % per) * threads + (id - o * threads);
+        }
+        if (at[k] < e4) x[k] = r4[at[k]];
+      }
+#pragma unroll
+      for (int k = 0; k < kAgain; ++k) {
+        const bool on = at[k] < e4;
+        const uint32_t out = kRules && on ? skip[at[k] >> 3] >> ((4 * at[k]) & 31) : 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = 4 * at[k] + e;
+          const bool in = on && !((out >> e) & 1u);
+          const float z = in ? scored(x[k][e], kRules && w.seen ? w.seen[j] : 0) : -INFINITY;
+          append(z >= least && z > -INFINITY, z, j);
+        }
+      }
+      if (*const_cast<volatile int32_t*>(&s.n) > kList) break;  // (each wave by itself)
+    }
+    extras([&](float z, int j) {
+      if (!(z >= least) || z == -INFINITY) return;
+      const int at = atomicAdd(&s.n, 1);
+      if (at < kList) s.list[at] = pack_key(z, j);
+    });
+    __syncthreads();
+    return s.n;
+  }
+
+  // The workgroup's largest.
+  __device__ __forceinline__ u64 all_max(u64 key) {
+    key = wave_max(key);
+    if (lane == 0) s.red[parity][wave] = key;
+    __syncthreads();
+    key = wave_max(lane < waves ? s.red[parity][lane] : 0ull);
+    parity ^= 1;
+    return key;
+  }
+  // The workgroup's sum; the terms are added in the same order always.
+  __device__ __forceinline__ double all_sum(double x) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) x += shfl_xor_f64(x, off);
+    if (lane == 0) s.redd[parity][wave] = x;
     __syncthreads();
-    if (lane == 0) s.redd[wave] = x;
-    __syncthreads();
-    x = lane < waves ? s.redd[lane] : 0.0;
+    x = lane < waves ? s.redd[parity][lane] : 0.0;
+    parity ^= 1;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) x += shfl_xor_f64(x, off);
     return x;
   }
 
-  // arg-max of score (or of the logit, without noise) plus noise over the row.
-  __device__ __forceinline__ u64 plain() const {
-    Top best;
-    u64 key = 0;
-    for (int i = tid; i < e4; i += kUnroll * threads) {
-      float z[4 * kUnroll], g[4 * kUnroll];
-      batch(i, z, w.noise ? &g : nullptr);
-#pragma unroll
-      for (int q = 0; q < 4 * kUnroll; ++q) best.ascending(w.noise ? add_rounded(z[q], g[q]) : z[q], token(i, q));
-    }
-    extras([&](float z, int j) { take(key, z, j); });
-    return all_max(max(key, best.key()));
-  }
   __device__ __forceinline__ void take(u64& key, float z, int j) const {
     const float x = w.noise ? add_rounded(z, w.noise[j]) : z;
     if (x > -INFINITY) key = max(key, pack_key(x, j));
   }
 
-  // The pass over the row: M, the segments' maxima, and the row's mass in units of
-  // the largest weight.  M is -inf where nothing is left.
+  // arg-max of score (or of the logit, without noise) plus noise over the row.  The
+  // loads of a batch are under way while the one before is scored.
+  template <bool kNoise>
+  __device__ __forceinline__ u64 plain() {
+    Top best;
+    u64 key = 0;
+    Batch t;
+    load<kNoise>(0, t);
+    const int n_b = batches();
+    for (int b = 0; b < n_b; ++b) {
+      Batch next;
+      if (b + 1 < n_b) load<kNoise>(b + 1, next);
+      float z[4 * kUnroll];
+      scores(b, t, z);
+#pragma unroll
+      for (int q = 0; q < 4 * kUnroll; ++q) best.ascending(kNoise ? add_rounded(z[q], t.g[q / 4][q % 4]) : z[q], token(b, q));
+      t = next;
+    }
+    extras([&](float z, int j) { take(key, z, j); });
+    return all_max(max(key, best.key()));
+  }
+
+  // The pass over the row: M (-inf where nothing is left), the segments' maxima and,
+  // if it is asked for, the row's mass in units of the largest weight.
+  template <bool kMass>
   __device__ __forceinline__ double first_pass() {
-    float m = -INFINITY, sum = 0.f, seg = -INFINITY;
-    int b = 0;
+    float m = -INFINITY, seg = -INFINITY;
+    double sum = 0.0;  // of parts of a batch each
     auto add = [&](float top) {  // the running maximum goes up to `top`
       if (top > m) {
-        sum *= exp_of(m - top);
+        if (kMass) sum *= exp_of(m - top);
         m = top;
       }
     };
-    for (int i = tid; i < e4; i += kUnroll * threads, ++b) {
-      float z[4 * kUnroll];
-      batch(i, z, nullptr);
-      float top = z[0];
+    Batch t, next;
+    load<false>(0, t);
+    const int n_b = batches();
+    if (n_b > 1) load<false>(1, next);
+    for (int b = 0; b < n_b; ++b) {
+      Batch later;
+      if (b + 2 < n_b) load<false>(b + 2, later);
+      if (first_of(b) < e4) {
+        float z[4 * kUnroll];
+        scores(b, t, z);
+        float top = z[0];
 #pragma unroll
-      for (int q = 1; q < 4 * kUnroll; ++q) top = __builtin_fmaxf(top, z[q]);
-      add(top);
-      const float ref = m == -INFINITY ? 0.f : m;
-      float part = 0.f;
+        for (int q = 1; q < 4 * kUnroll; ++q) top = __builtin_fmaxf(top, z[q]);
+        add(top);
+        if (kMass) {
+          // (the difference first: a large score's product with log2(e) has lost what parts it from the maximum)
+          const float ref = m == -INFINITY ? 0.f : m;
+          float part[2] = {0.f, 0.f};
 #pragma unroll
-      for (int q = 0; q < 4 * kUnroll; ++q) part += exp_of(z[q] - ref);
-      sum += part;
-      seg = __builtin_fmaxf(seg, top);
-      if ((b + 1) % seg_batches == 0 || i + kUnroll * threads >= e4) {
-        s.seg[b / seg_batches * threads + tid] = static_cast<uint16_t>(key16(seg));
+          for (int q = 0; q < 4 * kUnroll; ++q) part[q & 1] += exp_of(z[q] - ref);
+          sum += part[0] + part[1];
+        }
+        if (batch_segs == 1) seg = __builtin_fmaxf(seg, top);
+        else
+#pragma unroll
+          for (int k = 0; k < kUnroll; ++k) {
+            const float four = __builtin_fmaxf(__builtin_fmaxf(z[4 * k], z[4 * k + 1]), __builtin_fmaxf(z[4 * k + 2], z[4 * k + 3]));
+            seg = __builtin_fmaxf(seg, four);
+            if ((k + 1) * batch_segs % kUnroll == 0) {
+              s.seg[(b * batch_segs + k * batch_segs / kUnroll) * threads + tid] = seg;
+              seg = -INFINITY;
+            }
+          }
+      } else if (batch_segs > 1) {
+        for (int g = 0; g < batch_segs; ++g) s.seg[(b * batch_segs + g) * threads + tid] = -INFINITY;
+      }
+      if (batch_segs == 1 && ((b + 1) % seg_batches == 0 || b + 1 == n_b)) {
+        s.seg[b / seg_batches * threads + tid] = seg;
         seg = -INFINITY;
       }
+      t = next;
+      next = later;
     }
     extras([&](float z, int) {
       add(z);
-      if (z > -INFINITY) sum += exp_of(z - m);
+      if (kMass && z > -INFINITY) sum += exp_of(z - m);
     });
-    const u64 top = all_max(m > -INFINITY ? pack_key(m, 0) : 0ull);
-    if (!top) {
-      M = -INFINITY;
-      return 0.0;
+    // Join: first the wave's lanes, then the waves.
+    float top = m;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) top = __builtin_fmaxf(top, shfl_xor(top, off));
+    double part = 0.0;
+    if (kMass) {
+      part = m > -INFINITY ? sum * exp_of(m - top) : 0.0;
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) part += shfl_xor_f64(part, off);
     }
-    const uint32_t u = static_cast<uint32_t>(top >> 32);
-    M = __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
-    // (m and M are finite here or M is +inf, where the sum is not used)
-    return all_sum(m > -INFINITY ? static_cast<double>(sum) * exp(static_cast<double>(m) - static_cast<double>(M)) : 0.0);
+    if (lane == 0) {
+      s.redm[wave] = top;
+      if (kMass) s.redd[0][wave] = part;
+    }
+    __syncthreads();
+    const float mine = lane < waves ? s.redm[lane] : -INFINITY;
+    M = mine;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) M = __builtin_fmaxf(M, shfl_xor(M, off));
+    if (!kMass) return 0.0;
+    part = mine > -INFINITY ? s.redd[0][lane] * exp_of(mine - M) : 0.0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) part += shfl_xor_f64(part, off);
+    return part;
   }
 
   // A score that no kept token is below, from the segments' maxima: `k` of them
-  // are at least it, or their mass is at least `mass` of the row's.  -inf if neither is found.
+  // are at least it, or together weigh at least `mass`.  -inf if neither is found.
+  // The bins have been cleared; every wave takes the sums by itself.
   __device__ __forceinline__ float least_kept(int k, double mass) {
-    uint32_t* cnt = s.hist.count;
-    __syncthreads();
-    for (int i = tid; i < kSegBins; i += threads) cnt[i] = 0;
-    __syncthreads();
-    int b = 0;
-    for (int i = tid; i < e4; i += kUnroll * threads * seg_batches, ++b) {
-      const uint32_t key = s.seg[b * threads + tid];
-      if (key <= kNothing) continue;
-      const float d = (M - floor16(key)) * 16.f;
-      if (d < kSegBins - 1) atomicAdd(&cnt[static_cast<int>(d)], 1u);
+    const int segs = (batches() + seg_batches - 1) / seg_batches * batch_segs;
+    for (int i = 0; i < segs; ++i) {
+      const float x = s.seg[i * threads + tid], d = (M - x) * 8.f;
+      if (d < kSegBins)  // (not where x is -inf)
+        atomicAdd(&s.segbin[static_cast<int>(d)], (1ull << kMassBits) + static_cast<u64>(exp_of(x - M) * 16777216.f));
     }
     __syncthreads();
-    if (wave == 0) {
-      constexpr int kPer = kSegBins / SRT_WAVE;
-      int c = 0;
-      float x = 0.f;
-      for (int i = 0; i < kPer; ++i) {
-        const int bin = lane * kPer + i, n = cnt[bin];
-        c += n;
-        x += n * exp_of(-(bin + 1) / 16.f);
-      }
-      int c0 = c;
-      float x0 = x;
+    constexpr int kPer = kSegBins / SRT_WAVE;
+    constexpr u64 kMassMask = (1ull << kMassBits) - 1;
+    u64 x[kPer], sum = 0;
 #pragma unroll
-      for (int d = 1; d < SRT_WAVE; d <<= 1) {
-        const int y = __shfl_up(c0, d, SRT_WAVE);
-        const float v = __shfl_up(x0, d, SRT_WAVE);
-        if (lane >= d) c0 += y, x0 += v;
-      }
-      c0 -= c;
-      x0 -= x;
-      int found = kSegBins;
-      for (int i = 0; i < kPer && found == kSegBins; ++i) {
-        const int bin = lane * kPer + i, n = cnt[bin];
-        c0 += n;
-        x0 += n * exp_of(-(bin + 1) / 16.f);
-        // (the mass needs a margin for the roundings of its fp32 sum)
-        if (n && (c0 >= k || x0 >= mass * 1.0001)) found = bin;
-      }
-#pragma unroll
-      for (int d = SRT_WAVE / 2; d >= 1; d >>= 1) found = min(found, __shfl_xor(found, d, SRT_WAVE));
-      if (lane == 0) s.bin = found;
+    for (int i = 0; i < kPer; ++i) {
+      x[i] = s.segbin[lane * kPer + i];
+      sum += x[i];  // (16 segments of 512 threads: neither field runs over)
     }
-    __syncthreads();
-    return s.bin < kSegBins ? M - (s.bin + 2) / 16.f : -INFINITY;
+    u64 before = wave_scan(sum, lane) - sum;
+    // (a margin for the weights' roundings)
+    const u64 want = mass < 1e6 ? static_cast<u64>(mass * 16777216.0 * 1.00001) + 1 : ~0ull;
+    int found = kSegBins;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      before += x[i];
+      if (found == kSegBins && (static_cast<int64_t>(before >> kMassBits) >= k || (before & kMassMask) >= want))
+        found = lane * kPer + i;
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) found = min(found, shfl_xor(found, off));
+    return found < kSegBins ? M - (found + 1.01f) * 0.125f : -INFINITY;
   }
 
-  // Sorts the list's first `count` entries, largest first.
+  // Sorts the list's first `count` entries, largest first; returns with the list in
+  // order for wave 0, or for all where there are more than 128.  A wave's 64 pairs at
+  // a distance of up to 64 lie in 128 entries of its own: such steps need no barrier.
   __device__ __forceinline__ void sort(int count) const {
-    int size = 64;
+    int size = 128;
     while (size < count) size *= 2;
-    __syncthreads();
     for (int i = count + tid; i < size; i += threads) s.list[i] = 0;
     __syncthreads();
+    volatile u64* list = s.list;
     for (int run = 2; run <= size; run *= 2) {
       for (int d = run / 2; d >= 1; d /= 2) {
+        if (d > SRT_WAVE) __syncthreads();
         for (int t = tid; t < size / 2; t += threads) {
           const int i = 2 * t - (t & (d - 1)), j = i + d;
-          const u64 x = s.list[i], y = s.list[j];
+          const u64 x = list[i], y = list[j];
           if ((x < y) == ((i & run) == 0)) {
-            s.list[i] = y;
-            s.list[j] = x;
+            list[i] = y;
+            list[j] = x;
           }
         }
-        __syncthreads();
+        if (d > SRT_WAVE) __syncthreads();
       }
     }
+    if (size > 2 * SRT_WAVE) __syncthreads();
   }
 
-  __device__ __forceinline__ static float score_of(u64 key) {
-    const uint32_t u = static_cast<uint32_t>(key >> 32);
-    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
-  }
+  __device__ __forceinline__ double weight(float z) const { return exp(static_cast<double>(z) - static_cast<double>(M)); }
 
-  // Weight of a score in fixed point.
-  __device__ __forceinline__ u64 fixed(float z) const { return static_cast<u64>(exp_of(z - M) * 1099511627776.f); }
-
-  // The choice from a list that holds every token that can be kept (and, with both a
-  // top-k and a top-p, the first k tokens).
-  __device__ __forceinline__ u64 from_list(int count, int k, double p, double row_mass, float least) const {
-    sort(count);
-    const int per = (count + threads - 1) / threads;
-    double mine = 0.0;
-    for (int i = tid * per; i < min(tid * per + per, min(count, k)); ++i)
-      mine += exp(static_cast<double>(score_of(s.list[i])) - static_cast<double>(M));
-    // exclusive prefix sums over the workgroup
-    double incl = mine;
+  // The choice from a list of up to 64 tokens, by wave 0: a lane each.
+  __device__ __forceinline__ u64 from_short(int count, int k, double p, double row_mass, float least) {
+    u64 best = 0;
+    if (wave == 0) {
+      u64 x = lane < count ? s.list[lane] : 0ull;
 #pragma unroll
-    for (int d = 1; d < SRT_WAVE; d <<= 1) {
-      const u64 y = __shfl_up(__builtin_bit_cast(u64, incl), d, SRT_WAVE);
-      if (lane >= d) incl += __builtin_bit_cast(double, y);
-    }
-    if (lane == SRT_WAVE - 1) s.redd[wave] = incl;
-    __syncthreads();
-    double before = incl - mine, all = 0.0;
-    for (int j = 0; j < waves; ++j) {
-      if (j == wave) before += all;
-      all += s.redd[j];
-    }
-    const double target = p * (k < a.V ? all : row_mass);
-    u64 key = 0;
-    for (int i = tid * per; i < min(tid * per + per, min(count, k)); ++i) {
-      const u64 x = s.list[i];
+      for (int run = 2; run <= SRT_WAVE; run *= 2)
+#pragma unroll
+        for (int d = run / 2; d >= 1; d /= 2) {
+          const u64 y = shfl_xor_u64(x, d);
+          const bool larger = ((lane & d) == 0) == ((lane & run) == 0);  // keeps the larger one
+          x = (x > y) == larger ? x : y;
+        }
       const float z = score_of(x);
-      if (i > 0 && (!(p >= 1.0 || before < target) || z < least)) break;
-      take(key, z, key_token(x));
-      before += exp(static_cast<double>(z) - static_cast<double>(M));
-    }
-    return all_max(key);
-  }
-
-  // Packed (score, token) of the last token, from the top, at which the count of
-  // tokens (kMass false) or their mass in fixed point reaches `target`; 0 if none does.
-  // Only tokens of `least` and more are looked at.
-  template <bool kMass>
-  __device__ __forceinline__ u64 border(double target, float least) {
-    float top = M, low = least;  // scores of the range
-    double base = 0.0;           // measure of the tokens above it
-    bool first = true;
-    for (;;) {
-      const float end = first ? __builtin_fmaxf(low, M - 64.f) : low;  // (what lies below falls into the last bin)
-      first = false;
-      if (!(end < top)) return ties<kMass>(top, target, base);
-      const double scale = kBins / (static_cast<double>(top) - static_cast<double>(end));
-      auto bin_of = [&](float z) { return static_cast<int>(fmin((static_cast<double>(top) - static_cast<double>(z)) * scale, kBins - 1.0)); };
-      auto in = [&](float z) { return z <= top && z >= low; };
-      __syncthreads();
-      for (int i = tid; i < kBins; i += threads) {
-        s.hist.mass[i] = 0;
-        s.hist.count[i] = 0;
+      bool keep = x && lane < k;
+      if (p < 1.0) {
+        const double wt = keep ? weight(z) : 0.0, incl = wave_scan(wt, lane);
+        const double all = __builtin_bit_cast(double, shfl_u64(__builtin_bit_cast(u64, incl), SRT_WAVE - 1));
+        keep = keep && (lane == 0 || incl - wt < p * (k < a.V ? all : row_mass));
       }
-      __syncthreads();
-      visit(low, [&](float z, int) {
-        if (!in(z)) return;
-        const int bin = bin_of(z);
-        if (kMass) atomicAdd(&s.hist.mass[bin], fixed(z));
-        atomicAdd(&s.hist.count[bin], 1u);
-      });
-      __syncthreads();
-      find<kMass>(target, base);
-      const int bin = s.bin, count = s.n;
-      const double above = s.before;
-      if (bin < 0) return 0;
-      __syncthreads();
-      if (count <= kList) {
-        if (tid == 0) s.n = 0;
-        __syncthreads();
-        visit(low, [&](float z, int j) {
-          if (in(z) && bin_of(z) == bin) s.list[atomicAdd(&s.n, 1)] = pack_key(z, j);
-        });
-        __syncthreads();
-        return in_list<kMass>(count, target - above);
-      }
-      // Too many: on with the range that the bin's own scores span.
-      if (tid == 0) {
-        s.lo = 0xFFFFFFFFu;
-        s.hi = 0;
-      }
-      __syncthreads();
-      uint32_t lo = 0xFFFFFFFFu, hi = 0;
-      visit(low, [&](float z, int) {
-        if (!in(z) || bin_of(z) != bin) return;
-        const uint32_t u = static_cast<uint32_t>(pack_key(z, 0) >> 32);
-        lo = min(lo, u);
-        hi = max(hi, u);
-      });
-      if (hi) {
-        atomicMin(&s.lo, lo);
-        atomicMax(&s.hi, hi);
-      }
-      __syncthreads();
-      top = score_of(static_cast<u64>(s.hi) << 32);
-      low = score_of(static_cast<u64>(s.lo) << 32);
-      base = above;
-    }
-  }
-
-  // First bin at which the running measure reaches `target` (s.bin, -1: none), with
-  // the measure before it (s.before) and its count (s.n).
-  template <bool kMass>
-  __device__ __forceinline__ void find(double target, double base) {
-    if (wave == 0) {
-      constexpr int kPer = kBins / SRT_WAVE;
-      u64 sum = 0;
-      for (int i = 0; i < kPer; ++i) sum += kMass ? s.hist.mass[lane * kPer + i] : s.hist.count[lane * kPer + i];
-      u64 incl = sum;
-#pragma unroll
-      for (int d = 1; d < SRT_WAVE; d <<= 1) {
-        const u64 y = __shfl_up(incl, d, SRT_WAVE);
-        if (lane >= d) incl += y;
-      }
-      u64 before = incl - sum;
-      int bin = kBins;
-      for (int i = 0; i < kPer; ++i) {
-        const u64 x = kMass ? s.hist.mass[lane * kPer + i] : s.hist.count[lane * kPer + i];
-        if (x && base + static_cast<double>(before + x) >= target) {
-          bin = lane * kPer + i;
-          break;
-        }
-        before += x;
-      }
-      int best = bin;
-#pragma unroll
-      for (int d = SRT_WAVE / 2; d >= 1; d >>= 1) best = min(best, __shfl_xor(best, d, SRT_WAVE));
-      if (best == kBins) {
-        if (lane == 0) s.bin = -1;
-      } else if (bin == best) {
-        s.bin = bin;
-        s.before = base + static_cast<double>(before);
-        s.n = static_cast<int>(s.hist.count[bin]);
-      }
-    }
-    __syncthreads();
-  }
-
-  // The first entry of the sorted list at which the measure reaches `target`, or the last one.
-  template <bool kMass>
-  __device__ __forceinline__ u64 in_list(int count, double target) {
-    sort(count);
-    if (tid == 0) s.found = s.list[count - 1];
-    __syncthreads();
-    if (wave == 0) {
-      u64 run = 0;
-      for (int i0 = 0; i0 < count; i0 += SRT_WAVE) {
-        const int i = i0 + lane;
-        const u64 x = i < count ? s.list[i] : 0ull;
-        u64 incl = !x ? 0ull : kMass ? fixed(score_of(x)) : 1ull;
-#pragma unroll
-        for (int d = 1; d < SRT_WAVE; d <<= 1) {
-          const u64 y = __shfl_up(incl, d, SRT_WAVE);
-          if (lane >= d) incl += y;
-        }
-        const u64 hit = __ballot(x && static_cast<double>(run + incl) >= target);
-        if (hit) {
-          if (lane == __ffsll(static_cast<long long>(hit)) - 1) s.found = x;
-          break;
-        }
-        run += __builtin_bit_cast(u64, __shfl(incl, SRT_WAVE - 1, SRT_WAVE));
-      }
+      keep = keep && (lane == 0 || z >= least);
+      if (keep) take(best, z, key_token(x));
+      best = wave_max(best);
+      if (lane == 0) s.found = best;
     }
     __syncthreads();
     return s.found;
   }
 
-  // More tokens of the very score z than the list holds: the cut among them goes by
-  // the token, whose range is narrowed in the same way.
-  template <bool kMass>
-  __device__ __forceinline__ u64 ties(float z, double target, double base) {
-    const double each = kMass ? static_cast<double>(fixed(z)) : 1.0;
-    const double r = each > 0.0 ? fmax(1.0, ceil((target - base) / each)) : INFINITY;  // tokens of the score that are kept
-    const int width = (a.V + kBins - 1) / kBins;  // at most 1024
-    __syncthreads();
-    for (int i = tid; i < kBins; i += threads) s.hist.count[i] = 0;
-    __syncthreads();
-    visit(z, [&](float x, int j) {
-      if (x == z) atomicAdd(&s.hist.count[j / width], 1u);
-    });
-    __syncthreads();
-    find<false>(r, 0.0);
-    const int bin = s.bin, count = s.n;
-    const double above = s.before;
-    if (bin < 0) return pack_key(z, a.V);  // all of them
-    __syncthreads();
-    if (tid == 0) s.n = 0;
-    __syncthreads();
-    visit(z, [&](float x, int j) {
-      if (x != z || j / width != bin) return;
-      const int at = atomicAdd(&s.n, 1);
-      if (at < kList) s.list[at] = pack_key(x, j);  // (always, but for bias lists with a token's entries apart)
-    });
-    __syncthreads();
-    return in_list<false>(min(count, kList), r - above);
-  }
-
-  // The choice at the node that the row belongs to: packed (score with noise, token), 0 if none.
-  __device__ __forceinline__ u64 choose(int k, float p, float mp) {
-    if (!(p > 0.f) || !(mp <= 1.f)) k = 1, p = 1.f, mp = 0.f;  // (a NaN too)
-    if (k <= 0 || k > a.V) k = a.V;
-    const bool by_k = k < a.V, by_p = p < 1.f, by_m = mp > 0.f;
-    if (!w.noise || !(by_k || by_p || by_m)) return plain();
-    const double mass = first_pass();
-    if (M == -INFINITY) return 0;
-    if (M == INFINITY) {  // one of the infinite scores: the lowest token, which is always kept
-      u64 key = 0;
-      visit(M, [&](float z, int j) { key = max(key, pack_key(z, j)); });
-      return all_max(key);
-    }
-    // The scores below which nothing is kept.
-    float least = -INFINITY;
-    if (by_m) {  // the smallest float whose distance from M is no more than log(min_p)
-      const double edge = static_cast<double>(M) + log(static_cast<double>(mp));
-      least = static_cast<float>(edge);
-      if (static_cast<double>(least) - static_cast<double>(M) < log(static_cast<double>(mp))) least = nextafterf(least, INFINITY);
-    }
-    const float by_min = least;
-    if (by_k && by_p) least = -INFINITY;  // (the mass of the first k is needed)
-    if (by_p && !by_k) {
-      // tokens below this weigh no more than 1 - p of the row together
-      const double d = log(static_cast<double>(a.V) / ((1.0 - static_cast<double>(p)) * mass));
-      least = __builtin_fmaxf(least, M - static_cast<float>(d) - 0.01f);
-    }
-    if (by_k) least = __builtin_fmaxf(least, least_kept(k, INFINITY));
-    else if (by_p) least = __builtin_fmaxf(least, least_kept(0x7fffffff, static_cast<double>(p) * mass));
-    __syncthreads();
-    if (tid == 0) s.n = 0;
-    __syncthreads();
-    visit(least, [&](float z, int j) {
-      const int at = atomicAdd(&s.n, 1);
-      if (at < kList) s.list[at] = pack_key(z, j);
-    });
-    __syncthreads();
-    const int count = s.n;
-    if (count <= kList) return from_list(count, k, by_p ? static_cast<double>(p) : 1.0, mass, by_min);
-    // A long list: the last kept token first, then the choice among those from it up.
-    u64 last = by_m ? pack_key(by_min, 0) & ~0xFFFFFFFFull : 0ull;
-    double row_mass = mass;
-    if (by_k) {
-      const u64 cut = border<false>(k, least);
-      last = max(last, cut);
-      if (by_p) {
-        double sum = 0.0;
-        visit(least, [&](float z, int j) {
-          if (pack_key(z, j) >= cut) sum += exp_of(z - M);
-        });
-        row_mass = all_sum(sum);
+  // The choice from a list that holds every token that can be kept (and, with both a
+  // top-k and a top-p, the first k tokens).
+  __device__ __forceinline__ u64 from_list(int count, int k, double p, double row_mass, float least) {
+    if (count <= SRT_WAVE) return from_short(count, k, p, row_mass, least);
+    sort(count);
+    if (count <= 2 * SRT_WAVE) __syncthreads();
+    const int per = (count + threads - 1) / threads, from = tid * per, to = min(from + per, min(count, k));
+    double before = 0.0, target = INFINITY;
+    if (p < 1.0) {
+      double mine = 0.0;
+      for (int i = from; i < to; ++i) mine += weight(score_of(s.list[i]));
+      const double incl = wave_scan(mine, lane);
+      if (lane == SRT_WAVE - 1) s.redd[parity][wave] = incl;
+      __syncthreads();
+      double all = 0.0;
+      before = incl - mine;
+      for (int j = 0; j < waves; ++j) {
+        if (j == wave) before += all;
+        all += s.redd[parity][j];
       }
+      parity ^= 1;
+      target = p * (k < a.V ? all : row_mass);
     }
-    if (by_p) last = max(last, border<true>(static_cast<double>(p) * row_mass * 1099511627776.0, least));
     u64 key = 0;
-    visit(least, [&](float z, int j) {
-      if (pack_key(z, j) >= last) take(key, z, j);
-    });
+    for (int i = from; i < to; ++i) {
+      const u64 x = s.list[i];
+      const float z = score_of(x);
+      if (i > 0 && (!(before < target) || z < least)) break;
+      take(key, z, key_token(x));
+      if (p < 1.0) before += weight(z);
+    }
     return all_max(key);
   }
+
+  // The best of the tokens before `after` in the order (packed (score with noise,
+  // token), 0 if there is none), and its own place there (s.found).
+  __device__ __forceinline__ u64 candidate(u64 after, float least) {
+    u64 best = 0, at = 0;
+    float most = -INFINITY;
+    auto offer = [&](float z, float g, int j) {  // (in ascending order of the token, but for the extras)
+      const float x = add_rounded(z, g);
+      if (!(x > most) || !(z >= least) || (after && pack_key(z, j) <= after)) return;
+      most = x;
+      best = pack_key(x, j);
+      at = pack_key(z, j);
+    };
+    const int n_b = batches();
+    for (int b = 0; b < n_b; ++b) {
+      if (!reaches(b, least)) continue;
+      Batch t;
+      float z[4 * kUnroll];
+      load<true>(b, t);
+      scores(b, t, z);
+#pragma unroll
+      for (int q = 0; q < 4 * kUnroll; ++q) offer(z[q], t.g[q / 4][q % 4], token(b, q));
+    }
+    const u64 best0 = best, at0 = at;
+    most = -INFINITY;  // (ties among them go by the keys)
+    extras([&](float z, int j) {
+      const u64 held = best, held_at = at;
+      best = 0;
+      most = -INFINITY;
+      offer(z, w.noise[j], j);
+      if (held >= best) best = held, at = held_at;
+    });
+    if (best0 > best) best = best0, at = at0;
+    const u64 all = all_max(best);
+    if (all && best == all) s.found = at;  // (one thread's: a token is seen once)
+    __syncthreads();
+    return all;
+  }
+
+  // How many tokens lie before a place in the order, or at it, and what they weigh.
+  struct Above {
+    double count, mass;
+  };
+  template <bool kAt>
+  __device__ __forceinline__ Above above(u64 place) {
+    Above r = {0.0, 0.0};
+    const float least = score_of(place);
+    const int last = key_token(place);
+    const int n_b = batches();
+    for (int b = 0; b < n_b; ++b) {
+      if (!reaches(b, least)) continue;
+      Batch t;
+      float z[4 * kUnroll], part = 0.f, c = 0.f;
+      load<false>(b, t);
+      scores(b, t, z);
+#pragma unroll
+      for (int q = 0; q < 4 * kUnroll; ++q) {
+        // (a token's place goes by the numbers; those that are searched for, by their bits)
+        const bool in = kAt ? z[q] > -INFINITY && pack_key(z[q], token(b, q)) >= place
+                            : z[q] > least || (z[q] == least && token(b, q) < last);
+        part += in ? exp_of(z[q] - M) : 0.f;
+        c += in ? 1.f : 0.f;
+      }
+      r.mass += part;
+      r.count += c;
+    }
+    extras([&](float z, int j) {
+      const u64 x = pack_key(z, j);
+      if (z > -INFINITY && (kAt ? x >= place : x > place)) {
+        r.mass += exp_of(z - M);
+        r.count += 1.0;
+      }
+    });
+    r.mass = all_sum(r.mass);
+    r.count = all_sum(r.count);
+    return r;
+  }
+
+  // The last place at which the tokens from the top up to it are `count` or weigh
+  // `mass`, whichever comes first; 0 if neither does.
+  __device__ __forceinline__ u64 last_place(double count, double mass) {
+    u64 place = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const Above x = above<true>(place | 1ull << bit);
+      if (x.count >= count || x.mass >= mass) place |= 1ull << bit;
+    }
+    return place;
+  }
+
+  // The choice among more tokens than the list holds, of which those below `least`
+  // are not kept.  The best of a set that has the kept ones is the choice if it is
+  // kept itself, for which what lies before it in the order is summed; if it is not,
+  // the kept ones lie before it.  A draw from a set's distribution is one of the kept
+  // ones' share of it, so a top-p of 0.9 takes 1.1 draws, and a kept set of a
+  // millionth a dozen.  Noise that is none could be arranged to take one for every
+  // token; after kDraws the last kept place is found bit by bit.
+  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float least) {
+    if (k == a.V && !(p < 1.f)) return candidate(0, least);
+    if (k < a.V && p < 1.f) mass = above<true>(last_place(k, INFINITY)).mass;
+    const double target = p < 1.f ? static_cast<double>(p) * mass : INFINITY;
+    u64 place = 0;
+    for (int draw = 0; draw < kDraws; ++draw) {
+      const u64 best = candidate(place, least);
+      if (!best) return 0;
+      place = s.found;
+      const Above x = above<false>(place);
+      if (x.count < k && (x.count == 0.0 || x.mass < target)) return best;
+    }
+    place = last_place(k, target);
+    return candidate(place ? place - 1 : 0, least);
+  }
 };
+
+// (Out of line: the registers of a case that is met seldom stay out of the others'.)
+template <bool kRules>
+__device__ __attribute__((noinline)) u64 from_row(SampleArgs a, Lds& s, const uint32_t* skip, Row w, int n, int threads,
+                                                  int seg_batches, int batch_segs, int parity, float M, int k, float p,
+                                                  double mass,
+                                                  float least) {
+  const int tid = threadIdx.x, e4 = a.V / 4;
+  Walker<kRules> walker = {a, s, skip, w, n, tid, threads, tid % SRT_WAVE,
+                           static_cast<int>(__builtin_amdgcn_readfirstlane(tid / SRT_WAVE)), threads / SRT_WAVE, e4,
+                           e4 / (kUnroll * threads), seg_batches, batch_segs, parity, M};
+  return walker.from_row(k, p, mass, least);
+}
+
+// The choice at the node that the row belongs to: packed (score with noise, token), 0 if none.
+template <bool kRules>
+__device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float mp) {
+  Lds& s = x.s;
+  const int V = x.a.V;
+  if (!(p > 0.f) || !(mp <= 1.f)) k = 1, p = 1.f, mp = 0.f;  // (a NaN too)
+  if (k <= 0 || k > V) k = V;
+  const bool by_k = k < V, by_p = p < 1.f, by_m = mp > 0.f;
+  if (!x.w.noise) return x.template plain<false>();
+  if (!(by_k || by_p || by_m)) return x.template plain<true>();
+  for (int i = x.tid; i < kSegBins; i += x.threads) s.segbin[i] = 0;
+  if (x.tid == 0) s.n = s.m = 0;
+  double mass = 0.0;
+  if (by_p && !by_k) mass = x.template first_pass<true>();
+  else x.template first_pass<false>();
+  const float M = x.M;
+  if (M == -INFINITY) return 0;
+  if (M == INFINITY) {  // one of the infinite scores: the lowest token, which is always kept
+    u64 key = 0;
+    x.visit(M, [&](float z, int j) { key = max(key, pack_key(z, j)); });
+    return x.all_max(key);
+  }
+  // The scores below which nothing is kept.
+  float by_min = -INFINITY;
+  if (by_m) {  // the smallest float whose distance from M is no more than log(min_p)
+    const double edge = log(static_cast<double>(mp));
+    by_min = static_cast<float>(static_cast<double>(M) + edge);
+    if (static_cast<double>(by_min) - static_cast<double>(M) < edge) by_min = nextafterf(by_min, INFINITY);
+  }
+  // (with both, the mass of the first k is needed, to which what weighs e^-104 adds nothing)
+  float least = by_k && by_p ? M - 104.f : by_min;
+  if (by_p && !by_k) {
+    // tokens below this weigh no more than 1 - p of the row together
+    const double d = log(static_cast<double>(V) / ((1.0 - static_cast<double>(p)) * mass));
+    least = __builtin_fmaxf(least, M - static_cast<float>(d) - 0.01f);
+  }
+  if (by_k || by_p)
+    least = __builtin_fmaxf(least, x.least_kept(by_k ? k : 0x7fffffff, by_k ? INFINITY : static_cast<double>(p) * mass));
+  const int count = x.collect(least);
+  if (count <= kList) return x.from_list(count, k, by_p ? static_cast<double>(p) : 1.0, mass, by_min);
+  return from_row<kRules>(x.a, s, x.skip, x.w, x.n, x.threads, x.seg_batches, x.batch_segs, x.parity, M, k, p, mass,
+                          __builtin_fmaxf(least, by_min));
+}
 
 template <bool kRules>
 __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
@@ -596,8 +709,10 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   }
   const int lane = tid % SRT_WAVE, wave = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE), e4 = a.V / 4;
   const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
-  Walker<kRules> walker = {a, s, skip, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4,
-                           max(1, (batches + kSegs - 1) / kSegs), 0.f};
+  Walker<kRules> walker = {a, s, skip, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
+                           max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f};
+  static_assert(kUnroll == 8 && kSegs % 8 == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
+  while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
   const float p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
   int u = 0, k = 0, tok;
@@ -606,8 +721,10 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
     stand_on(a, walker.w, b, u);
     walker.w.invT = a.inv_temperature && a.gumbel ? a.inv_temperature[b] : 1.f;
     walker.n = k;
+    // (what the thread's place decides is worked out where it is used, not kept over the walk in 100 registers)
+    asm volatile("" : "+v"(walker.tid), "+v"(walker.lane));
     if constexpr (kRules) mark(a, walker.w, s.path, k, 0, a.V, skip, threads);
-    const u64 key = walker.choose(top_k, p, mp);
+    const u64 key = choose<kRules>(walker, top_k, p, mp);
     tok = key ? key_token(key) : -1;
     __syncthreads();  // (the staged tree, at the first step; LDS is the next row's from here on)
     int child = -1;
