@@ -53,26 +53,46 @@ typedef unsigned long long u64;
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-__device__ __forceinline__ double shfl_xor_f64(double v, int m) {
-  return __builtin_bit_cast(double, shfl_xor_u64(__builtin_bit_cast(u64, v), m));
+// Reductions and prefix sums over the wave by DPP moves, as wave_sum of common.h (a
+// few cycles a step, where a shuffle of 64 bits goes through the LDS crossbar twice).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ u64 from_lane(u64 x) {  // 0 where there is none
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, kRows, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), kCtrl, kRows, 0xf, false);
+  return static_cast<u64>(hi) << 32 | lo;
 }
-
-// Inclusive prefix sum over the wave.
-__device__ __forceinline__ u64 wave_scan(u64 x, int lane) {
-#pragma unroll
-  for (int d = 1; d < SRT_WAVE; d <<= 1) {
-    const u64 y = __shfl_up(x, d, SRT_WAVE);
-    if (lane >= d) x += y;
-  }
-  return x;
+template <typename Fn>
+__device__ __forceinline__ u64 wave_steps(u64 x, Fn join) {  // inclusive over the lanes up to each
+  x = join(x, from_lane<0x111, 0xf>(x));  // row_shr:1
+  x = join(x, from_lane<0x112, 0xf>(x));
+  x = join(x, from_lane<0x114, 0xf>(x));
+  x = join(x, from_lane<0x118, 0xf>(x));
+  x = join(x, from_lane<0x142, 0xa>(x));  // row_bcast:15
+  return join(x, from_lane<0x143, 0xc>(x));  // row_bcast:31
 }
-__device__ __forceinline__ double wave_scan(double x, int lane) {
-#pragma unroll
-  for (int d = 1; d < SRT_WAVE; d <<= 1) {
-    const double y = __builtin_bit_cast(double, __shfl_up(__builtin_bit_cast(u64, x), d, SRT_WAVE));
-    if (lane >= d) x += y;
-  }
-  return x;
+__device__ __forceinline__ u64 last_lane(u64 x) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), SRT_WAVE - 1);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), SRT_WAVE - 1);
+  return static_cast<u64>(hi) << 32 | lo;
+}
+__device__ __forceinline__ u64 wave_top(u64 x) {
+  return last_lane(wave_steps(x, [](u64 p, u64 q) { return p > q ? p : q; }));
+}
+__device__ __forceinline__ u64 wave_scan(u64 x) {
+  return wave_steps(x, [](u64 p, u64 q) { return p + q; });
+}
+__device__ __forceinline__ double wave_scan(double x) {
+  return __builtin_bit_cast(double, wave_steps(__builtin_bit_cast(u64, x), [](u64 p, u64 q) {
+    return __builtin_bit_cast(u64, __builtin_bit_cast(double, p) + __builtin_bit_cast(double, q));
+  }));
+}
+__device__ __forceinline__ double last_lane(double x) {
+  return __builtin_bit_cast(double, last_lane(__builtin_bit_cast(u64, x)));
+}
+__device__ __forceinline__ float wave_largest(float x) {
+  const u64 key = wave_top(pack_key(x, 0));
+  const uint32_t u = static_cast<uint32_t>(key >> 32);
+  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
 __device__ __forceinline__ float score_of(u64 key) {
@@ -270,24 +290,21 @@ struct Walker {
 
   // The workgroup's largest.
   __device__ __forceinline__ u64 all_max(u64 key) {
-    key = wave_max(key);
+    key = wave_top(key);
     if (lane == 0) s.red[parity][wave] = key;
     __syncthreads();
-    key = wave_max(lane < waves ? s.red[parity][lane] : 0ull);
+    key = wave_top(lane < waves ? s.red[parity][lane] : 0ull);
     parity ^= 1;
     return key;
   }
   // The workgroup's sum; the terms are added in the same order always.
   __device__ __forceinline__ double all_sum(double x) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x += shfl_xor_f64(x, off);
+    x = last_lane(wave_scan(x));
     if (lane == 0) s.redd[parity][wave] = x;
     __syncthreads();
     x = lane < waves ? s.redd[parity][lane] : 0.0;
     parity ^= 1;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x += shfl_xor_f64(x, off);
-    return x;
+    return last_lane(wave_scan(x));
   }
 
   __device__ __forceinline__ void take(u64& key, float z, int j) const {
@@ -307,6 +324,7 @@ struct Walker {
     for (int b = 0; b < n_b; ++b) {
       Batch next;
       if (b + 1 < n_b) load<kNoise>(b + 1, next);
+      __builtin_amdgcn_sched_barrier(0);  // (no load waits for the scores)
       float z[4 * kUnroll];
       scores(b, t, z);
 #pragma unroll
@@ -336,6 +354,7 @@ struct Walker {
     for (int b = 0; b < n_b; ++b) {
       Batch later;
       if (b + 2 < n_b) load<false>(b + 2, later);
+      __builtin_amdgcn_sched_barrier(0);
       if (first_of(b) < e4) {
         float z[4 * kUnroll];
         scores(b, t, z);
@@ -377,29 +396,18 @@ struct Walker {
       if (kMass && z > -INFINITY) sum += exp_of(z - m);
     });
     // Join: first the wave's lanes, then the waves.
-    float top = m;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) top = __builtin_fmaxf(top, shfl_xor(top, off));
+    const float top = wave_largest(m);
     double part = 0.0;
-    if (kMass) {
-      part = m > -INFINITY ? sum * exp_of(m - top) : 0.0;
-#pragma unroll
-      for (int off = 32; off >= 1; off >>= 1) part += shfl_xor_f64(part, off);
-    }
+    if (kMass) part = last_lane(wave_scan(m > -INFINITY ? sum * exp_of(m - top) : 0.0));
     if (lane == 0) {
       s.redm[wave] = top;
       if (kMass) s.redd[0][wave] = part;
     }
     __syncthreads();
     const float mine = lane < waves ? s.redm[lane] : -INFINITY;
-    M = mine;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) M = __builtin_fmaxf(M, shfl_xor(M, off));
+    M = wave_largest(mine);
     if (!kMass) return 0.0;
-    part = mine > -INFINITY ? s.redd[0][lane] * exp_of(mine - M) : 0.0;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) part += shfl_xor_f64(part, off);
-    return part;
+    return last_lane(wave_scan(mine > -INFINITY ? s.redd[0][lane] * exp_of(mine - M) : 0.0));
   }
 
   // A score that no kept token is below, from the segments' maxima: `k` of them
@@ -421,7 +429,7 @@ struct Walker {
       x[i] = s.segbin[lane * kPer + i];
       sum += x[i];  // (16 segments of 512 threads: neither field runs over)
     }
-    u64 before = wave_scan(sum, lane) - sum;
+    u64 before = wave_scan(sum) - sum;
     // (a margin for the weights' roundings)
     const u64 want = mass < 1e6 ? static_cast<u64>(mass * 16777216.0 * 1.00001) + 1 : ~0ull;
     int found = kSegBins;
@@ -436,11 +444,10 @@ struct Walker {
     return found < kSegBins ? M - (found + 1.01f) * 0.125f : -INFINITY;
   }
 
-  // Sorts the list's first `count` entries, largest first; returns with the list in
-  // order for wave 0, or for all where there are more than 128.  A wave's 64 pairs at
-  // a distance of up to 64 lie in 128 entries of its own: such steps need no barrier.
+  // Sorts the list's first `count` entries, largest first.  A wave's 64 pairs at a
+  // distance of up to 64 lie in 128 entries of its own: such steps need no barrier.
   __device__ __forceinline__ void sort(int count) const {
-    int size = 128;
+    int size = 4 * SRT_WAVE;
     while (size < count) size *= 2;
     for (int i = count + tid; i < size; i += threads) s.list[i] = 0;
     __syncthreads();
@@ -459,34 +466,57 @@ struct Walker {
         if (d > SRT_WAVE) __syncthreads();
       }
     }
-    if (size > 2 * SRT_WAVE) __syncthreads();
+    __syncthreads();
   }
 
   __device__ __forceinline__ double weight(float z) const { return exp(static_cast<double>(z) - static_cast<double>(M)); }
 
-  // The choice from a list of up to 64 tokens, by wave 0: a lane each.
+  // The choice from a list of up to 64 R tokens, by wave 0 in registers: R a lane,
+  // place 64 r + lane.  Exact: the tokens are sorted and their weights summed in order.
+  template <int R>
   __device__ __forceinline__ u64 from_short(int count, int k, double p, double row_mass, float least) {
-    u64 best = 0;
     if (wave == 0) {
-      u64 x = lane < count ? s.list[lane] : 0ull;
+      u64 x[R], best = 0;
 #pragma unroll
-      for (int run = 2; run <= SRT_WAVE; run *= 2)
+      for (int r = 0; r < R; ++r) x[r] = SRT_WAVE * r + lane < count ? s.list[SRT_WAVE * r + lane] : 0ull;
 #pragma unroll
-        for (int d = run / 2; d >= 1; d /= 2) {
-          const u64 y = shfl_xor_u64(x, d);
-          const bool larger = ((lane & d) == 0) == ((lane & run) == 0);  // keeps the larger one
-          x = (x > y) == larger ? x : y;
-        }
-      const float z = score_of(x);
-      bool keep = x && lane < k;
-      if (p < 1.0) {
-        const double wt = keep ? weight(z) : 0.0, incl = wave_scan(wt, lane);
-        const double all = __builtin_bit_cast(double, shfl_u64(__builtin_bit_cast(u64, incl), SRT_WAVE - 1));
-        keep = keep && (lane == 0 || incl - wt < p * (k < a.V ? all : row_mass));
+      for (int run = 2; run <= SRT_WAVE * R; run *= 2) {
+#pragma unroll
+        for (int d = run / 2; d >= SRT_WAVE; d /= 2)  // pairs in one lane
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const int o = r ^ (d / SRT_WAVE);
+            if (o < r) continue;
+            const bool falls = ((SRT_WAVE * r) & run) == 0;
+            const u64 hi = max(x[r], x[o]), lo = min(x[r], x[o]);
+            x[r] = falls ? hi : lo;
+            x[o] = falls ? lo : hi;
+          }
+        for (int d = min(run / 2, SRT_WAVE / 2); d >= 1; d /= 2)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const u64 y = shfl_xor_u64(x[r], d);
+            const bool larger = ((lane & d) == 0) == (((SRT_WAVE * r + lane) & run) == 0);
+            x[r] = (x[r] > y) == larger ? x[r] : y;
+          }
       }
-      keep = keep && (lane == 0 || z >= least);
-      if (keep) take(best, z, key_token(x));
-      best = wave_max(best);
+      double before = 0.0, incl[R], wt[R];
+      if (p < 1.0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          wt[r] = x[r] && SRT_WAVE * r + lane < k ? weight(score_of(x[r])) : 0.0;
+          incl[r] = wave_scan(wt[r]) + before;
+          before = last_lane(incl[r]);
+        }
+      const double target = p * (k < a.V ? before : row_mass);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int i = SRT_WAVE * r + lane;
+        const float z = score_of(x[r]);
+        const bool keep = x[r] && i < k && (i == 0 || ((p >= 1.0 || incl[r] - wt[r] < target) && z >= least));
+        if (keep) take(best, z, key_token(x[r]));
+      }
+      best = wave_top(best);
       if (lane == 0) s.found = best;
     }
     __syncthreads();
@@ -496,15 +526,21 @@ struct Walker {
   // The choice from a list that holds every token that can be kept (and, with both a
   // top-k and a top-p, the first k tokens).
   __device__ __forceinline__ u64 from_list(int count, int k, double p, double row_mass, float least) {
-    if (count <= SRT_WAVE) return from_short(count, k, p, row_mass, least);
+    if (k == a.V && p >= 1.0) {  // the cut is `least` alone
+      u64 key = 0;
+      for (int i = tid; i < count; i += threads) take(key, score_of(s.list[i]), key_token(s.list[i]));
+      return all_max(key);
+    }
+    if (count <= SRT_WAVE) return from_short<1>(count, k, p, row_mass, least);
+    if (count <= 4 * SRT_WAVE) return from_short<4>(count, k, p, row_mass, least);
+    if (k == a.V) return draw_from_list(count, p * row_mass, least);
     sort(count);
-    if (count <= 2 * SRT_WAVE) __syncthreads();
     const int per = (count + threads - 1) / threads, from = tid * per, to = min(from + per, min(count, k));
     double before = 0.0, target = INFINITY;
     if (p < 1.0) {
       double mine = 0.0;
       for (int i = from; i < to; ++i) mine += weight(score_of(s.list[i]));
-      const double incl = wave_scan(mine, lane);
+      const double incl = wave_scan(mine);
       if (lane == SRT_WAVE - 1) s.redd[parity][wave] = incl;
       __syncthreads();
       double all = 0.0;
@@ -527,6 +563,43 @@ struct Walker {
     return all_max(key);
   }
 
+  // from_row's draws, in the list: the kept tokens are those before which less than
+  // `target` lies, from `least` up.
+  __device__ __forceinline__ u64 draw_from_list(int count, double target, float least) {
+    u64 place = 0;
+    for (int draw = 0; draw < kDraws; ++draw) {
+      u64 best = 0, at = 0;
+      for (int i = tid; i < count; i += threads) {
+        const u64 x = s.list[i], held = best;
+        if (x <= place || score_of(x) < least) continue;
+        take(best, score_of(x), key_token(x));
+        if (best != held) at = x;
+      }
+      const u64 all = all_max(best);
+      if (!all) return 0;
+      if (best == all) s.found = at;
+      __syncthreads();
+      place = s.found;
+      double mass = 0.0;
+      for (int i = tid; i < count; i += threads)
+        if (s.list[i] > place) mass += weight(score_of(s.list[i]));
+      mass = all_sum(mass);
+      if (mass < target) return all;  // (nothing lies before the first)
+    }
+    sort(count);
+    u64 best = 0;
+    if (tid == 0) {
+      double before = 0.0;
+      for (int i = 0; i < count; ++i) {
+        const float z = score_of(s.list[i]);
+        if (i > 0 && (!(before < target) || z < least)) break;
+        take(best, z, key_token(s.list[i]));
+        before += weight(z);
+      }
+    }
+    return all_max(best);
+  }
+
   // The best of the tokens before `after` in the order (packed (score with noise,
   // token), 0 if there is none), and its own place there (s.found).
   __device__ __forceinline__ u64 candidate(u64 after, float least) {
@@ -540,14 +613,19 @@ struct Walker {
       at = pack_key(z, j);
     };
     const int n_b = batches();
+    Batch t;
+    if (reaches(0, least)) load<true>(0, t);
     for (int b = 0; b < n_b; ++b) {
-      if (!reaches(b, least)) continue;
-      Batch t;
+      const bool on = reaches(b, least);
+      Batch next;
+      if (b + 1 < n_b && reaches(b + 1, least)) load<true>(b + 1, next);
+      const Batch now = t;
+      t = next;
+      if (!on) continue;
       float z[4 * kUnroll];
-      load<true>(b, t);
-      scores(b, t, z);
+      scores(b, now, z);
 #pragma unroll
-      for (int q = 0; q < 4 * kUnroll; ++q) offer(z[q], t.g[q / 4][q % 4], token(b, q));
+      for (int q = 0; q < 4 * kUnroll; ++q) offer(z[q], now.g[q / 4][q % 4], token(b, q));
     }
     const u64 best0 = best, at0 = at;
     most = -INFINITY;  // (ties among them go by the keys)
@@ -575,12 +653,17 @@ struct Walker {
     const float least = score_of(place);
     const int last = key_token(place);
     const int n_b = batches();
+    Batch t;
+    if (reaches(0, least)) load<false>(0, t);
     for (int b = 0; b < n_b; ++b) {
-      if (!reaches(b, least)) continue;
-      Batch t;
+      const bool on = reaches(b, least);
+      Batch next;
+      if (b + 1 < n_b && reaches(b + 1, least)) load<false>(b + 1, next);
+      const Batch now = t;
+      t = next;
+      if (!on) continue;
       float z[4 * kUnroll], part = 0.f, c = 0.f;
-      load<false>(b, t);
-      scores(b, t, z);
+      scores(b, now, z);
 #pragma unroll
       for (int q = 0; q < 4 * kUnroll; ++q) {
         // (a token's place goes by the numbers; those that are searched for, by their bits)
