@@ -39,6 +39,7 @@ constexpr int kSegBins = 512;     // of the segments' maxima, 1 / 8 of the score
 constexpr int kMassBits = 44;     // of a bin's word: mass in units of 2^-24 below, count above
 constexpr int64_t kMaxVocab = int64_t(1) << 21;
 constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LDS
+constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
 constexpr int kShortVocab = 4096;  // rows up to which 256 threads walk
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -119,7 +120,12 @@ template <bool kRules>
 struct Walker {
   const SampleArgs& a;
   Lds& s;
-  const uint32_t* skip;  // marked entries (kRules)
+  // Under rules: marked entries; the tokens with a count word and their scores (-1
+  // of them: more than there is room for, and the stream reads the words).
+  uint32_t* skip;
+  int32_t* said;
+  float* said_z;
+  int n_said;
   Row w;
   int n;                 // tokens emitted on this walk
   int tid, threads, lane, wave, waves;
@@ -127,18 +133,36 @@ struct Walker {
   int seg_batches, batch_segs;  // batches of a segment, or segments of a batch
   int parity;            // of the reductions' arrays: the next one's writes meet no reads of the last one's
   float M;               // largest score of the row
+  bool long_row;         // the row before had more candidates than the list holds
+
+  // The best of a set of tokens by score and noise (packed, 0 if there is none), and
+  // its place in the order.
+  struct Draw {
+    u64 best = 0, at = 0;
+    float most = -INFINITY;
+    __device__ __forceinline__ void ascending(float z, float x, int j) {
+      if (x > most) any(z, x, j);
+    }
+    __device__ __forceinline__ void any(float z, float x, int j) {
+      const u64 key = pack_key(x, j);
+      if (!(x > -INFINITY) || key <= best) return;
+      most = x;
+      best = key;
+      at = pack_key(z, j);
+    }
+  };
 
   // Score of a logit under the rules; a NaN counts as -inf.
   __device__ __forceinline__ float scored(float l, int word) const {
     if (kRules && word) l = penalised(w, l, word & kPrompt, word & kCount);
     return __builtin_fmaxf(mul_rounded(l, w.invT), -INFINITY);
   }
+  __device__ __forceinline__ bool streams_words() const { return w.seen && n_said < 0; }
   __device__ __forceinline__ bool marked(int j) const { return kRules && ((skip[j >> 5] >> (j & 31)) & 1u); }
 
   // A batch: quartets i, i + threads, .. of a row, i the thread's first.
   struct Batch {
     f32x4 x[kUnroll], g[kUnroll];
-    u16x4 c[kUnroll];
   };
   __device__ __forceinline__ int first_of(int b) const { return b * kUnroll * threads + tid; }
   __device__ __forceinline__ int batches() const { return full + (full * kUnroll * threads < e4); }
@@ -148,7 +172,6 @@ struct Walker {
   __device__ __forceinline__ void load(int b, Batch& t) const {
     const f32x4u* r4 = reinterpret_cast<const f32x4u*>(w.logits);
     const f32x4u* g4 = reinterpret_cast<const f32x4u*>(w.noise);
-    const u16x4* s4 = reinterpret_cast<const u16x4*>(w.seen);
     const int i = first_of(b);
     if (i >= e4) return;
 #pragma unroll
@@ -156,7 +179,6 @@ struct Walker {
       const int at = i + k * threads < e4 ? i + k * threads : i;
       t.x[k] = r4[at];
       if (kNoise) t.g[k] = g4[at];
-      if (kRules && w.seen) t.c[k] = s4[at];
     }
   }
   // Its scores (-inf: none, or marked).
@@ -167,9 +189,11 @@ struct Walker {
       const int at = i + k * threads;
       uint32_t out = b < full || at < e4 ? 0u : 15u;
       if (kRules && out == 0) out = (skip[at >> 3] >> ((4 * at) & 31)) & 15u;
+      u16x4 c = {0, 0, 0, 0};
+      if (kRules && streams_words() && out != 15u) c = reinterpret_cast<const u16x4*>(w.seen)[at];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = scored(t.x[k][e], kRules && w.seen ? t.c[k][e] : 0);
+        const float x = scored(t.x[k][e], c[e]);
         z[4 * k + e] = (out >> e) & 1u ? -INFINITY : x;
       }
     }
@@ -181,12 +205,47 @@ struct Walker {
   template <typename Fn>
   __device__ __forceinline__ void extras(Fn f) const {
     const int j = 4 * e4 + tid;
-    if (j < a.V && !marked(j)) f(scored(w.logits[j], w.seen ? w.seen[j] : 0), j);
-    if constexpr (kRules)
+    if (j < a.V && !marked(j)) f(scored(w.logits[j], kRules && streams_words() ? w.seen[j] : 0), j);
+    if constexpr (kRules) {
+      for (int i = tid; i < n_said; i += threads) f(said_z[i], said[i]);
       for_special(a, w, s.path, n, 0, a.V, threads, [&](int t, int from) {
         if (allowed_token(w, t))
           f(__builtin_fmaxf(mul_rounded(special_logit(a, w, s.path, n, t, from, w.logits[t]), w.invT), -INFINITY), t);
       });
+    }
+  }
+
+  // Lists the tokens with a count word.  A penalty costs a division, which one such
+  // token in a wave's 64 entries makes it take for all: of a row with one in 50 most
+  // of the time went there (64 sequences, 9 levels: 617 us, and 362 with the list).
+  __device__ __forceinline__ void list_said() {
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    const u16x4* s4 = reinterpret_cast<const u16x4*>(w.seen);
+    auto push = [&](uint16_t word, int j) {
+      if (!word) return;
+      const int at = atomicAdd(&s.n, 1);
+      if (at < kSaid) said[at] = j;
+    };
+    for (int i = tid; i < e4; i += threads) {
+      const u16x4 c = s4[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) push(c[e], 4 * i + e);
+    }
+    if (4 * e4 + tid < a.V) push(w.seen[4 * e4 + tid], 4 * e4 + tid);
+    __syncthreads();
+    n_said = s.n <= kSaid ? s.n : -1;
+  }
+  // Scores and marks them; one that is marked is forbidden or scored as a special token.
+  __device__ __forceinline__ void mark_said() {
+    for (int i = tid; i < n_said; i += threads) {
+      const int t = said[i];
+      const uint32_t bit = 1u << (t & 31);
+      const float l = w.logits[t];
+      const int word = w.seen[t];
+      said_z[i] = atomicOr(&skip[t >> 5], bit) & bit ? -INFINITY : scored(l, word);
+    }
+    __syncthreads();
   }
 
   // Whether the thread has an entry of score `least` or more in a batch.
@@ -273,7 +332,7 @@ struct Walker {
         for (int e = 0; e < 4; ++e) {
           const int j = 4 * at[k] + e;
           const bool in = on && !((out >> e) & 1u);
-          const float z = in ? scored(x[k][e], kRules && w.seen ? w.seen[j] : 0) : -INFINITY;
+          const float z = in ? scored(x[k][e], kRules && streams_words() ? w.seen[j] : 0) : -INFINITY;
           append(z >= least && z > -INFINITY, z, j);
         }
       }
@@ -337,8 +396,8 @@ struct Walker {
 
   // The pass over the row: M (-inf where nothing is left), the segments' maxima and,
   // if it is asked for, the row's mass in units of the largest weight.
-  template <bool kMass>
-  __device__ __forceinline__ double first_pass() {
+  template <bool kMass, bool kDraw>
+  __device__ __forceinline__ double first_pass(Draw& d) {
     float m = -INFINITY, seg = -INFINITY;
     double sum = 0.0;  // of parts of a batch each
     auto add = [&](float top) {  // the running maximum goes up to `top`
@@ -348,12 +407,13 @@ struct Walker {
       }
     };
     Batch t, next;
-    load<false>(0, t);
+    load<kDraw>(0, t);
     const int n_b = batches();
-    if (n_b > 1) load<false>(1, next);
+    if (!kDraw && n_b > 1) load<kDraw>(1, next);
     for (int b = 0; b < n_b; ++b) {
-      Batch later;
-      if (b + 2 < n_b) load<false>(b + 2, later);
+      Batch later;  // (two batches ahead, or one where the noise's take as many registers)
+      if (kDraw && b + 1 < n_b) load<kDraw>(b + 1, next);
+      if (!kDraw && b + 2 < n_b) load<kDraw>(b + 2, later);
       __builtin_amdgcn_sched_barrier(0);
       if (first_of(b) < e4) {
         float z[4 * kUnroll];
@@ -370,6 +430,9 @@ struct Walker {
           for (int q = 0; q < 4 * kUnroll; ++q) part[q & 1] += exp_of(z[q] - ref);
           sum += part[0] + part[1];
         }
+        if (kDraw)
+#pragma unroll
+          for (int q = 0; q < 4 * kUnroll; ++q) d.ascending(z[q], add_rounded(z[q], t.g[q / 4][q % 4]), token(b, q));
         if (batch_segs == 1) seg = __builtin_fmaxf(seg, top);
         else
 #pragma unroll
@@ -389,11 +452,12 @@ struct Walker {
         seg = -INFINITY;
       }
       t = next;
-      next = later;
+      if (!kDraw) next = later;
     }
-    extras([&](float z, int) {
+    extras([&](float z, int j) {
       add(z);
       if (kMass && z > -INFINITY) sum += exp_of(z - m);
+      if (kDraw && z > -INFINITY) d.any(z, add_rounded(z, w.noise[j]), j);
     });
     // Join: first the wave's lanes, then the waves.
     const float top = wave_largest(m);
@@ -600,91 +664,92 @@ struct Walker {
     return all_max(best);
   }
 
-  // The best of the tokens before `after` in the order (packed (score with noise,
-  // token), 0 if there is none), and its own place there (s.found).
-  __device__ __forceinline__ u64 candidate(u64 after, float least) {
-    u64 best = 0, at = 0;
-    float most = -INFINITY;
-    auto offer = [&](float z, float g, int j) {  // (in ascending order of the token, but for the extras)
-      const float x = add_rounded(z, g);
-      if (!(x > most) || !(z >= least) || (after && pack_key(z, j) <= after)) return;
-      most = x;
-      best = pack_key(x, j);
-      at = pack_key(z, j);
-    };
-    const int n_b = batches();
-    Batch t;
-    if (reaches(0, least)) load<true>(0, t);
-    for (int b = 0; b < n_b; ++b) {
-      const bool on = reaches(b, least);
-      Batch next;
-      if (b + 1 < n_b && reaches(b + 1, least)) load<true>(b + 1, next);
-      const Batch now = t;
-      t = next;
-      if (!on) continue;
-      float z[4 * kUnroll];
-      scores(b, now, z);
-#pragma unroll
-      for (int q = 0; q < 4 * kUnroll; ++q) offer(z[q], now.g[q / 4][q % 4], token(b, q));
-    }
-    const u64 best0 = best, at0 = at;
-    most = -INFINITY;  // (ties among them go by the keys)
-    extras([&](float z, int j) {
-      const u64 held = best, held_at = at;
-      best = 0;
-      most = -INFINITY;
-      offer(z, w.noise[j], j);
-      if (held >= best) best = held, at = held_at;
-    });
-    if (best0 > best) best = best0, at = at0;
-    const u64 all = all_max(best);
-    if (all && best == all) s.found = at;  // (one thread's: a token is seen once)
+  // The workgroup's best; its place is s.found.
+  __device__ __forceinline__ u64 drawn(const Draw& d) {
+    const u64 all = all_max(d.best);
+    if (all && d.best == all) s.found = d.at;  // (one thread's: a token is seen once)
     __syncthreads();
     return all;
   }
 
-  // How many tokens lie before a place in the order, or at it, and what they weigh.
+  // Calls f(batch number, batch, whether it is the thread's) in a wave for the batches
+  // that have a score of `least` or more in one of its threads, the next one's loads
+  // under way.
+  template <bool kNoise, typename Fn>
+  __device__ __forceinline__ void batches_from(float least, Fn f) {
+    const int n_b = batches();
+    Batch t;
+    bool on = reaches(0, least);
+    if (on) load<kNoise>(0, t);
+    for (int b = 0; b < n_b; ++b) {
+      Batch next;
+      const bool more = b + 1 < n_b && reaches(b + 1, least);
+      if (more) load<kNoise>(b + 1, next);
+      __builtin_amdgcn_sched_barrier(0);
+      if (__ballot(on)) f(b, t, on);
+      t = next;
+      on = more;
+    }
+  }
+
+  // The best of the tokens of `least` and more before `after` in the order.
+  __device__ __forceinline__ u64 candidate(u64 after, float least) {
+    Draw d;
+    batches_from<true>(least, [&](int b, const Batch& t, bool on) {
+      float z[4 * kUnroll];
+      scores(b, t, z);
+#pragma unroll
+      for (int q = 0; q < 4 * kUnroll; ++q) {
+        const float x = add_rounded(z[q], t.g[q / 4][q % 4]);
+        if (on && x > d.most && z[q] >= least && (!after || pack_key(z[q], token(b, q)) > after)) d.any(z[q], x, token(b, q));
+      }
+    });
+    extras([&](float z, int j) {
+      if (z >= least && z > -INFINITY && pack_key(z, j) > after) d.any(z, add_rounded(z, w.noise[j]), j);
+    });
+    return drawn(d);
+  }
+
+  // How many tokens lie before a place in the order, and what they weigh (kAt: up to
+  // a place, which need not be a token's).
   struct Above {
     double count, mass;
   };
   template <bool kAt>
-  __device__ __forceinline__ Above above(u64 place) {
-    Above r = {0.0, 0.0};
+  __device__ __forceinline__ Above above(u64 place, bool weigh) {
     const float least = score_of(place);
     const int last = key_token(place);
-    const int n_b = batches();
-    Batch t;
-    if (reaches(0, least)) load<false>(0, t);
-    for (int b = 0; b < n_b; ++b) {
-      const bool on = reaches(b, least);
-      Batch next;
-      if (b + 1 < n_b && reaches(b + 1, least)) load<false>(b + 1, next);
-      const Batch now = t;
-      t = next;
-      if (!on) continue;
-      float z[4 * kUnroll], part = 0.f, c = 0.f;
-      scores(b, now, z);
+    double mass = 0.0;
+    int count = 0;  // of the wave
+    batches_from<false>(least, [&](int b, const Batch& t, bool on) {
+      float z[4 * kUnroll], part = 0.f;
+      scores(b, t, z);
+      u64 equal = 0;
 #pragma unroll
       for (int q = 0; q < 4 * kUnroll; ++q) {
-        // (a token's place goes by the numbers; those that are searched for, by their bits)
-        const bool in = kAt ? z[q] > -INFINITY && pack_key(z[q], token(b, q)) >= place
-                            : z[q] > least || (z[q] == least && token(b, q) < last);
-        part += in ? exp_of(z[q] - M) : 0.f;
-        c += in ? 1.f : 0.f;
+        // (a token's place goes by the numbers; one that is searched for, by its bits)
+        const bool in = on && (kAt ? z[q] > -INFINITY && pack_key(z[q], token(b, q)) >= place : z[q] > least);
+        if (weigh) part += in ? exp_of(z[q] - M) : 0.f;
+        count += __popcll(__ballot(in));
+        if (!kAt) equal |= __ballot(on && z[q] == least);
       }
-      r.mass += part;
-      r.count += c;
-    }
-    extras([&](float z, int j) {
-      const u64 x = pack_key(z, j);
-      if (z > -INFINITY && (kAt ? x >= place : x > place)) {
-        r.mass += exp_of(z - M);
-        r.count += 1.0;
+      if (equal) {  // ties with the token at the place, itself among them: seldom
+#pragma unroll
+        for (int q = 0; q < 4 * kUnroll; ++q) {
+          const bool in = on && z[q] == least && token(b, q) < last;
+          if (weigh) part += in ? exp_of(z[q] - M) : 0.f;
+          count += __popcll(__ballot(in));
+        }
       }
+      mass += part;
     });
-    r.mass = all_sum(r.mass);
-    r.count = all_sum(r.count);
-    return r;
+    double c = 0.0;
+    extras([&](float z, int j) {
+      if (!(z > -INFINITY) || !(kAt ? pack_key(z, j) >= place : pack_key(z, j) > place)) return;
+      mass += exp_of(z - M);
+      c += 1.0;
+    });
+    return {all_sum(c + (lane == 0 ? count : 0)), weigh ? all_sum(mass) : 0.0};
   }
 
   // The last place at which the tokens from the top up to it are `count` or weigh
@@ -692,7 +757,7 @@ struct Walker {
   __device__ __forceinline__ u64 last_place(double count, double mass) {
     u64 place = 0;
     for (int bit = 63; bit >= 0; --bit) {
-      const Above x = above<true>(place | 1ull << bit);
+      const Above x = above<true>(place | 1ull << bit, mass < INFINITY);
       if (x.count >= count || x.mass >= mass) place |= 1ull << bit;
     }
     return place;
@@ -705,35 +770,25 @@ struct Walker {
   // ones' share of it, so a top-p of 0.9 takes 1.1 draws, and a kept set of a
   // millionth a dozen.  Noise that is none could be arranged to take one for every
   // token; after kDraws the last kept place is found bit by bit.
-  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float least) {
+  // `best`, at `place`: the first draw, if it has been made.
+  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float least, u64 best, u64 place) {
     if (k == a.V && !(p < 1.f)) return candidate(0, least);
-    if (k < a.V && p < 1.f) mass = above<true>(last_place(k, INFINITY)).mass;
+    if (k < a.V && p < 1.f) mass = above<true>(last_place(k, INFINITY), true).mass;
     const double target = p < 1.f ? static_cast<double>(p) * mass : INFINITY;
-    u64 place = 0;
     for (int draw = 0; draw < kDraws; ++draw) {
-      const u64 best = candidate(place, least);
-      if (!best) return 0;
-      place = s.found;
-      const Above x = above<false>(place);
+      if (draw > 0 || !best) {
+        best = candidate(place, least);
+        if (!best) return 0;
+        place = s.found;
+      }
+      if (!(score_of(place) >= least)) continue;
+      const Above x = above<false>(place, p < 1.f);
       if (x.count < k && (x.count == 0.0 || x.mass < target)) return best;
     }
     place = last_place(k, target);
     return candidate(place ? place - 1 : 0, least);
   }
 };
-
-// (Out of line: the registers of a case that is met seldom stay out of the others'.)
-template <bool kRules>
-__device__ __attribute__((noinline)) u64 from_row(SampleArgs a, Lds& s, const uint32_t* skip, Row w, int n, int threads,
-                                                  int seg_batches, int batch_segs, int parity, float M, int k, float p,
-                                                  double mass,
-                                                  float least) {
-  const int tid = threadIdx.x, e4 = a.V / 4;
-  Walker<kRules> walker = {a, s, skip, w, n, tid, threads, tid % SRT_WAVE,
-                           static_cast<int>(__builtin_amdgcn_readfirstlane(tid / SRT_WAVE)), threads / SRT_WAVE, e4,
-                           e4 / (kUnroll * threads), seg_batches, batch_segs, parity, M};
-  return walker.from_row(k, p, mass, least);
-}
 
 // The choice at the node that the row belongs to: packed (score with noise, token), 0 if none.
 template <bool kRules>
@@ -748,8 +803,19 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   for (int i = x.tid; i < kSegBins; i += x.threads) s.segbin[i] = 0;
   if (x.tid == 0) s.n = s.m = 0;
   double mass = 0.0;
-  if (by_p && !by_k) mass = x.template first_pass<true>();
-  else x.template first_pass<false>();
+  // Where the row before had a long list, this one's first draw is made along with the pass.
+  u64 draw = 0, place = 0;
+  typename Walker<kRules>::Draw d;
+  if (by_p && !by_k && x.long_row) {
+    mass = x.template first_pass<true, true>(d);
+    draw = x.drawn(d);
+    place = s.found;
+  } else if (by_p && !by_k) {
+    mass = x.template first_pass<true, false>(d);
+  } else {
+    x.template first_pass<false, false>(d);
+  }
+  x.long_row = false;
   const float M = x.M;
   if (M == -INFINITY) return 0;
   if (M == INFINITY) {  // one of the infinite scores: the lowest token, which is always kept
@@ -775,14 +841,16 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
     least = __builtin_fmaxf(least, x.least_kept(by_k ? k : 0x7fffffff, by_k ? INFINITY : static_cast<double>(p) * mass));
   const int count = x.collect(least);
   if (count <= kList) return x.from_list(count, k, by_p ? static_cast<double>(p) : 1.0, mass, by_min);
-  return from_row<kRules>(x.a, s, x.skip, x.w, x.n, x.threads, x.seg_batches, x.batch_segs, x.parity, M, k, p, mass,
-                          __builtin_fmaxf(least, by_min));
+  x.long_row = true;
+  return x.from_row(k, p, mass, __builtin_fmaxf(least, by_min), draw, place);
 }
 
 template <bool kRules>
 __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   __shared__ Lds s;
   __shared__ uint32_t skip[kRules ? kMaxRuled / 32 : 1];
+  __shared__ int32_t said[kRules ? kSaid : 1];
+  __shared__ float said_z[kRules ? kSaid : 1];
   const int b = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
   const int64_t tr = static_cast<int64_t>(b) * a.N, orow = static_cast<int64_t>(b) * (a.Dmax + 1);
   const int n = min(max(a.n_nodes[b], 1), a.N);
@@ -792,8 +860,8 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   }
   const int lane = tid % SRT_WAVE, wave = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE), e4 = a.V / 4;
   const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
-  Walker<kRules> walker = {a, s, skip, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
-                           max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f};
+  Walker<kRules> walker = {a, s, skip, said, said_z, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
+                           max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f, false};
   static_assert(kUnroll == 8 && kSegs % 8 == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
   while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
   const float p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
@@ -806,7 +874,13 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
     walker.n = k;
     // (what the thread's place decides is worked out where it is used, not kept over the walk in 100 registers)
     asm volatile("" : "+v"(walker.tid), "+v"(walker.lane));
-    if constexpr (kRules) mark(a, walker.w, s.path, k, 0, a.V, skip, threads);
+    if constexpr (kRules) {
+      // (penalties that change nothing: no counts are read)
+      if (walker.w.r == 1.f && walker.w.f == 0.f && walker.w.p == 0.f) walker.w.seen = nullptr;
+      if (k == 0 && walker.w.seen) walker.list_said();
+      mark(a, walker.w, s.path, k, 0, a.V, skip, threads);
+      walker.mark_said();
+    }
     const u64 key = choose<kRules>(walker, top_k, p, mp);
     tok = key ? key_token(key) : -1;
     __syncthreads();  // (the staged tree, at the first step; LDS is the next row's from here on)
