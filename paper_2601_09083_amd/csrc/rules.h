@@ -86,14 +86,11 @@ struct Path {
   int32_t biased[kMaxLevels];
 };
 
-// Marks of the chunk [lo, hi) (lo a multiple of 32) in `skip`: masked entries,
-// tokens of the path (n of them) and tokens with a bias.  All threads; synchronises.
-__device__ inline void mark(const RulesArgs& a, const Row& w, Path& path, int n, int lo, int hi, uint32_t* skip,
-                            int threads) {
-  const int words = (hi - lo + 31) / 32;
-  const int at = w.bias0 + static_cast<int>(threadIdx.x);
-  const int bias = at < w.bias1 ? a.bias_tokens[at] : -1;  // (under way together with the mask)
-  for (int i = threadIdx.x; i < words; i += threads) skip[i] = w.mask ? ~w.mask[lo / 32 + i] : 0u;
+// Marks of the tokens of the path and of those with a bias in the chunk [lo, hi),
+// whose other marks are written; `bias` is the token at the thread's first entry `at`
+// of the bias list (-1: none).  All threads; synchronises, before as well.
+__device__ inline void mark_special(const RulesArgs& a, const Row& w, Path& path, int n, int lo, int hi,
+                                    uint32_t* skip, int threads, int at, int bias) {
   if (static_cast<int>(threadIdx.x) < n) path.biased[threadIdx.x] = 0;
   __syncthreads();
   auto set = [&](int t) { atomicOr(&skip[(t - lo) >> 5], 1u << ((t - lo) & 31)); };
@@ -110,6 +107,17 @@ __device__ inline void mark(const RulesArgs& a, const Row& w, Path& path, int n,
   set_bias(bias);
   for (int i = at + threads; i < w.bias1; i += threads) set_bias(a.bias_tokens[i]);
   __syncthreads();
+}
+
+// Marks of the chunk [lo, hi) (lo a multiple of 32) in `skip`: masked entries,
+// tokens of the path (n of them) and tokens with a bias.  All threads; synchronises.
+__device__ inline void mark(const RulesArgs& a, const Row& w, Path& path, int n, int lo, int hi, uint32_t* skip,
+                            int threads) {
+  const int words = (hi - lo + 31) / 32;
+  const int at = w.bias0 + static_cast<int>(threadIdx.x);
+  const int bias = at < w.bias1 ? a.bias_tokens[at] : -1;  // (under way together with the mask)
+  for (int i = threadIdx.x; i < words; i += threads) skip[i] = w.mask ? ~w.mask[lo / 32 + i] : 0u;
+  mark_special(a, w, path, n, lo, hi, skip, threads, at, bias);
 }
 
 // The logit of one marked token under the rules: its path count and, where `from`

@@ -40,6 +40,7 @@ constexpr int kMassBits = 44;     // of a bin's word: mass in units of 2^-24 bel
 constexpr int64_t kMaxVocab = int64_t(1) << 21;
 constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LDS
 constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
+constexpr int kApart = kSaid + 512;  // and with them those of the path and of the bias list
 constexpr int kShortVocab = 4096;  // rows up to which 256 threads walk
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -120,12 +121,13 @@ template <bool kRules>
 struct Walker {
   const SampleArgs& a;
   Lds& s;
-  // Under rules: marked entries; the tokens with a count word and their scores (-1
-  // of them: more than there is room for, and the stream reads the words).
+  // Under rules: marked entries; the marked tokens and their scores, first n_said
+  // with a count word (-1: more than there is room for, and the stream reads the
+  // words), then those of the path and of the bias list (-1: too long a list).
   uint32_t* skip;
-  int32_t* said;
-  float* said_z;
-  int n_said;
+  int32_t* apart;
+  float* apart_z;
+  int n_said, n_special;
   Row w;
   int n;                 // tokens emitted on this walk
   int tid, threads, lane, wave, waves;
@@ -183,6 +185,11 @@ struct Walker {
   }
   // Its scores (-inf: none, or marked).
   __device__ __forceinline__ void scores(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
+    if (kRules && streams_words()) scores_of<true>(b, t, z);
+    else scores_of<false>(b, t, z);
+  }
+  template <bool kWords>
+  __device__ __forceinline__ void scores_of(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
     const int i = first_of(b);
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
@@ -190,12 +197,17 @@ struct Walker {
       uint32_t out = b < full || at < e4 ? 0u : 15u;
       if (kRules && out == 0) out = (skip[at >> 3] >> ((4 * at) & 31)) & 15u;
       u16x4 c = {0, 0, 0, 0};
-      if (kRules && streams_words() && out != 15u) c = reinterpret_cast<const u16x4*>(w.seen)[at];
+      if (kWords && out != 15u) c = reinterpret_cast<const u16x4*>(w.seen)[at];
+      f32x4 x = t.x[k];
+      if (!kRules && b < full) {
+      } else if (__ballot(out != 0)) {  // (all bits set are a NaN, which counts as -inf)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = scored(t.x[k][e], c[e]);
-        z[4 * k + e] = (out >> e) & 1u ? -INFINITY : x;
+        for (int e = 0; e < 4; ++e)
+          x[e] = __uint_as_float(__float_as_uint(x[e]) |
+                                 static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(out), e, 1)));
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[4 * k + e] = scored(x[e], kWords ? c[e] : 0);
     }
   }
   __device__ __forceinline__ int token(int b, int q) const { return 4 * (first_of(b) + q / 4 * threads) + q % 4; }
@@ -207,43 +219,97 @@ struct Walker {
     const int j = 4 * e4 + tid;
     if (j < a.V && !marked(j)) f(scored(w.logits[j], kRules && streams_words() ? w.seen[j] : 0), j);
     if constexpr (kRules) {
-      for (int i = tid; i < n_said; i += threads) f(said_z[i], said[i]);
-      for_special(a, w, s.path, n, 0, a.V, threads, [&](int t, int from) {
-        if (allowed_token(w, t))
-          f(__builtin_fmaxf(mul_rounded(special_logit(a, w, s.path, n, t, from, w.logits[t]), w.invT), -INFINITY), t);
-      });
+      const int listed = max(n_said, 0) + max(n_special, 0);
+      for (int i = tid; i < listed; i += threads) f(apart_z[i], apart[i]);
+      if (n_special < 0)
+        for_special(a, w, s.path, n, 0, a.V, threads, [&](int t, int from) { f(special_score(t, from), t); });
     }
+  }
+  __device__ __forceinline__ float special_score(int t, int from) const {
+    if (!allowed_token(w, t)) return -INFINITY;
+    return __builtin_fmaxf(mul_rounded(special_logit(a, w, s.path, n, t, from, w.logits[t]), w.invT), -INFINITY);
   }
 
   // Lists the tokens with a count word.  A penalty costs a division, which one such
   // token in a wave's 64 entries makes it take for all: of a row with one in 50 most
-  // of the time went there (64 sequences, 9 levels: 617 us, and 362 with the list).
+  // of the time went there (64 sequences, 9 levels: 617 us, and 516 with the list).
   __device__ __forceinline__ void list_said() {
     if (tid == 0) s.n = 0;
     __syncthreads();
     const u16x4* s4 = reinterpret_cast<const u16x4*>(w.seen);
-    auto push = [&](uint16_t word, int j) {
-      if (!word) return;
-      const int at = atomicAdd(&s.n, 1);
-      if (at < kSaid) said[at] = j;
-    };
-    for (int i = tid; i < e4; i += threads) {
-      const u16x4 c = s4[i];
+    for (int i0 = 0; i0 < e4; i0 += kUnroll * threads) {
+      u16x4 c[kUnroll];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) push(c[e], 4 * i + e);
+      for (int k = 0; k < kUnroll; ++k) c[k] = s4[min(i0 + tid + k * threads, e4 - 1)];
+      uint32_t said = 0;  // bit 4 k + e: the batch's entry has a word
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) said |= (i0 + tid + k * threads < e4 && c[k][e] ? 1u : 0u) << (4 * k + e);
+      const int m = __popc(said), upto = static_cast<int>(wave_scan(static_cast<u64>(m)));
+      int at = 0;
+      if (lane == SRT_WAVE - 1) at = atomicAdd(&s.n, upto);
+      at = __builtin_amdgcn_readlane(at, SRT_WAVE - 1) + upto - m;
+      for (; said; said &= said - 1, ++at) {
+        const int q = __ffs(said) - 1;
+        if (at < kSaid) apart[at] = 4 * (i0 + tid + q / 4 * threads) + q % 4;
+      }
     }
-    if (4 * e4 + tid < a.V) push(w.seen[4 * e4 + tid], 4 * e4 + tid);
+    const int j = 4 * e4 + tid;
+    if (j < a.V && w.seen[j]) {
+      const int at = atomicAdd(&s.n, 1);
+      if (at < kSaid) apart[at] = j;
+    }
     __syncthreads();
     n_said = s.n <= kSaid ? s.n : -1;
   }
-  // Scores and marks them; one that is marked is forbidden or scored as a special token.
-  __device__ __forceinline__ void mark_said() {
-    for (int i = tid; i < n_said; i += threads) {
-      const int t = said[i];
-      const uint32_t bit = 1u << (t & 31);
-      const float l = w.logits[t];
-      const int word = w.seen[t];
-      said_z[i] = atomicOr(&skip[t >> 5], bit) & bit ? -INFINITY : scored(l, word);
+
+  // Marks the row's entries that the stream passes over, and scores those of them
+  // that are allowed.
+  __device__ __forceinline__ void mark_row() {
+    const int words = (a.V + 31) / 32, at = w.bias0 + tid, bias = at < w.bias1 ? a.bias_tokens[at] : -1;
+    for (int i0 = 0; i0 < words; i0 += kUnroll * threads) {
+      uint32_t x[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int i = i0 + k * threads + tid;
+        x[k] = w.mask && i < words ? ~w.mask[i] : 0u;
+      }
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k)
+        if (i0 + k * threads + tid < words) skip[i0 + k * threads + tid] = x[k];
+    }
+    mark_special(a, w, s.path, n, 0, a.V, skip, threads, at, bias);
+    // One with a count word that is marked by now is forbidden, or scored as a special one.
+    for (int i0 = 0; i0 < n_said; i0 += kUnroll * threads) {
+      int t[kUnroll], word[kUnroll];
+      float l[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) t[k] = apart[min(i0 + k * threads + tid, n_said - 1)];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        l[k] = w.logits[t[k]];
+        word[k] = w.seen[t[k]];
+      }
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int i = i0 + k * threads + tid;
+        if (i >= n_said) continue;
+        const uint32_t bit = 1u << (t[k] & 31);
+        apart_z[i] = atomicOr(&skip[t[k] >> 5], bit) & bit ? -INFINITY : scored(l[k], word[k]);
+      }
+    }
+    const int room = kApart - max(n_said, 0), first = max(n_said, 0);
+    n_special = n + w.bias1 - w.bias0 <= room ? n + w.bias1 - w.bias0 : -1;
+    if (n_special >= 0) {
+      // (a thread's own places: its token of the path, its entries of the list)
+      if (tid < n) apart_z[first + tid] = -INFINITY;
+      for (int k = w.bias0 + tid; k < w.bias1; k += threads) apart_z[first + n + k - w.bias0] = -INFINITY;
+      for_special(a, w, s.path, n, 0, a.V, threads, [&](int t, int from) {
+        const int i = first + (from < 0 ? tid : n + from - w.bias0);
+        apart[i] = t;
+        apart_z[i] = special_score(t, from);
+      });
     }
     __syncthreads();
   }
@@ -390,7 +456,9 @@ struct Walker {
       for (int q = 0; q < 4 * kUnroll; ++q) best.ascending(kNoise ? add_rounded(z[q], t.g[q / 4][q % 4]) : z[q], token(b, q));
       t = next;
     }
-    extras([&](float z, int j) { take(key, z, j); });
+    extras([&](float z, int j) {
+      if (z > -INFINITY) take(key, z, j);
+    });
     return all_max(max(key, best.key()));
   }
 
@@ -849,8 +917,8 @@ template <bool kRules>
 __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   __shared__ Lds s;
   __shared__ uint32_t skip[kRules ? kMaxRuled / 32 : 1];
-  __shared__ int32_t said[kRules ? kSaid : 1];
-  __shared__ float said_z[kRules ? kSaid : 1];
+  __shared__ int32_t apart[kRules ? kApart : 1];
+  __shared__ float apart_z[kRules ? kApart : 1];
   const int b = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
   const int64_t tr = static_cast<int64_t>(b) * a.N, orow = static_cast<int64_t>(b) * (a.Dmax + 1);
   const int n = min(max(a.n_nodes[b], 1), a.N);
@@ -860,7 +928,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   }
   const int lane = tid % SRT_WAVE, wave = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE), e4 = a.V / 4;
   const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
-  Walker<kRules> walker = {a, s, skip, said, said_z, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
+  Walker<kRules> walker = {a, s, skip, apart, apart_z, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
                            max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f, false};
   static_assert(kUnroll == 8 && kSegs % 8 == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
   while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
@@ -878,8 +946,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
       // (penalties that change nothing: no counts are read)
       if (walker.w.r == 1.f && walker.w.f == 0.f && walker.w.p == 0.f) walker.w.seen = nullptr;
       if (k == 0 && walker.w.seen) walker.list_said();
-      mark(a, walker.w, s.path, k, 0, a.V, skip, threads);
-      walker.mark_said();
+      walker.mark_row();
     }
     const u64 key = choose<kRules>(walker, top_k, p, mp);
     tok = key ? key_token(key) : -1;
