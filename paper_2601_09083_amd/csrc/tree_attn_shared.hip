@@ -33,6 +33,7 @@ struct SharedArgs : AttnBase {
   int32_t* seq_prefix;   // [B] keys that the sequence's group takes for it
   int32_t* node_of;      // live nodes of the sharing sequences, group by group: sequence << 8 | node
 };
+constexpr int kPlanChunk = 4;  // word of the plan: keys per split
 constexpr uint32_t kPrefixItem = 1u << 31;  // of an item's first word: sequence or group | row block << 16
 
 // Buffer descriptor over `nbytes` bytes at `base` (loads past nbytes read 0).
@@ -67,6 +68,7 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
   const int lane = tid % SRT_WAVE;
   const int l32 = lane % 32;  // query row of this lane inside the wave's 32
   const int h = lane / 32;    // lane half
+  const int chunk = a.plan[kPlanChunk];
 
   // `b`: a sequence, or a group whose rows take a split of their shared prefix.
   auto run_item = [&](const int b, const int g, const int s, const int rb, const bool prefix) {
@@ -81,14 +83,14 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
   } else {
     si = seq_info(a, b);
     k0 = a.seq_prefix[b];
-    part += (k0 + a.chunk - 1) / a.chunk;
-    nsplit = part - s + (si.total - k0 + a.chunk - 1) / a.chunk;
+    part += (k0 + chunk - 1) / chunk;
+    nsplit = part - s + (si.total - k0 + chunk - 1) / chunk;
   }
   const int rows = si.n * a.G;
   if (rb * kRowsPerBlock >= rows) return;
-  const int k_begin = k0 + s * a.chunk;
+  const int k_begin = k0 + s * chunk;
   if (k_begin >= si.total) return;
-  const int k_end = min(k_begin + a.chunk, si.total);
+  const int k_end = min(k_begin + chunk, si.total);
   const int ntiles = (k_end - k_begin + kTile - 1) / kTile;
   const int row0 = rb * kRowsPerBlock + w * kRowsPerWave;
   const bool wave_active = row0 < rows;  // wave-uniform
@@ -462,72 +464,127 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
 
 
 constexpr int kMaxGroups = 4096;   // groups of a batch, whose counts are held in LDS
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanWaves = kPlanThreads / SRT_WAVE;
-constexpr int kGroupsEach = kMaxGroups / kPlanThreads;
-constexpr int kSeqs = 16;          // sequences or groups that a wave of the plan kernel lists at a time
+constexpr int kGroupsEach = 4;     // of a thread of the plan kernel
+// Sequences and groups up to which the plan kernel has 256 threads: a wave to a SIMD
+// runs the steps that do not depend on the batch's size in a quarter of the time.
+constexpr int kSmallPlan = 512;
+constexpr int kFew = 16;           // items or nodes up to which a thread lists them by itself
+constexpr int kMaxSplits = 32;     // of all keys of a sequence, about: a row's partial results are joined one by one
 
 struct PlanArgs {
   const int32_t* group_ids;
   const int32_t* prefix_len;
-  int32_t n_groups;
+  int32_t n_groups, slots, least_chunk;  // (slots: workgroups that run at a time)
 };
 
-// One workgroup: groups, item classes (as tree_attn_plan_kernel), then the lists.
+// What a thread lists, or leaves to a wave: a group's or a sequence's items.
+struct Listing {
+  int id, nodes, keys, at0, at1, list;  // (a sequence's place in its group's list of nodes, or -1)
+};
+
+// Sum over the wave in its last lane, by DPP adds as wave_sum's.
+__device__ inline float wave_sum_f(float x) {
+  auto step = [&](auto ctrl, auto rows) {
+    x += __uint_as_float(__builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(x)), decltype(ctrl)::value,
+                                                     decltype(rows)::value, 0xf, false));
+  };
+  typedef std::integral_constant<int, 0xf> all;
+  step(std::integral_constant<int, 0x111>(), all());
+  step(std::integral_constant<int, 0x112>(), all());
+  step(std::integral_constant<int, 0x114>(), all());
+  step(std::integral_constant<int, 0x118>(), all());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+  return x;
+}
+
+// What a batch takes with each number of keys per split, in tiles of a CU's time.
+constexpr int kChunks = 6;  // 256 .. 8192
+struct Load {
+  float full = 0.f, rest = 0.f, items = 0.f, parts = 0.f;  // of a KV head: whole splits, other tiles, items, row parts
+  __device__ void add(int total, int rbs, int c) {
+    const int whole = total / (kSmallChunk << c), left = total - whole * (kSmallChunk << c);
+    full += static_cast<float>(whole) * rbs;
+    rest += static_cast<float>((left + kTile - 1) / kTile) * rbs;
+    items += static_cast<float>(whole + (left > 0)) * rbs;
+  }
+};
+constexpr float kItemTiles = 2.f;      // of an item's start and end
+constexpr float kPartTiles = 1e-4f;    // of a row's part (1 KB written and read, by all CUs), times CUs
+
+// One workgroup: groups, keys per split, item classes (as tree_attn_plan_kernel),
+// then the lists.  A thread of a batch has at most one group or sequence of 1024 at a
+// time, and lists its items if they are few; a wave at a time lists the others.
+// (A wave for every sequence took 19 us for 256 of them, 12 so.)
+template <int kPlanThreads>
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a, PlanArgs p) {
+  constexpr int kPlanWaves = kPlanThreads / SRT_WAVE, kGroups = kGroupsEach * kPlanThreads;
   __shared__ int32_t cnt[kPlanKeys], off[kPlanKeys];
-  __shared__ int32_t members[kMaxGroups], nodes[kMaxGroups], keys[kMaxGroups], lead[kMaxGroups];
+  __shared__ int32_t members[kGroups], nodes[kGroups], keys[kGroups], lead[kGroups], alone[kGroups];
   __shared__ int32_t wsum[2][kPlanWaves];
-  __shared__ int32_t ncomb, widest;
+  __shared__ Listing left[kPlanThreads];
+  __shared__ int32_t ncomb, widest, n_left, most;
+  __shared__ float loads[kPlanWaves][4 * kChunks], totals[4 * kChunks];
   const int tid = threadIdx.x, lane = tid % SRT_WAVE, wv = tid / SRT_WAVE;
-  const int cshift = 31 - __clz(a.chunk);
   auto group_of = [&](int b) {
     const int g = p.n_groups > 0 ? p.group_ids[b] : -1;
     return g >= 0 && g < p.n_groups ? g : -1;
   };
-  auto row_blocks = [&](int rows) { return (rows + kRowsPerBlock - 1) / kRowsPerBlock; };
-  // Visits the item classes of `n` nodes against `total` keys: f(class, key, splits).
-  auto classes = [&](int total, int n, auto&& f) {
-    const int full = total >> cshift, tail = total - (full << cshift);
-    const int waves = min(kWaves, (n * a.G + kRowsPerWave - 1) / kRowsPerWave);
-    if (full > 0) f(0, plan_key(a.chunk / kTile, waves), full);
-    if (tail > 0) f(1, plan_key((tail + kTile - 1) / kTile, waves), 1);
-  };
-  auto count = [&](int total, int n) {
-    const int per = a.Hkv * row_blocks(n * a.G);
-    classes(total, n, [&](int, int key, int ns) { atomicAdd(&cnt[key], ns * per); });
-  };
+  auto row_blocks = [&](int n) { return (n * a.G + kRowsPerBlock - 1) / kRowsPerBlock; };
+  // What a tile of keys costs for the rows of n nodes: a workgroup's part in it, and its waves'.
+  auto tile_cost = [&](int n) { return kWaves * row_blocks(n) + (n * a.G + kRowsPerWave - 1) / kRowsPerWave; };
 
   for (int k = tid; k < kPlanKeys; k += kPlanThreads) cnt[k] = 0;
   for (int g = tid; g < p.n_groups; g += kPlanThreads) {
-    members[g] = nodes[g] = 0;
+    members[g] = nodes[g] = alone[g] = 0;
     keys[g] = lead[g] = 0x7fffffff;
   }
-  if (tid == 0) ncomb = widest = 0;
-  __syncthreads();
-  for (int b = tid; b < a.B; b += kPlanThreads) {
-    const int g = group_of(b);
-    if (g < 0) continue;
-    const SeqInfo si = seq_info(a, b);
-    atomicAdd(&members[g], 1);
-    atomicAdd(&nodes[g], si.n);
-    atomicMin(&keys[g], si.L);
-    atomicMin(&lead[g], b);
-  }
-  __syncthreads();
-  // Keys that each group shares, and where its nodes' list starts.
-  int mine[kGroupsEach], sum = 0;
+  if (tid == 0) ncomb = widest = most = 0;
+  SeqInfo si = {0, 0, 0};  // of this thread's sequence of the current 1024, and its group
+  int mine = -1;
+  auto take = [&](int b) {
+    si = seq_info(a, b);
+    mine = group_of(b);
+  };
+  if (tid < a.B) take(tid);
+  int stated[kGroupsEach];
 #pragma unroll
   for (int j = 0; j < kGroupsEach; ++j) {
     const int g = tid * kGroupsEach + j;
-    mine[j] = 0;
+    stated[j] = g < p.n_groups ? p.prefix_len[g] : 0;
+  }
+  __syncthreads();
+  for (int b = tid; b < a.B; b += kPlanThreads) {
+    if (b >= kPlanThreads) take(b);
+    if (mine < 0) continue;
+    atomicAdd(&members[mine], 1);
+    atomicAdd(&nodes[mine], si.n);
+    atomicAdd(&alone[mine], tile_cost(si.n));
+    atomicMin(&keys[mine], si.L);
+    atomicMin(&lead[mine], b);
+  }
+  __syncthreads();
+  // Keys that each group shares, where its nodes' list starts, and what the items take.
+  int sum = 0;
+  Load load[kChunks];
+  int longest = 0;  // keys of a group or a sequence
+#pragma unroll
+  for (int j = 0; j < kGroupsEach; ++j) {
+    const int g = tid * kGroupsEach + j;
     if (g >= p.n_groups) continue;
-    int P = min(p.prefix_len[g], keys[g]);
+    int P = min(stated[j], keys[g]);
     P = members[g] > 1 && P > 0 ? P & ~(a.page - 1) : 0;
+    // Where the rows fill the tiles by themselves, sharing saves less than the parts
+    // cost that it makes of every row (32 prompts of 2k to 4k keys with eight answers,
+    // 28 heads, full trees of 64 nodes: 929 us a call shared, 738 not; trees of 1 to
+    // 64 nodes of 12 heads: 139 and 156).
+    if (static_cast<int64_t>(alone[g] - tile_cost(nodes[g])) * (P / kTile) < static_cast<int64_t>(nodes[g]) * a.G) P = 0;
     keys[g] = P;
-    if (P > 0) mine[j] = nodes[g];
-    sum += mine[j];
-    if (P > 0) count(P, nodes[g]);
+    if (P == 0) nodes[g] = 0;
+    sum += nodes[g];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) load[c].add(P, row_blocks(nodes[g]), c);
+    longest = max(longest, P);
   }
   auto scan = [&](int x, int32_t* ws) {  // exclusive prefix sum over the workgroup
     int incl = x;
@@ -539,79 +596,169 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a,
     if (lane == SRT_WAVE - 1) ws[wv] = incl;
     __syncthreads();
     int before = 0;
-    for (int j = 0; j < wv; ++j) before += ws[j];
+#pragma unroll
+    for (int j = 0; j < kPlanWaves; ++j) before += j < wv ? ws[j] : 0;
     return before + incl - x;
   };
-  int at = scan(sum, wsum[0]);
+  int at = scan(sum, wsum[0]);  // (its barrier orders keys[] and nodes[] too)
 #pragma unroll
   for (int j = 0; j < kGroupsEach; ++j) {
     const int g = tid * kGroupsEach + j;
     if (g >= p.n_groups) continue;
-    a.group[g] = make_int4(lead[g], keys[g], at, mine[j]);
+    a.group[g] = make_int4(lead[g], keys[g], at, nodes[g]);
     members[g] = at;  // from here on: the next free entry of the group's list
-    at += mine[j];
+    at += nodes[g];
   }
-  // Own keys of the sequences.  (The barrier of the scan ordered keys[].)
   for (int b = tid; b < a.B; b += kPlanThreads) {
-    const SeqInfo si = seq_info(a, b);
-    const int g = group_of(b);
-    count(si.total - (g >= 0 ? keys[g] : 0), si.n);
+    if (a.B > kPlanThreads) take(b);
+    const int P = mine >= 0 ? keys[mine] : 0;
+    a.seq_prefix[b] = P;
+    longest = max(longest, si.total - P);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      load[c].add(si.total - P, row_blocks(si.n), c);
+      const int least = kSmallChunk << c, parts = (P + least - 1) / least + (si.total - P + least - 1) / least;
+      if (parts > 1) load[c].parts += static_cast<float>(parts) * si.n * a.G;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const float x[4] = {wave_sum_f(load[c].full), wave_sum_f(load[c].rest), wave_sum_f(load[c].items),
+                        wave_sum_f(load[c].parts)};
+    if (lane == SRT_WAVE - 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) loads[wv][4 * c + j] = x[j];
+  }
+#pragma unroll
+  for (int d = SRT_WAVE / 2; d >= 1; d >>= 1) longest = max(longest, shfl_xor(longest, d));
+  if (lane == 0) atomicMax(&most, longest);
+  __syncthreads();
+  if (tid < 4 * kChunks) {  // (in the same order always, so that a batch's splits are the same ones)
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPlanWaves; ++i) x += loads[i][tid];
+    totals[tid] = x;
   }
   __syncthreads();
-  static_assert(kPlanKeys <= kPlanThreads, "one class per thread");
-  const int n = tid < kPlanKeys ? cnt[tid] : 0;
-  const int before = scan(n, wsum[1]);
-  if (tid < kPlanKeys) off[tid] = before;
+  // Keys per split: those with which the batch is done first.
+  int chunk = kChunk;
+  float least_time = INFINITY;
+#pragma unroll
+  for (int c = kChunks - 1; c >= 0; --c) {
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = totals[4 * c + j];
+    // Rounds of whole splits, then the rest of them, around which the others lie.
+    const float each = (kSmallChunk << c) / kTile, whole = x[0] * a.Hkv, rounds = floorf(whole / p.slots);
+    const float over = whole - rounds * p.slots, fill = (over * each + x[1] * a.Hkv) / p.slots;
+    const float time = fmaxf(rounds * each + (over > 0.f ? fmaxf(each, fill) : fill),
+                             fminf(each, static_cast<float>(most / kTile))) +
+                       x[2] * a.Hkv / p.slots * kItemTiles + x[3] * a.Hkv * kPartTiles;
+    if (time < least_time && (kSmallChunk << c) >= p.least_chunk) {
+      least_time = time;
+      chunk = kSmallChunk << c;
+    }
+  }
+  const int cshift = 31 - __clz(chunk);
+  auto splits_of = [&](int total) { return (total + chunk - 1) >> cshift; };
+  // Visits the item classes of `n` nodes against `total` keys: f(class, key, splits).
+  auto classes = [&](int total, int n, auto&& f) {
+    const int full = total >> cshift, tail = total - (full << cshift);
+    const int waves = min(kWaves, (n * a.G + kRowsPerWave - 1) / kRowsPerWave);
+    if (full > 0) f(0, plan_key(chunk / kTile, waves), full);
+    if (tail > 0) f(1, plan_key((tail + kTile - 1) / kTile, waves), 1);
+  };
+  auto count = [&](int total, int n) {
+    const int per = a.Hkv * row_blocks(n);
+    if (n > 0) classes(total, n, [&](int, int key, int ns) { atomicAdd(&cnt[key], ns * per); });
+  };
+  for (int g = tid; g < p.n_groups; g += kPlanThreads) count(keys[g], nodes[g]);
+  for (int b = tid; b < a.B; b += kPlanThreads) {
+    if (a.B > kPlanThreads) take(b);
+    count(si.total - (mine >= 0 ? keys[mine] : 0), si.n);
+  }
+  __syncthreads();
+  static_assert(kPlanKeys % kPlanThreads == 0, "classes of a thread");
+  constexpr int kKeysEach = kPlanKeys / kPlanThreads;
+  int n[kKeysEach], in_all = 0;
+#pragma unroll
+  for (int j = 0; j < kKeysEach; ++j) in_all += n[j] = cnt[tid * kKeysEach + j];
+  int before = scan(in_all, wsum[1]);
+#pragma unroll
+  for (int j = 0; j < kKeysEach; ++j) {
+    off[tid * kKeysEach + j] = before;
+    before += n[j];
+  }
   if (tid == kPlanThreads - 1) {
-    a.plan[0] = before + n;  // all classes
+    a.plan[0] = before;  // all classes
     a.plan[1] = 0;
+    a.plan[kPlanChunk] = chunk;
   }
   __syncthreads();
-  // The lists: a wave takes kSeqs groups, then sequences, at a time; a lane each
-  // reserves its places, and all lanes write the items.
+  // The lists, 1024 groups and then 1024 sequences at a time.
   int wide = 0;
-  const int group_steps = (p.n_groups + kSeqs - 1) / kSeqs, seq_steps = (a.B + kSeqs - 1) / kSeqs;
-  for (int step = wv; step < group_steps + seq_steps; step += kPlanWaves) {
+  const int group_steps = (p.n_groups + kPlanThreads - 1) / kPlanThreads;
+  const int seq_steps = (a.B + kPlanThreads - 1) / kPlanThreads;
+  for (int step = 0; step < group_steps + seq_steps; ++step) {
     const bool prefix = step < group_steps;
-    const int x = (prefix ? step : step - group_steps) * kSeqs + lane;
-    int total = 0, n = 0, listed = -1, pos[2] = {0, 0};
-    if (lane < kSeqs && x < (prefix ? p.n_groups : a.B)) {
+    const int x = (prefix ? step : step - group_steps) * kPlanThreads + tid;
+    const uint32_t kind = prefix ? kPrefixItem : 0u;
+    auto write = [&](int to, int id, int g, int s, int rb) {
+      *reinterpret_cast<int2*>(a.plan + kPlanHeader + 2 * to) =
+          make_int2(static_cast<int>(static_cast<uint32_t>(id | rb << 16) | kind), g | s << 8);
+    };
+    if (tid == 0) n_left = 0;
+    __syncthreads();
+    Listing m = {x, 0, 0, 0, 0, -1};
+    if (x < (prefix ? p.n_groups : a.B)) {
       if (prefix) {
-        total = keys[x];
-        n = total > 0 ? nodes[x] : 0;
+        m.keys = keys[x];
+        m.nodes = nodes[x];
       } else {
-        const SeqInfo si = seq_info(a, x);
-        const int g = group_of(x), P = g >= 0 ? keys[g] : 0;
-        total = si.total - P;
-        n = si.n;
-        a.seq_prefix[x] = P;
-        const int parts = ((P + a.chunk - 1) >> cshift) + ((total + a.chunk - 1) >> cshift);
-        if (P > 0) listed = atomicAdd(&members[g], n);
+        if (a.B > kPlanThreads) take(x);
+        const int P = mine >= 0 ? keys[mine] : 0;
+        m.keys = si.total - P;
+        m.nodes = si.n;
+        if (P > 0) m.list = atomicAdd(&members[mine], si.n);
+        const int parts = splits_of(P) + splits_of(m.keys);
         if (parts > 1) {
-          *reinterpret_cast<int2*>(a.plan + a.combine_at + 2 * atomicAdd(&ncomb, 1)) = make_int2(x | parts << 16, n * a.G);
-          wide = max(wide, n * a.G);
+          *reinterpret_cast<int2*>(a.plan + a.combine_at + 2 * atomicAdd(&ncomb, 1)) =
+              make_int2(x | parts << 16, si.n * a.G);
+          wide = max(wide, si.n * a.G);
         }
       }
-      const int per = a.Hkv * row_blocks(n * a.G);
-      classes(total, n, [&](int c, int key, int ns) { pos[c] = atomicAdd(&off[key], ns * per); });
     }
-    for (int i = 0; i < kSeqs; ++i) {
-      const int n_i = __builtin_amdgcn_readlane(n, i);
-      if (n_i == 0) continue;
-      const int total_i = __builtin_amdgcn_readlane(total, i), id = __builtin_amdgcn_readlane(x, i);
-      const int p0 = __builtin_amdgcn_readlane(pos[0], i), p1 = __builtin_amdgcn_readlane(pos[1], i);
-      const int list = __builtin_amdgcn_readlane(listed, i);
-      const int rbs = row_blocks(n_i * a.G), per = a.Hkv * rbs, full = total_i >> cshift;
-      const int splits = (total_i + a.chunk - 1) >> cshift;
-      for (int y = lane; y < splits * per; y += SRT_WAVE) {
-        const int s = y / per, r = y - s * per, g = r / rbs, rb = r - g * rbs;
-        const int to = s < full ? p0 + y : p1 + y - full * per;
-        *reinterpret_cast<int2*>(a.plan + kPlanHeader + 2 * to) =
-            make_int2(static_cast<int>(static_cast<uint32_t>(id | rb << 16) | (prefix ? kPrefixItem : 0u)), g | s << 8);
+    if (m.nodes > 0) {
+      const int rbs = row_blocks(m.nodes), per = a.Hkv * rbs, splits = splits_of(m.keys);
+      classes(m.keys, m.nodes, [&](int c, int key, int ns) {
+        const int to = atomicAdd(&off[key], ns * per);
+        (c == 0 ? m.at0 : m.at1) = to;
+      });
+      if (splits * per <= kFew && (m.list < 0 || m.nodes <= kFew)) {
+        const int full = m.keys >> cshift;
+        for (int s = 0; s < splits; ++s) {
+          int to = s < full ? m.at0 + s * per : m.at1;
+          for (int g = 0; g < a.Hkv; ++g)
+            for (int rb = 0; rb < rbs; ++rb, ++to) write(to, x, g, s, rb);
+        }
+        if (m.list >= 0)
+          for (int y = 0; y < m.nodes; ++y) a.node_of[m.list + y] = x << 8 | y;
+      } else {
+        left[atomicAdd(&n_left, 1)] = m;
       }
-      if (list >= 0)
-        for (int y = lane; y < n_i; y += SRT_WAVE) a.node_of[list + y] = id << 8 | y;
     }
+    __syncthreads();
+    for (int i = wv; i < n_left; i += kPlanWaves) {
+      const Listing l = left[i];
+      const int rbs = row_blocks(l.nodes), per = a.Hkv * rbs, full = l.keys >> cshift, splits = splits_of(l.keys);
+      for (int y = lane; y < splits * per; y += SRT_WAVE) {
+        const int s = y / per, r = y - s * per, g = r / rbs;
+        write(s < full ? l.at0 + y : l.at1 + y - full * per, l.id, g, s, r - g * rbs);
+      }
+      if (l.list >= 0)
+        for (int y = lane; y < l.nodes; y += SRT_WAVE) a.node_of[l.list + y] = l.id << 8 | y;
+    }
+    __syncthreads();
   }
 #pragma unroll
   for (int d = SRT_WAVE / 2; d >= 1; d >>= 1) wide = max(wide, __shfl_xor(wide, d, SRT_WAVE));
@@ -626,7 +773,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a,
 // What the sizes alone decide.
 struct Sizes {
   int64_t rb, items, units, rows;
-  int chunk, slots;      // keys per split; partial results of a row, at most
+  int chunk, slots;      // keys per split, at least; partial results of a row, at most
   size_t plan, groups, prefixes, nodes, part_rows, total;  // bytes
 };
 
@@ -636,7 +783,12 @@ Sizes sizes_for(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int64_
   Sizes z;
   const int32_t G = Hq / Hkv;
   z.rb = (static_cast<int64_t>(N) * G + kRowsPerBlock - 1) / kRowsPerBlock;
-  z.chunk = chunk_for(B, Hkv, z.rb, cap, false, 0);
+  // The least keys per split that the plan kernel may choose: kMaxSplits of all keys, and
+  // partial results of 1 GiB.
+  const int64_t row = static_cast<int64_t>(B) * Hkv * N * G * (d + 2) * sizeof(float);
+  z.chunk = kSmallChunk;
+  while (z.chunk < kChunk && (splits_for(cap, z.chunk) > kMaxSplits || (splits_for(cap, z.chunk) + 1) * row > (int64_t(1) << 30)))
+    z.chunk *= 2;
   // a prefix and a rest, each in splits of its own, take at most one part more than all keys together
   z.slots = splits_for(cap, z.chunk) + 1;
   z.items = static_cast<int64_t>(B) * Hkv * z.slots * z.rb;  // (a group's row blocks are no more than its members')
@@ -647,7 +799,17 @@ Sizes sizes_for(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d, int64_
   z.prefixes = round256(static_cast<size_t>(B) * sizeof(int32_t));
   z.nodes = round256(static_cast<size_t>(B) * N * sizeof(int32_t));
   z.total = z.plan + z.groups + z.prefixes + z.nodes + static_cast<size_t>(z.rows) * (d + 2) * sizeof(float);
+  z.total = std::max(z.total, scratch_for(B, N, Hq, Hkv, d, cap, chunk_for(B, Hkv, z.rb, cap, true, 0), false));
   return z;
+}
+
+// Whether srt_tree_attn gives every item a CU of its own: sharing has nothing to save
+// there, and a plan to make and parts to join (28 heads, 4 KV heads, single tokens: 4
+// answers to 2048 keys 28 us a call shared, 18 not; 16 to 2048 32 and 26; 32 to 2048, one
+// item too many for the CUs, 33 and 40).
+bool each_alone(int32_t B, int32_t Hkv, int64_t rb, int64_t cap, int cus) {
+  const int c = chunk_for(B, Hkv, rb, cap, true, 0);
+  return static_cast<int64_t>(B) * Hkv * splits_for(cap, c) * rb <= cus;
 }
 
 // Work-list packing: 16 bits of a sequence or group, 15 of a row block, 8 of a KV head, 24 of a split.
@@ -656,7 +818,6 @@ bool fits(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap, int32_t n_
   const int64_t rows = static_cast<int64_t>(B) * N * (Hq / Hkv);
   if (rows / kRowsPerBlock > 32766) return false;
   const Sizes z = sizes_for(B, N, Hq, Hkv, 128, cap, n_groups);
-  // (split counts of the combine's entries are 16 bits, and the tile kernel's offsets 31)
   return z.slots <= 32767 && z.items <= (int64_t(1) << 29) && z.units <= (int64_t(1) << 30);
 }
 
@@ -694,6 +855,12 @@ extern "C" int srt_tree_attn_shared(int32_t B, int32_t N, int32_t Hq, int32_t Hk
   if (!scratch || scratch_bytes < z.total) return SRT_ERR_CAPACITY;
   if (reinterpret_cast<uintptr_t>(scratch) % 256) return SRT_ERR_INVALID;
 
+  const int cus = cu_count();
+  if (cus <= 0) return SRT_ERR_HIP;
+  if (n_groups == 0 || each_alone(B, Hkv, z.rb, cap, cus))
+    return srt_tree_attn(B, N, Hq, Hkv, d, page, max_pages, num_pages, q, k_cache, v_cache, block_table, ctx_len,
+                         tree_parent, n_nodes, scale, out, scratch, scratch_bytes, stream);
+
   SharedArgs a;
   a.q = q;
   a.k = k_cache;
@@ -729,11 +896,11 @@ extern "C" int srt_tree_attn_shared(int32_t B, int32_t N, int32_t Hq, int32_t Hk
   a.part_o = reinterpret_cast<float*>(base + z.plan + z.groups + z.prefixes + z.nodes);
   a.part_ml = a.part_o + z.rows * d;
 
-  const int cus = cu_count();
-  if (cus <= 0) return SRT_ERR_HIP;
   const unsigned grid = static_cast<unsigned>(std::min<int64_t>(z.items, cus));
   hipStream_t s = as_stream(stream);
-  shared_plan_kernel<<<1, kPlanThreads, 0, s>>>(a, PlanArgs{group_ids, prefix_len, n_groups});
+  const PlanArgs plan = {group_ids, prefix_len, n_groups, cus, z.chunk};
+  if (B <= kSmallPlan && n_groups <= kSmallPlan) shared_plan_kernel<256><<<1, 256, 0, s>>>(a, plan);
+  else shared_plan_kernel<1024><<<1, 1024, 0, s>>>(a, plan);
   if (d == 128) shared_attn_kernel<128><<<grid, kThreads, 0, s>>>(a);
   else shared_attn_kernel<64><<<grid, kThreads, 0, s>>>(a);
   launch_combine(a, d, false, static_cast<unsigned>(combine_grid(a, cus)), s);
