@@ -7,7 +7,11 @@ paged KV cache, queries, logits, noise) and runs the calls of a step:
 and attends from the grown sequence).  With ``kv="e4m3"`` or ``"int8"`` the KV
 cache is held in 8 bits (``srt_tree_attn_quant``, ``srt_commit_quant``); with
 ``use_rules`` the policy decodes under sampling rules (``srt_accept_rules``,
-``srt_seen_add``).
+``srt_seen_add``), with ``use_sampling`` with a temperature, top-k, top-p and min-p of
+each sequence's own (``srt_accept_sample``).  With ``use_rope`` a step's queries, keys
+and values come from a projection, and are turned by their positions and written to
+the cache (``srt_rope_append``, ``srt_rope_rows``); with ``prefix`` the sequences of a
+prompt share its pages, which attention reads once (``srt_tree_attn_shared``).
 Only buffer management and argument passing happen here; every step of the
 path runs in the HIP kernels of libsrt.
 """
@@ -151,11 +155,17 @@ class VerifyState:
     rules: Optional[srt.Rules] = None
     seen: Optional[torch.Tensor] = None    # count rows [B, V] that the penalties read
     ended: Optional[torch.Tensor] = None   # [B] bool: under rules, sequences whose walk found every token forbidden
+    sampling: Optional[srt.Sampling] = None
+    prefix_len: Optional[torch.Tensor] = None  # [n_prompts] positions that the sequences of a prompt share
+    rope: Optional[srt.Rope] = None
+    projected: Optional[tuple] = None      # queries, keys and values of the tree's nodes before their positions turn them
 
     # ---- set-up ---------------------------------------------------------
     @classmethod
     def build(cls, cfg: W.Config, device="cuda", tokens: Optional[W.TokenWorkload] = None,
-              steps_headroom: int = 64, with_seqs: bool = True, kv_headroom: int = 0, kv: str = "bf16"):
+              steps_headroom: int = 64, with_seqs: bool = True, kv_headroom: int = 0, kv: str = "bf16", prefix=None):
+        """``prefix`` [n_prompts]: the sequences of a prompt have the keys and values of
+        their first prefix[p] positions in the same pages, as far as whole pages go."""
         tw = W.make_tokens(cfg) if tokens is None else tokens
         B = tw.batch
         streams, sp = [], []
@@ -177,6 +187,15 @@ class VerifyState:
         caches.insert(sp, ids, streams)
         seq_stream = ids[n_prior:] if with_seqs else caches.new_streams(B)
         q, k, v, bt, P = W.make_kv(cfg, tw.ctx_len, device=device, headroom=kv_headroom)
+        if prefix is not None:
+            if kv != "bf16":
+                raise ValueError("a shared prefix is of the bf16 cache")
+            bt = bt.to(torch.int32)
+            for p in range(cfg.n_prompts):
+                own = np.flatnonzero(tw.seq_prompt == p)
+                whole = min([int(prefix[p]), *(int(tw.ctx_len[b]) for b in own)]) // cfg.page
+                for b in own[1:]:
+                    bt[b, :whole] = bt[own[0], :whole]
         st = cls(cfg=cfg, tokens=tw, caches=caches, seq_stream=seq_stream.astype(np.int32), device=device,
                  prompt_ids=_dev(tw.seq_prompt, device), ctx_tail=_dev(tw.ctx_tail(), device),
                  draft_len=_dev(tw.draft_len(), device), attn_len=_dev(tw.ctx_len, device), q=q, k_cache=k,
@@ -189,6 +208,10 @@ class VerifyState:
         if kv != "bf16":
             st._quantise(kv)
             need = srt.srt_tree_attn_quant_scratch_bytes(st.kv, cfg.n_nodes, cfg.hq)
+        if prefix is not None:
+            st.prefix_len = _dev(np.asarray(prefix), device)
+            need = srt.srt_tree_attn_shared_scratch_bytes(B, cfg.n_nodes, cfg.hq, cfg.hkv, cfg.head_dim, cfg.page,
+                                                          int(bt.shape[1]), cfg.n_prompts)
         st.scratch = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
         return st
 
@@ -228,6 +251,23 @@ class VerifyState:
                                mask=mask, **(bias_lists(biases, dev) if biases is not None else {}))
         return self.rules
 
+    def use_sampling(self, inv_temperature=None, top_k=None, top_p=None, min_p=None):
+        """Sampling parameters (lists or arrays [B], or None) for the steps that
+        follow; the temperatures take the place of the steps' own."""
+        f = lambda x, d: None if x is None else _dev(np.asarray(x), self.device, d)
+        self.sampling = srt.Sampling(f(inv_temperature, torch.float32), f(top_k, torch.int32), f(top_p, torch.float32),
+                                     f(min_p, torch.float32))
+        return self.sampling
+
+    def use_rope(self, inv_freq, projected, interleaved: bool = False, factor: float = 1.0):
+        """The tree's vectors of the steps that follow are ``projected``: queries
+        [B, N, Hq, d], keys and values [B, N, Hkv, d], turned by their positions."""
+        self.rope = srt.Rope(inv_freq, interleaved, factor)
+        self.projected = tuple(projected)
+        if self.kv is not None:
+            self.k_new = torch.zeros_like(self.projected[1], memory_format=torch.contiguous_format)
+            self.v_new = self.projected[2].contiguous()
+
     def make_logits(self, boost: Optional[str] = None, sampled: bool = True, sigma: Optional[float] = None):
         """Per-node logits (boosting each node's first drafted child) and
         per-depth Gumbel noise, from the current tree."""
@@ -245,7 +285,21 @@ class VerifyState:
                                   chain=chain)
         return self.tree
 
+    def write_tree(self):
+        """The tree's vectors, turned by their positions, to where attention reads them."""
+        q, k, v = self.projected
+        n, depth = self.tree["n_nodes"], self.tree["tree_depth"]
+        if self.kv is not None:
+            srt.srt_rope_rows(self.rope, q, k, n, self.kv.ctx_len, depth=depth, q_out=self.q, k_out=self.k_new)
+        else:
+            srt.srt_rope_append(self.rope, q, k, v, n, self.k_cache, self.v_cache, self.block_table, self.attn_len,
+                                depth=depth, q_out=self.q)
+
     def attention(self):
+        if self.prefix_len is not None:
+            return srt.srt_tree_attn_shared(self.q, self.k_cache, self.v_cache, self.block_table, self.attn_len,
+                                            self.tree["tree_parent"], self.tree["n_nodes"], self.prompt_ids,
+                                            self.prefix_len, self.scale, out=self.attn_out, scratch=self.scratch)
         if self.kv is not None:
             return srt.srt_tree_attn_quant(self.q, self.kv, self.k_new, self.v_new, self.tree["tree_parent"],
                                            self.tree["n_nodes"], self.scale, out=self.attn_out, scratch=self.scratch)
@@ -257,7 +311,11 @@ class VerifyState:
         if self.accept_scratch is None:
             self.accept_scratch = torch.empty(max(srt.srt_accept_scratch_bytes(self.tokens.batch), 1),
                                               dtype=torch.uint8, device=self.device)
-        if self.rules is not None:
+        if self.sampling is not None:
+            self.acc = srt.srt_accept_sample(self.logits, self.gumbel, self.sampling, self.tree["tree_tokens"],
+                                             self.tree["tree_parent"], self.tree["n_nodes"], self.cfg.max_depth,
+                                             rules=self.rules, out=self.acc or None)
+        elif self.rules is not None:
             self.acc = srt.srt_accept_rules(self.logits, self.gumbel, inv_temperature, self.rules,
                                             self.tree["tree_tokens"], self.tree["tree_parent"], self.tree["n_nodes"],
                                             self.cfg.max_depth, out=self.acc or None, scratch=self.accept_scratch)
@@ -299,6 +357,8 @@ class VerifyState:
 
     def step(self, inv_temperature: float = 1.0):
         self.draft()
+        if self.rope is not None:
+            self.write_tree()
         self.attention()
         self.accept(inv_temperature)
         self.insert()

@@ -22,6 +22,13 @@ def i32(x):
     return torch.as_tensor(np.ascontiguousarray(x), dtype=torch.int32, device="cuda")
 
 
+def room(pairs):
+    """Positions of a block table at which srt_tree_attn would not give each of the
+    batch's items (1024 keys of a (sequence, KV head) pair) a CU of its own, so that the
+    call takes its own way whatever the number of pairs."""
+    return 0 if pairs > 256 else 1024 * (300 // pairs + 1)
+
+
 class Case:
     """Groups of given sizes and prefixes; own[b] keys behind the prefix.  Pages
     that no call may read hold NaN."""
@@ -47,7 +54,7 @@ class Case:
         for p in self.prefix // page:
             heads.append(order[at:at + p])
             at += p
-        self.bt = np.full((B, int(need.max()) + spare), -1, dtype=np.int32)
+        self.bt = np.full((B, max(int(need.max()) + spare, room(B * hkv) // page)), -1, dtype=np.int32)
         for b in range(B):
             w, m = int(whole[b]), int(need[b])
             if w:
@@ -105,10 +112,20 @@ def test_groups_of_many_sizes(hq, hkv, d, N):
     c.check(c.run())
 
 
-@pytest.mark.parametrize("P", [15, 16, 63, 64, 65, 1023, 1024, 1025, 1040, 5000])
+@pytest.mark.parametrize("P", [15, 16, 63, 64, 65, 255, 256, 257, 272, 511, 1023, 1024, 1025, 1040, 5000])
 def test_prefixes_around_tiles_and_splits(P):
-    """Nothing behind the prefix but the tree (own 0), or a few keys."""
-    c = Case(P, [3, 4], [P, 2 * P + 1], [0, 0, 0, 1, 15, 16, 64], 5, 4, 2, 64, shuffle=False)
+    """Nothing behind the prefix but the tree (own 0), or a few keys; splits of 256 keys
+    and more (336 pairs of a sequence and a KV head)."""
+    c = Case(P, [3, 4] * 6, [P, 2 * P + 1] * 6, [0, 0, 0, 1, 15, 16, 64] * 6, 5, 16, 8, 64, shuffle=False)
+    c.check(c.run(), seqs=[*range(7), 20, 41])
+
+
+def test_small_batches_take_the_plain_way():
+    """Every item has a CU of its own: the result is srt_tree_attn's."""
+    c = Case(21, [2, 3], [400, 500], (0, 100), 5, 4, 1, 64)
+    c.bt = np.ascontiguousarray(c.bt[:, :40])
+    live = torch.arange(5, device="cuda") < i32(c.n)[:, None]
+    assert torch.equal(c.run()[live], c.plain()[live])
     c.check(c.run())
 
 
@@ -137,7 +154,7 @@ def test_many_groups_and_more_than_1024_sequences():
 def test_pages_larger_than_the_prefix_and_large_pages():
     c = Case(7, [4, 3], [200, 700], (0, 600), 6, 4, 2, 128, page=256)
     c.check(c.run())
-    c = Case(8, [4], [100], (0, 600), 6, 4, 2, 128, page=1024)  # no whole page: nothing is shared
+    c = Case(8, [40], [100], (0, 600), 6, 16, 8, 128, page=1024)  # no whole page: nothing is shared
     c.check(c.run())
 
 
@@ -185,7 +202,7 @@ def test_sizes_out_of_range_on_the_device_are_clamped():
     for x in c.cache:  # (pages that nobody has are read by the bad sequences)
         x.nan_to_num_(0.0)
     c.n[1], c.L[2] = 900, -7
-    c.bt[1, -1], c.bt[5, 15] = 1 << 30, -77
+    c.bt[1, 30:], c.bt[5, 15] = 1 << 30, -77
     c.prefix[0] = 0  # (sequence 2's context is empty)
     c.run(scratch=torch.full((srt.srt_tree_attn_shared_scratch_bytes(6, 5, 4, 2, 64, 16, c.bt.shape[1], 2),), 255,
                              dtype=torch.uint8, device="cuda"))
