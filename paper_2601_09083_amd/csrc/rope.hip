@@ -8,9 +8,11 @@
 //   y0 = x0 cos - x1 sin,   y1 = x1 cos + x0 sin.
 //
 // GPU design: one read and one write of every vector, bound by HBM.  A wave takes
-// a token (or a part of its heads where the batch is small): a lane keeps one
-// 16-byte piece of the pairs for all heads that it visits, so the 8 (halves) or 4
-// (neighbouring dims) angles of its pairs are worked out once.  Angles are formed
+// a token (or a part of its heads where the batch is small).  Its lanes work out an
+// angle each while the first heads' loads are under way, and hand them round through
+// LDS: a lane keeps one 16-byte piece of the pairs for all heads that it visits, and
+// the 8 (halves) or 4 (neighbouring dims) angles of it.  (Every lane working out its
+// own took a third of the time of 7000 tokens: 42 us a pass, 31 so.)  Angles are formed
 // in 64 bits and reduced to a part of a turn there -- in fp32 position 10^6 would
 // be off by 0.03 of a radian -- and their sine and cosine in fp32; products and
 // sums are fp32 and a result is rounded to bf16 once.
@@ -24,6 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / SRT_WAVE;
+constexpr int kMaxDims = 512;
 constexpr int kMaxSplit = 4;    // waves that share a token, at most
 constexpr int kBatch = 4;       // heads of a lane whose loads are under way together
 constexpr int kManyWaves = 4096;  // waves from which a token is one wave's
@@ -53,6 +56,7 @@ __device__ inline uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t,
 template <bool kNeighbours, bool kCache>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   constexpr int kPairs = kNeighbours ? 4 : 8;  // of a lane's piece
+  __shared__ float2 turns_of[kWaves][kMaxDims / 2];
   const int lane = threadIdx.x % SRT_WAVE;
   // (a launch has fewer than 2^32 threads)
   const uint32_t wave = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / SRT_WAVE);
@@ -81,14 +85,6 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   const int pieces = a.rot / (2 * kPairs);    // of a head
   const int abreast = SRT_WAVE / pieces;      // heads that a wave takes at a time
   const int c = lane % pieces, hs = lane / pieces;
-  float cs[kPairs], sn[kPairs];
-#pragma unroll
-  for (int e = 0; e < kPairs; ++e) {
-    const double turns = pos * static_cast<double>(a.inv_freq[kPairs * c + e]) * 0.15915494309189533577;  // 1 / (2 pi)
-    sincospif(2.f * static_cast<float>(turns - rint(turns)), &sn[e], &cs[e]);
-    sn[e] *= a.factor;
-    cs[e] *= a.factor;
-  }
   const int heads = a.Hq + a.Hkv;
   const uint16_t* q = a.q + token * a.ldq;
   const uint16_t* k = a.k + token * a.ldk;
@@ -96,8 +92,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   // A lane's 16 bytes are 8 first members of pairs and, half the rotated dims on,
   // their partners; or, of neighbouring dims, four whole pairs.
   const int at0 = 8 * c, at1 = kNeighbours ? 0 : at0 + a.rot / 2;
-  for (int h0 = part * abreast; h0 < heads; h0 += kBatch * abreast * a.split) {
-    u16x8 x0[kBatch], x1[kBatch];
+  u16x8 x0[kBatch], x1[kBatch];
+  auto load = [&](int h0) {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int h = h0 + j * abreast * a.split + hs;
@@ -106,6 +102,27 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
       x0[j] = *reinterpret_cast<const u16x8*>(src + at0);
       if (!kNeighbours) x1[j] = *reinterpret_cast<const u16x8*>(src + at1);
     }
+  };
+  load(part * abreast);
+  // The angles' sines and cosines: a lane works out every 64th, and takes its own.
+  // (The wave's part of LDS is its own: its writes come before its reads.)
+  float2* turn = turns_of[threadIdx.x / SRT_WAVE];
+  for (int m = lane; m < a.rot / 2; m += SRT_WAVE) {
+    const double turns = pos * static_cast<double>(a.inv_freq[m]) * 0.15915494309189533577;  // 1 / (2 pi)
+    float sine, cosine;
+    sincospif(2.f * static_cast<float>(turns - rint(turns)), &sine, &cosine);
+    turn[m] = make_float2(cosine * a.factor, sine * a.factor);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  float cs[kPairs], sn[kPairs];
+#pragma unroll
+  for (int e = 0; e < kPairs; ++e) {
+    const float2 t = turn[kPairs * c + e];
+    cs[e] = t.x;
+    sn[e] = t.y;
+  }
+  for (int h0 = part * abreast; h0 < heads; h0 += kBatch * abreast * a.split) {
+    if (h0 != part * abreast) load(h0);
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int h = h0 + j * abreast * a.split + hs;
@@ -163,7 +180,7 @@ int check_rope(const srt_rope* rope, int32_t B, int32_t T, int32_t Hq, int32_t H
   if (!rope || B < 0 || T < 1 || Hq < 1 || Hkv < 1 || d < 1 || rope->rot < 1 || rope->rot > d || rope->reserved != 0 ||
       (rope->interleaved & ~1) || !std::isfinite(rope->factor))
     return SRT_ERR_INVALID;
-  if (d > 512 || d % 8 || rope->rot % 16 || Hq > (1 << 16) || Hkv > (1 << 16)) return SRT_ERR_UNSUPPORTED;
+  if (d > kMaxDims || d % 8 || rope->rot % 16 || Hq > (1 << 16) || Hkv > (1 << 16)) return SRT_ERR_UNSUPPORTED;
   return SRT_OK;
 }
 
