@@ -725,13 +725,14 @@ def srt_accept_sample(logits, gumbel, sampling: Sampling, tree_tokens, tree_pare
             out = _walk_outputs(B, max_depth, dev)
     else:
         _check_walk_outputs(out, B, max_depth)
+    em = out.get("n_emitted")
     _check("srt_accept_sample", _on_device(
-        dev, lib().srt_accept_sample, B, N, V, max_depth, _arg(logits, f32, dev, "logits"),
-        _maybe(gumbel, f32, dev, "gumbel"), sampling._ref, rules._ref if rules is not None else None,
-        _arg(tree_tokens, i32, dev, "tree_tokens"), _arg(tree_parent, i32, dev, "tree_parent"),
-        _arg(n_nodes, i32, dev, "n_nodes"), _arg(out["n_accepted"], i32, dev, "n_accepted"),
-        _arg(out["out_tokens"], i32, dev, "out_tokens"), _arg(out["out_nodes"], i32, dev, "out_nodes"),
-        _maybe(out.get("n_emitted"), i32, dev, "n_emitted"), _stream_of(dev, stream)))
+        dev, lib().srt_accept_sample, B, N, V, max_depth, _at(logits, f32, dev, "logits"),
+        None if gumbel is None else _at(gumbel, f32, dev, "gumbel"), sampling._ref, rules._ref if rules is not None else None,
+        _at(tree_tokens, i32, dev, "tree_tokens"), _at(tree_parent, i32, dev, "tree_parent"),
+        _at(n_nodes, i32, dev, "n_nodes"), _at(out["n_accepted"], i32, dev, "n_accepted"),
+        _at(out["out_tokens"], i32, dev, "out_tokens"), _at(out["out_nodes"], i32, dev, "out_nodes"),
+        None if em is None else _at(em, i32, dev, "n_emitted"), _stream_of(dev, stream)))
     return out
 
 
@@ -754,32 +755,40 @@ class Rope:
         self._ref = ctypes.byref(self._args)
 
 
-def _rope_rows(x, B, T, H, d, dev, name):
+def _at(t, dtype, device, name):
+    """_arg for calls whose time is the binding's own: the device by its number."""
+    if t.dtype is not dtype or t.get_device() != device.index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _rope_rows(x, shape, dev, name):
     """Elements from one token to the next of rows [B,T,H,d]."""
-    if x.shape != (B, T, H, d) or x.dtype is not torch.bfloat16 or x.device != dev:
-        raise ValueError(f"{name} must be {[B, T, H, d]} of bfloat16 on {dev}")
-    ld = _lead(x.stride(), B, T, H, d)
+    if x.shape != shape or x.dtype is not torch.bfloat16 or x.get_device() != dev.index:
+        raise ValueError(f"{name} must be {list(shape)} of bfloat16 on {dev}")
+    ld = _lead(x.stride(), *shape)
     if ld < 0:
         raise ValueError(f"{name}: a token's heads must lie side by side, sequences T tokens apart")
     return ld
 
 
 def _rope_sizes(rope, q, k, counts, ctx_len, depth):
-    if q.dim() != 4 or k.dim() != 4 or q.shape[1] < 1:
+    if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q must be [B, T, Hq, d], k [B, T, Hkv, d]")
-    B, T, Hq, d = q.shape
-    if counts.numel() != B or ctx_len.numel() != B or (depth is not None and depth.shape != (B, T)):
-        raise ValueError("counts and ctx_len must be [B], depth [B, T]")
-    return B, T, Hq, k.shape[2], d, rope.device
+    shape = q.shape
+    B, T, _, d = shape
+    if T < 1 or counts.numel() != B or ctx_len.numel() != B or (depth is not None and depth.shape != (B, T)):
+        raise ValueError("T must be at least 1, counts and ctx_len [B], depth [B, T]")
+    return shape, (B, T, k.shape[2], d), rope.device
 
 
-def _rope_out(out, like, heads, dev, stream, name):
+def _rope_out(out, shape, dev, stream, name):
     """The packed output: the given one, or zeros (rows that no count covers are not written)."""
     if out is None:
         with _device(dev), _on(stream):
-            return torch.zeros(like.shape, dtype=torch.bfloat16, device=dev)
-    if out.shape != like.shape:
-        raise ValueError(f"{name} must be [B, T, {heads}, d]")
+            return torch.zeros(shape, dtype=torch.bfloat16, device=dev)
+    if out.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
     return out
 
 
@@ -789,22 +798,24 @@ def srt_rope_append(rope: Rope, q, k, v, counts, k_cache, v_cache, block_table, 
     positions ctx_len + depth (or ctx_len + i), writes the keys and the values v
     to slots ctx_len + i of the caches [P,Hkv,page,d] and returns the queries
     [B,T,Hq,d].  Rows from counts[b] on are left alone (zero in a new q_out)."""
-    B, T, Hq, Hkv, d, dev = _rope_sizes(rope, q, k, counts, ctx_len, depth)
-    ldq, ldk = _rope_rows(q, B, T, Hq, d, dev, "q"), _rope_rows(k, B, T, Hkv, d, dev, "k")
-    if _rope_rows(v, B, T, Hkv, d, dev, "v") != ldk:
+    sq, sk, dev = _rope_sizes(rope, q, k, counts, ctx_len, depth)
+    B, T, Hkv, d = sk
+    ldq, ldk = _rope_rows(q, sq, dev, "q"), _rope_rows(k, sk, dev, "k")
+    if _rope_rows(v, sk, dev, "v") != ldk:
         raise ValueError("k and v must have the same strides")
-    if k_cache.dim() != 4 or k_cache.shape[1] != Hkv or k_cache.shape[3] != d or v_cache.shape != k_cache.shape:
+    cache, table = k_cache.shape, block_table.shape
+    if len(cache) != 4 or cache[1] != Hkv or cache[3] != d or v_cache.shape != cache:
         raise ValueError("caches must be [P, Hkv, page, d]")
-    if block_table.dim() != 2 or block_table.shape[0] != B:
+    if len(table) != 2 or table[0] != B:
         raise ValueError("block_table must be [B, max_pages]")
-    q_out = _rope_out(q_out, q, Hq, dev, stream, "q_out")
+    q_out = _rope_out(q_out, sq, dev, stream, "q_out")
     bf16, i32 = torch.bfloat16, torch.int32
     _check("srt_rope_append", _on_device(
-        dev, lib().srt_rope_append, rope._ref, B, T, Hq, Hkv, d, k_cache.shape[2], block_table.shape[1], k_cache.shape[0],
-        q.data_ptr(), ldq, k.data_ptr(), v.data_ptr(), ldk, _maybe(depth, i32, dev, "depth"),
-        _arg(counts, i32, dev, "counts"), _arg(q_out, bf16, dev, "q_out"), _arg(k_cache, bf16, dev, "k_cache"),
-        _arg(v_cache, bf16, dev, "v_cache"), _arg(block_table, i32, dev, "block_table"),
-        _arg(ctx_len, i32, dev, "ctx_len"), _stream_of(dev, stream)))
+        dev, lib().srt_rope_append, rope._ref, B, T, sq[2], Hkv, d, cache[2], table[1], cache[0], q.data_ptr(), ldq,
+        k.data_ptr(), v.data_ptr(), ldk, None if depth is None else _at(depth, i32, dev, "depth"),
+        _at(counts, i32, dev, "counts"), _at(q_out, bf16, dev, "q_out"), _at(k_cache, bf16, dev, "k_cache"),
+        _at(v_cache, bf16, dev, "v_cache"), _at(block_table, i32, dev, "block_table"), _at(ctx_len, i32, dev, "ctx_len"),
+        _stream_of(dev, stream)))
     return q_out
 
 
@@ -812,15 +823,16 @@ def srt_rope_rows(rope: Rope, q, k, counts, ctx_len, depth=None, q_out=None, k_o
     """The turned queries [B,T,Hq,d] and keys [B,T,Hkv,d] as rows; k_out may have
     rows of its own leading size and may be k itself (as where k and v are parts of
     one projection, which the 8-bit cache's calls read)."""
-    B, T, Hq, Hkv, d, dev = _rope_sizes(rope, q, k, counts, ctx_len, depth)
-    ldq, ldk = _rope_rows(q, B, T, Hq, d, dev, "q"), _rope_rows(k, B, T, Hkv, d, dev, "k")
-    q_out, k_out = _rope_out(q_out, q, Hq, dev, stream, "q_out"), _rope_out(k_out, k, Hkv, dev, stream, "k_out")
-    ldo = _rope_rows(k_out, B, T, Hkv, d, dev, "k_out")
-    i32 = torch.int32
+    sq, sk, dev = _rope_sizes(rope, q, k, counts, ctx_len, depth)
+    B, T, Hkv, d = sk
+    ldq, ldk = _rope_rows(q, sq, dev, "q"), _rope_rows(k, sk, dev, "k")
+    q_out, k_out = _rope_out(q_out, sq, dev, stream, "q_out"), _rope_out(k_out, sk, dev, stream, "k_out")
+    ldo, i32 = _rope_rows(k_out, sk, dev, "k_out"), torch.int32
     _check("srt_rope_rows", _on_device(
-        dev, lib().srt_rope_rows, rope._ref, B, T, Hq, Hkv, d, q.data_ptr(), ldq, k.data_ptr(), ldk,
-        _maybe(depth, i32, dev, "depth"), _arg(counts, i32, dev, "counts"), _arg(ctx_len, i32, dev, "ctx_len"),
-        _arg(q_out, torch.bfloat16, dev, "q_out"), k_out.data_ptr(), ldo, _stream_of(dev, stream)))
+        dev, lib().srt_rope_rows, rope._ref, B, T, sq[2], Hkv, d, q.data_ptr(), ldq, k.data_ptr(), ldk,
+        None if depth is None else _at(depth, i32, dev, "depth"), _at(counts, i32, dev, "counts"),
+        _at(ctx_len, i32, dev, "ctx_len"), _at(q_out, torch.bfloat16, dev, "q_out"), k_out.data_ptr(), ldo,
+        _stream_of(dev, stream)))
     return q_out, k_out
 
 
@@ -856,10 +868,10 @@ def srt_tree_attn_shared(q, k_cache, v_cache, block_table, ctx_len, tree_parent,
                                       dtype=torch.uint8, device=dev)
     if scratch.device != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be a contiguous tensor on {dev}")
-    args = (B, N, Hq, Hkv, d, page, mp, P, n_groups, _arg(q, bf16, dev, "q"), _arg(k_cache, bf16, dev, "k_cache"),
-            _arg(v_cache, bf16, dev, "v_cache"), _arg(block_table, i32, dev, "block_table"), _arg(ctx_len, i32, dev, "ctx_len"),
-            _arg(tree_parent, i32, dev, "tree_parent"), _arg(n_nodes, i32, dev, "n_nodes"),
-            _arg(group_ids, i32, dev, "group_ids"), _arg(prefix_len, i32, dev, "prefix_len"), scale, _arg(out, bf16, dev, "out"))
+    args = (B, N, Hq, Hkv, d, page, mp, P, n_groups, _at(q, bf16, dev, "q"), _at(k_cache, bf16, dev, "k_cache"),
+            _at(v_cache, bf16, dev, "v_cache"), _at(block_table, i32, dev, "block_table"), _at(ctx_len, i32, dev, "ctx_len"),
+            _at(tree_parent, i32, dev, "tree_parent"), _at(n_nodes, i32, dev, "n_nodes"),
+            _at(group_ids, i32, dev, "group_ids"), _at(prefix_len, i32, dev, "prefix_len"), scale, _at(out, bf16, dev, "out"))
     call = lambda x: _on_device(dev, lib().srt_tree_attn_shared, *args, x.data_ptr(), x.numel() * x.element_size(),
                                 _stream_of(dev, stream))
     st = call(scratch)

@@ -20,7 +20,7 @@ def test_sizes_and_pointers():
     for kw in (dict(B=-1), dict(N=0), dict(N=257), dict(V=0), dict(Dmax=-1), dict(Dmax=64), dict(logits=None), dict(tok=None),
                dict(par=None), dict(n=None), dict(acc=None), dict(out=None), dict(nodes=None), dict(reserved=1)):
         assert walk(**kw) == bad, kw
-    assert walk(V=(1 << 21) + 1) == un and walk(B=1 << 24) == un and walk(B=1 << 22, V=9000) == un
+    assert walk(V=(1 << 21) + 1) == un and walk(B=1 << 24) == un and walk(B=1 << 23, V=9000) == un
     assert walk(B=0) == S.SRT_OK
     assert S.lib().srt_accept_sample(4, 8, 100, 4, P, P, None, None, P, P, P, P, P, P, P, None) == bad
 
