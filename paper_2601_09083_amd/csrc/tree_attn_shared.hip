@@ -43,13 +43,13 @@ __device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const uint16_t* base, int nby
 
 // kLoads 16-byte loads through one descriptor: lane byte offset voff plus
 // j * step for load j.
-template <int kLoads, int kStep>
+template <int kLoads, int kStep, int kAux>
 __device__ inline void buffer_load16(const uint16_t* base, int nbytes, int voff, uint4 (&r)[kLoads]) {
   const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(base, nbytes);
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
     typedef int i32x4 __attribute__((ext_vector_type(4)));
-    const i32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff + j * kStep, 0, 0);
+    const i32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff + j * kStep, 0, kAux);
     r[j] = __builtin_bit_cast(uint4, x);
   }
 }
@@ -88,6 +88,7 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
   }
   const int rows = si.n * a.G;
   if (rb * kRowsPerBlock >= rows) return;
+  const bool once = rows <= kRowsPerBlock;  // no other item reads these keys
   const int k_begin = k0 + s * chunk;
   if (k_begin >= si.total) return;
   const int k_end = min(k_begin + chunk, si.total);
@@ -187,7 +188,8 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
     const bool ok = pg >= 0 && pg < a.num_pages && p0 < k_end;
     const int nbytes = ok ? min(kSubRows, k_end - p0) * D * 2 : 0;
     const int64_t off = ok ? (static_cast<int64_t>(pg) * a.Hkv + g) * head_stride + (p0 & pmask) * D : 0;
-    buffer_load16<kLoadsPerWave, kRowsPerLoad * D * 2>(base + off, nbytes, gl_off, r);
+    if (once) buffer_load16<kLoadsPerWave, kRowsPerLoad * D * 2, 2>(base + off, nbytes, gl_off, r);
+    else buffer_load16<kLoadsPerWave, kRowsPerLoad * D * 2, 0>(base + off, nbytes, gl_off, r);
   };
   auto store_k = [&](uint8_t* Kb) {
 #pragma unroll
