@@ -34,6 +34,7 @@ constexpr int kDraws = 12;        // of a long list's choice, before the last ke
 constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kUnroll = 8;        // quartets of a thread in a batch
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
+constexpr int kStage = 2;         // batches after which a sum over a row is looked at
 constexpr int kMost = 512;        // threads
 constexpr int kSegBins = 512;     // of the segments' maxima, 1 / 8 of the score wide
 constexpr int kMassBits = 44;     // of a bin's word: mass in units of 2^-24 below, count above
@@ -52,6 +53,9 @@ struct SampleArgs : RulesArgs {
 };
 
 typedef unsigned long long u64;
+
+// The larger of two that are no NaN (fmaxf would quiet each operand first).
+__device__ __forceinline__ float larger_of(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
@@ -488,7 +492,7 @@ struct Walker {
         scores(b, t, z);
         float top = z[0];
 #pragma unroll
-        for (int q = 1; q < 4 * kUnroll; ++q) top = __builtin_fmaxf(top, z[q]);
+        for (int q = 1; q < 4 * kUnroll; ++q) top = larger_of(top, z[q]);
         add(top);
         if (kMass) {
           // (the difference first: a large score's product with log2(e) has lost what parts it from the maximum)
@@ -501,12 +505,12 @@ struct Walker {
         if (kDraw)
 #pragma unroll
           for (int q = 0; q < 4 * kUnroll; ++q) d.ascending(z[q], add_rounded(z[q], t.g[q / 4][q % 4]), token(b, q));
-        if (batch_segs == 1) seg = __builtin_fmaxf(seg, top);
+        if (batch_segs == 1) seg = larger_of(seg, top);
         else
 #pragma unroll
           for (int k = 0; k < kUnroll; ++k) {
-            const float four = __builtin_fmaxf(__builtin_fmaxf(z[4 * k], z[4 * k + 1]), __builtin_fmaxf(z[4 * k + 2], z[4 * k + 3]));
-            seg = __builtin_fmaxf(seg, four);
+            const float four = larger_of(larger_of(z[4 * k], z[4 * k + 1]), larger_of(z[4 * k + 2], z[4 * k + 3]));
+            seg = larger_of(seg, four);
             if ((k + 1) * batch_segs % kUnroll == 0) {
               s.seg[(b * batch_segs + k * batch_segs / kUnroll) * threads + tid] = seg;
               seg = -INFINITY;
@@ -778,42 +782,86 @@ struct Walker {
     return drawn(d);
   }
 
-  // How many tokens lie before a place in the order, and what they weigh (kAt: up to
-  // a place, which need not be a token's).
+  // Whether the tokens before a place in the order weigh less than `target` of the
+  // row's `all`.  The wave's batches are summed a few at a time; what the rest weighs
+  // is known with what has been read, and most places are decided by a part of the row
+  // (at a top-p of 0.9 by a third of it, on average).
+  __device__ __forceinline__ bool weighs_less(u64 place, double target, double all) {
+    const float edge = score_of(place);
+    const int last = key_token(place), n_b = batches();
+    double mass = 0.0, read = 0.0;
+    extras([&](float z, int j) {
+      if (!(z > -INFINITY)) return;
+      const double x = exp_of(z - M);
+      read += x;
+      if (pack_key(z, j) > place) mass += x;
+    });
+    Batch t;
+    if (first_of(0) < e4) load<false>(0, t);
+    for (int b = 0; b < n_b; ++b) {
+      Batch next;
+      if (b + 1 < n_b && first_of(b + 1) < e4) load<false>(b + 1, next);
+      __builtin_amdgcn_sched_barrier(0);
+      if (first_of(b) < e4) {
+        float z[4 * kUnroll], in = 0.f, out = 0.f;
+        scores(b, t, z);
+        bool equal = false;
+#pragma unroll
+        for (int q = 0; q < 4 * kUnroll; ++q) {
+          const float x = exp_of(z[q] - M);
+          in += z[q] > edge ? x : 0.f;
+          out += z[q] > edge ? 0.f : x;
+          equal |= z[q] == edge;
+        }
+        if (equal)  // ties with the token at the place, itself among them: seldom
+#pragma unroll
+          for (int q = 0; q < 4 * kUnroll; ++q)
+            if (z[q] == edge && token(b, q) < last) {
+              const float x = exp_of(z[q] - M);
+              mass += x;
+              read -= x;
+            }
+        mass += in;
+        read += static_cast<double>(in) + out;
+      }
+      t = next;
+      if ((b + 1) % kStage == 0 || b + 1 == n_b) {
+        const double before = all_sum(mass);
+        if (b + 1 == n_b) return before < target;
+        const double rest = all - all_sum(read);
+        if (before >= target) return false;
+        if (before + rest + 1e-5 * all < target) return true;  // (a margin for the sums' roundings)
+      }
+    }
+    return all_sum(mass) < target;  // (a row of extras alone)
+  }
+
+  // How many tokens lie up to a place in the order, and what they weigh.
   struct Above {
     double count, mass;
   };
-  template <bool kAt>
-  __device__ __forceinline__ Above above(u64 place, bool weigh) {
+  __device__ __forceinline__ Above above(u64 place, bool before, bool weigh) {
     const float least = score_of(place);
-    const int last = key_token(place);
     double mass = 0.0;
     int count = 0;  // of the wave
+    auto counts = [&](float z, int j) {
+      const u64 x = pack_key(z, j);
+      return z > -INFINITY && (x > place || (x == place && !before));
+    };
     batches_from<false>(least, [&](int b, const Batch& t, bool on) {
       float z[4 * kUnroll], part = 0.f;
       scores(b, t, z);
-      u64 equal = 0;
 #pragma unroll
       for (int q = 0; q < 4 * kUnroll; ++q) {
-        // (a token's place goes by the numbers; one that is searched for, by its bits)
-        const bool in = on && (kAt ? z[q] > -INFINITY && pack_key(z[q], token(b, q)) >= place : z[q] > least);
+        const bool in = on && counts(z[q], token(b, q));
         if (weigh) part += in ? exp_of(z[q] - M) : 0.f;
         count += __popcll(__ballot(in));
-        if (!kAt) equal |= __ballot(on && z[q] == least);
-      }
-      if (equal) {  // ties with the token at the place, itself among them: seldom
-#pragma unroll
-        for (int q = 0; q < 4 * kUnroll; ++q) {
-          const bool in = on && z[q] == least && token(b, q) < last;
-          if (weigh) part += in ? exp_of(z[q] - M) : 0.f;
-          count += __popcll(__ballot(in));
-        }
       }
       mass += part;
     });
     double c = 0.0;
     extras([&](float z, int j) {
-      if (!(z > -INFINITY) || !(kAt ? pack_key(z, j) >= place : pack_key(z, j) > place)) return;
+      if (!counts(z, j)) return;
       mass += exp_of(z - M);
       c += 1.0;
     });
@@ -825,7 +873,7 @@ struct Walker {
   __device__ __forceinline__ u64 last_place(double count, double mass) {
     u64 place = 0;
     for (int bit = 63; bit >= 0; --bit) {
-      const Above x = above<true>(place | 1ull << bit, mass < INFINITY);
+      const Above x = above(place | 1ull << bit, false, mass < INFINITY);
       if (x.count >= count || x.mass >= mass) place |= 1ull << bit;
     }
     return place;
@@ -841,7 +889,7 @@ struct Walker {
   // `best`, at `place`: the first draw, if it has been made.
   __device__ __forceinline__ u64 from_row(int k, float p, double mass, float least, u64 best, u64 place) {
     if (k == a.V && !(p < 1.f)) return candidate(0, least);
-    if (k < a.V && p < 1.f) mass = above<true>(last_place(k, INFINITY), true).mass;
+    if (k < a.V && p < 1.f) mass = above(last_place(k, INFINITY), false, true).mass;
     const double target = p < 1.f ? static_cast<double>(p) * mass : INFINITY;
     for (int draw = 0; draw < kDraws; ++draw) {
       if (draw > 0 || !best) {
@@ -850,8 +898,12 @@ struct Walker {
         place = s.found;
       }
       if (!(score_of(place) >= least)) continue;
-      const Above x = above<false>(place, p < 1.f);
-      if (x.count < k && (x.count == 0.0 || x.mass < target)) return best;
+      if (k == a.V) {
+        if (weighs_less(place, target, mass)) return best;  // (nothing lies before the first)
+      } else {
+        const Above x = above(place, true, p < 1.f);
+        if (x.count < k && (x.count == 0.0 || x.mass < target)) return best;
+      }
     }
     place = last_place(k, target);
     return candidate(place ? place - 1 : 0, least);
