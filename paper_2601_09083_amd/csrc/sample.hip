@@ -608,51 +608,93 @@ struct Walker {
   __device__ __forceinline__ double weight(float z) const { return exp(static_cast<double>(z) - static_cast<double>(M)); }
 
   // The choice from a list of up to 64 R tokens, by wave 0 in registers: R a lane,
-  // place 64 r + lane.  Exact: the tokens are sorted and their weights summed in order.
+  // place 64 r + lane.  Drawn from as a long list is (weighs_less); it is sorted, and
+  // its weights summed in order, where the mass of the first k is asked for and more
+  // than k are there, or no draw was kept.
   template <int R>
   __device__ __forceinline__ u64 from_short(int count, int k, double p, double row_mass, float least) {
     if (wave == 0) {
       u64 x[R], best = 0;
 #pragma unroll
       for (int r = 0; r < R; ++r) x[r] = SRT_WAVE * r + lane < count ? s.list[SRT_WAVE * r + lane] : 0ull;
-#pragma unroll
-      for (int run = 2; run <= SRT_WAVE * R; run *= 2) {
-#pragma unroll
-        for (int d = run / 2; d >= SRT_WAVE; d /= 2)  // pairs in one lane
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const int o = r ^ (d / SRT_WAVE);
-            if (o < r) continue;
-            const bool falls = ((SRT_WAVE * r) & run) == 0;
-            const u64 hi = max(x[r], x[o]), lo = min(x[r], x[o]);
-            x[r] = falls ? hi : lo;
-            x[o] = falls ? lo : hi;
-          }
-        for (int d = min(run / 2, SRT_WAVE / 2); d >= 1; d /= 2)
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const u64 y = shfl_xor_u64(x[r], d);
-            const bool larger = ((lane & d) == 0) == (((SRT_WAVE * r + lane) & run) == 0);
-            x[r] = (x[r] > y) == larger ? x[r] : y;
-          }
-      }
-      double before = 0.0, incl[R], wt[R];
-      if (p < 1.0)
+      bool done = false;
+      if (!(k < count && p < 1.0)) {
+        u64 key[R], place = 0;
+        double wt[R], all = 0.0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          wt[r] = x[r] && SRT_WAVE * r + lane < k ? weight(score_of(x[r])) : 0.0;
-          incl[r] = wave_scan(wt[r]) + before;
-          before = last_lane(incl[r]);
+          key[r] = 0;
+          if (x[r] && score_of(x[r]) >= least) take(key[r], score_of(x[r]), key_token(x[r]));
+          wt[r] = p < 1.0 && x[r] ? weight(score_of(x[r])) : 0.0;
+          all += wt[r];
         }
-      const double target = p * (k < a.V ? before : row_mass);
+        const double target = p < 1.0 ? p * (k < a.V ? last_lane(wave_scan(all)) : row_mass) : INFINITY;
+        for (int draw = 0; draw < kDraws && !done; ++draw) {
+          u64 mine = 0, at = 0;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int i = SRT_WAVE * r + lane;
-        const float z = score_of(x[r]);
-        const bool keep = x[r] && i < k && (i == 0 || ((p >= 1.0 || incl[r] - wt[r] < target) && z >= least));
-        if (keep) take(best, z, key_token(x[r]));
+          for (int r = 0; r < R; ++r)
+            if (key[r] > mine && x[r] > place) {
+              mine = key[r];
+              at = x[r];
+            }
+          best = wave_top(mine);
+          if (!best) break;
+          const int owner = __ffsll(static_cast<long long>(__ballot(mine == best))) - 1;
+          place = static_cast<u64>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at >> 32), owner))) << 32 |
+                  static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), owner));
+          int before = 0;
+          double mass = 0.0;
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const bool in = x[r] > place;
+            before += __popcll(__ballot(in));
+            mass += in ? wt[r] : 0.0;
+          }
+          done = before == 0 || (before < k && (p >= 1.0 || last_lane(wave_scan(mass)) < target));
+        }
+        done = done || !best;
       }
-      best = wave_top(best);
+      if (!done) {
+        best = 0;
+#pragma unroll
+        for (int run = 2; run <= SRT_WAVE * R; run *= 2) {
+#pragma unroll
+          for (int d = run / 2; d >= SRT_WAVE; d /= 2)  // pairs in one lane
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const int o = r ^ (d / SRT_WAVE);
+              if (o < r) continue;
+              const bool falls = ((SRT_WAVE * r) & run) == 0;
+              const u64 hi = max(x[r], x[o]), lo = min(x[r], x[o]);
+              x[r] = falls ? hi : lo;
+              x[o] = falls ? lo : hi;
+            }
+          for (int d = min(run / 2, SRT_WAVE / 2); d >= 1; d /= 2)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const u64 y = shfl_xor_u64(x[r], d);
+              const bool larger = ((lane & d) == 0) == (((SRT_WAVE * r + lane) & run) == 0);
+              x[r] = (x[r] > y) == larger ? x[r] : y;
+            }
+        }
+        double before = 0.0, incl[R], wt[R];
+        if (p < 1.0)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            wt[r] = x[r] && SRT_WAVE * r + lane < k ? weight(score_of(x[r])) : 0.0;
+            incl[r] = wave_scan(wt[r]) + before;
+            before = last_lane(incl[r]);
+          }
+        const double target = p * (k < a.V ? before : row_mass);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int i = SRT_WAVE * r + lane;
+          const float z = score_of(x[r]);
+          const bool keep = x[r] && i < k && (i == 0 || ((p >= 1.0 || incl[r] - wt[r] < target) && z >= least));
+          if (keep) take(best, z, key_token(x[r]));
+        }
+        best = wave_top(best);
+      }
       if (lane == 0) s.found = best;
     }
     __syncthreads();
