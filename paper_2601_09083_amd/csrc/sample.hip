@@ -32,7 +32,7 @@ namespace {
 constexpr int kList = 4096;       // candidates that are sorted in LDS
 constexpr int kDraws = 12;        // of a long list's choice, before the last kept token is searched for
 constexpr int kSegs = 16;         // segments of a thread, at most
-constexpr int kUnroll = 8;        // quartets of a thread in a batch
+constexpr int kUnroll = 4;        // quartets of a thread in a batch
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
 constexpr int kStage = 2;         // batches after which a sum over a row is looked at
 constexpr int kMost = 512;        // threads
@@ -326,25 +326,6 @@ struct Walker {
     return any;
   }
 
-  // f(score, token) for every entry of score `least` and more.
-  template <typename Fn>
-  __device__ __forceinline__ void visit(float least, Fn f) const {
-    const int n_b = batches();
-    for (int b = 0; b < n_b; ++b) {
-      if (!reaches(b, least)) continue;
-      Batch t;
-      float z[4 * kUnroll];
-      load<false>(b, t);
-      scores(b, t, z);
-#pragma unroll
-      for (int q = 0; q < 4 * kUnroll; ++q)
-        if (z[q] >= least && z[q] > -INFINITY) f(z[q], token(b, q));
-    }
-    extras([&](float z, int j) {
-      if (z >= least && z > -INFINITY) f(z, j);
-    });
-  }
-
   // Appends a token to the list where `in`; s.n counts all, also those that find no room.
   __device__ __forceinline__ void append(bool in, float z, int j) const {
     const u64 lanes = __ballot(in);
@@ -481,11 +462,13 @@ struct Walker {
     Batch t, next;
     load<kDraw>(0, t);
     const int n_b = batches();
+    Batch third;
     if (!kDraw && n_b > 1) load<kDraw>(1, next);
+    if (!kDraw && n_b > 2) load<kDraw>(2, third);
     for (int b = 0; b < n_b; ++b) {
       Batch later;  // (two batches ahead, or one where the noise's take as many registers)
       if (kDraw && b + 1 < n_b) load<kDraw>(b + 1, next);
-      if (!kDraw && b + 2 < n_b) load<kDraw>(b + 2, later);
+      if (!kDraw && b + 3 < n_b) load<kDraw>(b + 3, later);
       __builtin_amdgcn_sched_barrier(0);
       if (first_of(b) < e4) {
         float z[4 * kUnroll];
@@ -524,7 +507,10 @@ struct Walker {
         seg = -INFINITY;
       }
       t = next;
-      if (!kDraw) next = later;
+      if (!kDraw) {
+        next = third;
+        third = later;
+      }
     }
     extras([&](float z, int j) {
       add(z);
@@ -910,58 +896,77 @@ struct Walker {
     return {all_sum(c + (lane == 0 ? count : 0)), weigh ? all_sum(mass) : 0.0};
   }
 
-  // The last place at which the tokens from the top up to it are `count` or weigh
-  // `mass`, whichever comes first; 0 if neither does.
-  __device__ __forceinline__ u64 last_place(double count, double mass) {
-    u64 place = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const Above x = above(place | 1ull << bit, false, mass < INFINITY);
-      if (x.count >= count || x.mass >= mass) place |= 1ull << bit;
-    }
-    return place;
-  }
-
   // The choice among more tokens than the list holds, of which those below `least`
   // are not kept.  The best of a set that has the kept ones is the choice if it is
   // kept itself, for which what lies before it in the order is summed; if it is not,
   // the kept ones lie before it.  A draw from a set's distribution is one of the kept
   // ones' share of it, so a top-p of 0.9 takes 1.1 draws, and a kept set of a
   // millionth a dozen.  Noise that is none could be arranged to take one for every
-  // token; after kDraws the last kept place is found bit by bit.
-  // `best`, at `place`: the first draw, if it has been made.
+  // token; after kDraws the last kept place is found bit by bit, as is the place of the
+  // k-th token where the mass of the first k is asked for.
+  // `best`, at `place`: the first draw, if it has been made.  (One loop, so that each
+  // pass over the row stands in the code once: what a walk runs fits the instruction
+  // cache.)
   __device__ __forceinline__ u64 from_row(int k, float p, double mass, float least, u64 best, u64 place) {
-    if (k == a.V && !(p < 1.f)) return candidate(0, least);
-    if (k < a.V && p < 1.f) mass = above(last_place(k, INFINITY), false, true).mass;
-    const double target = p < 1.f ? static_cast<double>(p) * mass : INFINITY;
-    for (int draw = 0; draw < kDraws; ++draw) {
-      if (draw > 0 || !best) {
-        best = candidate(place, least);
-        if (!best) return 0;
-        place = s.found;
-      }
-      if (!(score_of(place) >= least)) continue;
-      if (k == a.V) {
-        if (weighs_less(place, target, mass)) return best;  // (nothing lies before the first)
+    const bool by_k = k < a.V, by_p = p < 1.f;
+    bool searching = by_k && by_p, summing = false, last = false;  // the k-th place; its mass; the last kept place is known
+    double target = by_p && !by_k ? static_cast<double>(p) * mass : INFINITY;
+    u64 found = 0;
+    for (int bit = 63, draw = 0;;) {
+      u64 at = place;
+      if (searching) {
+        at = found | 1ull << bit;
+      } else if (summing) {
+        at = found;
       } else {
-        const Above x = above(place, true, p < 1.f);
-        if (x.count < k && (x.count == 0.0 || x.mass < target)) return best;
+        if (!best || draw > 0) {
+          best = candidate(place, least);
+          if (!best) return 0;
+          place = at = s.found;
+        }
+        if (last || !(by_k || by_p)) return best;
+        if (!by_k) {
+          if (score_of(place) >= least && weighs_less(place, target, mass)) return best;  // (nothing lies before the first)
+          if (++draw < kDraws) continue;
+          searching = true;
+          continue;
+        }
+      }
+      const Above x = above(at, !searching && !summing, searching ? target < INFINITY : by_p);
+      if (searching) {
+        if (x.count >= k || x.mass >= target) found = at;
+        if (--bit >= 0) continue;
+        searching = false;
+        if (draw == 0) {  // the k-th place
+          summing = true;
+        } else {          // the last kept place: its best is the choice
+          last = true;
+          place = found ? found - 1 : 0;
+        }
+      } else if (summing) {
+        summing = false;
+        target = static_cast<double>(p) * x.mass;
+      } else {
+        if (score_of(place) >= least && x.count < k && (x.count == 0.0 || x.mass < target)) return best;
+        if (++draw == kDraws) {
+          searching = true;
+          bit = 63;
+          found = 0;
+        }
       }
     }
-    place = last_place(k, target);
-    return candidate(place ? place - 1 : 0, least);
   }
 };
 
 // The choice at the node that the row belongs to: packed (score with noise, token), 0 if none.
-template <bool kRules>
+template <bool kRules, bool kNoise>
 __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float mp) {
   Lds& s = x.s;
   const int V = x.a.V;
   if (!(p > 0.f) || !(mp <= 1.f)) k = 1, p = 1.f, mp = 0.f;  // (a NaN too)
   if (k <= 0 || k > V) k = V;
-  const bool by_k = k < V, by_p = p < 1.f, by_m = mp > 0.f;
-  if (!x.w.noise) return x.template plain<false>();
-  if (!(by_k || by_p || by_m)) return x.template plain<true>();
+  bool by_k = k < V, by_p = p < 1.f, by_m = mp > 0.f;
+  if (!kNoise || !(by_k || by_p || by_m)) return x.template plain<kNoise>();
   for (int i = x.tid; i < kSegBins; i += x.threads) s.segbin[i] = 0;
   if (x.tid == 0) s.n = s.m = 0;
   double mass = 0.0;
@@ -980,11 +985,8 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   x.long_row = false;
   const float M = x.M;
   if (M == -INFINITY) return 0;
-  if (M == INFINITY) {  // one of the infinite scores: the lowest token, which is always kept
-    u64 key = 0;
-    x.visit(M, [&](float z, int j) { key = max(key, pack_key(z, j)); });
-    return x.all_max(key);
-  }
+  // (infinite scores: the lowest token of them, which is always kept)
+  if (M == INFINITY) k = V, p = 1.f, by_k = by_p = by_m = false;
   // The scores below which nothing is kept.
   float by_min = -INFINITY;
   if (by_m) {  // the smallest float whose distance from M is no more than log(min_p)
@@ -993,7 +995,7 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
     if (static_cast<double>(by_min) - static_cast<double>(M) < edge) by_min = nextafterf(by_min, INFINITY);
   }
   // (with both, the mass of the first k is needed, to which what weighs e^-104 adds nothing)
-  float least = by_k && by_p ? M - 104.f : by_min;
+  float least = M == INFINITY ? M : by_k && by_p ? M - 104.f : by_min;
   if (by_p && !by_k) {
     // tokens below this weigh no more than 1 - p of the row together
     const double d = log(static_cast<double>(V) / ((1.0 - static_cast<double>(p)) * mass));
@@ -1001,13 +1003,13 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   }
   if (by_k || by_p)
     least = __builtin_fmaxf(least, x.least_kept(by_k ? k : 0x7fffffff, by_k ? INFINITY : static_cast<double>(p) * mass));
-  const int count = x.collect(least);
+  const int count = M == INFINITY ? kList + 1 : x.collect(least);
   if (count <= kList) return x.from_list(count, k, by_p ? static_cast<double>(p) : 1.0, mass, by_min);
   x.long_row = true;
   return x.from_row(k, p, mass, __builtin_fmaxf(least, by_min), draw, place);
 }
 
-template <bool kRules>
+template <bool kRules, bool kNoise>
 __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   __shared__ Lds s;
   __shared__ uint32_t skip[kRules ? kMaxRuled / 32 : 1];
@@ -1024,7 +1026,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
   Walker<kRules> walker = {a, s, skip, apart, apart_z, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
                            max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f, false};
-  static_assert(kUnroll == 8 && kSegs % 8 == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
+  static_assert(kSegs % kUnroll == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
   while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
   const float p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
@@ -1042,7 +1044,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
       if (k == 0 && walker.w.seen) walker.list_said();
       walker.mark_row();
     }
-    const u64 key = choose<kRules>(walker, top_k, p, mp);
+    const u64 key = choose<kRules, kNoise>(walker, top_k, p, mp);
     tok = key ? key_token(key) : -1;
     __syncthreads();  // (the staged tree, at the first step; LDS is the next row's from here on)
     int child = -1;
@@ -1109,9 +1111,11 @@ extern "C" int srt_accept_sample(int32_t B, int32_t N, int32_t V, int32_t Dmax, 
   hipStream_t s = as_stream(stream);
   if (rules) {
     take_rules(a, *rules);
-    sample_walk_kernel<true><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
+    if (gumbel) sample_walk_kernel<true, true><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
+    else sample_walk_kernel<true, false><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
   } else {
-    sample_walk_kernel<false><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
+    if (gumbel) sample_walk_kernel<false, true><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
+    else sample_walk_kernel<false, false><<<static_cast<unsigned>(B), threads, 0, s>>>(a);
   }
   return launch_status();
 }
