@@ -285,23 +285,9 @@ struct Walker {
     }
     mark_special(a, w, s.path, n, 0, a.V, skip, threads, at, bias);
     // One with a count word that is marked by now is forbidden, or scored as a special one.
-    for (int i0 = 0; i0 < n_said; i0 += kUnroll * threads) {
-      int t[kUnroll], word[kUnroll];
-      float l[kUnroll];
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) t[k] = apart[min(i0 + k * threads + tid, n_said - 1)];
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        l[k] = w.logits[t[k]];
-        word[k] = w.seen[t[k]];
-      }
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        const int i = i0 + k * threads + tid;
-        if (i >= n_said) continue;
-        const uint32_t bit = 1u << (t[k] & 31);
-        apart_z[i] = atomicOr(&skip[t[k] >> 5], bit) & bit ? -INFINITY : scored(l[k], word[k]);
-      }
+    for (int i = tid; i < n_said; i += threads) {
+      const uint32_t t = apart[i], bit = 1u << (t & 31);
+      apart_z[i] = atomicOr(&skip[t >> 5], bit) & bit ? -INFINITY : 0.f;
     }
     const int room = kApart - max(n_said, 0), first = max(n_said, 0);
     n_special = n + w.bias1 - w.bias0 <= room ? n + w.bias1 - w.bias0 : -1;
@@ -316,6 +302,29 @@ struct Walker {
       });
     }
     __syncthreads();
+  }
+
+  // The scores of the tokens with a count word, each by the thread that marked it and
+  // adds it to a pass.  After the stream: read before it, these few entries bring most
+  // of the row's lines out of HBM, one at a time.
+  __device__ __forceinline__ void score_said() {
+    if (!kRules) return;
+    for (int i0 = tid; i0 < n_said; i0 += kUnroll * threads) {
+      int t[kUnroll], word[kUnroll];
+      float l[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) t[k] = apart[min(i0 + k * threads, n_said - 1)];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        l[k] = w.logits[t[k]];
+        word[k] = w.seen[t[k]];
+      }
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int i = i0 + k * threads;
+        if (i < n_said && apart_z[i] == 0.f) apart_z[i] = scored(l[k], word[k]);
+      }
+    }
   }
 
   // Whether the thread has an entry of score `least` or more in a batch.
@@ -441,6 +450,7 @@ struct Walker {
       for (int q = 0; q < 4 * kUnroll; ++q) best.ascending(kNoise ? add_rounded(z[q], t.g[q / 4][q % 4]) : z[q], token(b, q));
       t = next;
     }
+    score_said();
     extras([&](float z, int j) {
       if (z > -INFINITY) take(key, z, j);
     });
@@ -512,6 +522,7 @@ struct Walker {
         third = later;
       }
     }
+    score_said();
     extras([&](float z, int j) {
       add(z);
       if (kMass && z > -INFINITY) sum += exp_of(z - m);
