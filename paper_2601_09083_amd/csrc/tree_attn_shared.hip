@@ -471,6 +471,10 @@ constexpr int kGroupsEach = 4;     // of a thread of the plan kernel
 // runs the steps that do not depend on the batch's size in a quarter of the time.
 constexpr int kSmallPlan = 512;
 constexpr int kFew = 16;           // items or nodes up to which a thread lists them by itself
+// Lanes that list the items and nodes of one group or sequence otherwise (64: 13.6 us
+// a plan for 128 trees of 1 to 64 nodes, 8.6 for 64 of 8 nodes with 129 splits of their
+// prompt; 32: 12.4 and 9.1; 16: 11.7 and 10.1).
+constexpr int kListLanes = 32;
 constexpr int kMaxSplits = 32;     // of all keys of a sequence, about: a row's partial results are joined one by one
 
 struct PlanArgs {
@@ -479,7 +483,7 @@ struct PlanArgs {
   int32_t n_groups, slots, least_chunk;  // (slots: workgroups that run at a time)
 };
 
-// What a thread lists, or leaves to a wave: a group's or a sequence's items.
+// What a thread lists, or leaves to kListLanes: a group's or a sequence's items.
 struct Listing {
   int id, nodes, keys, at0, at1, list;  // (a sequence's place in its group's list of nodes, or -1)
 };
@@ -516,8 +520,8 @@ constexpr float kPartTiles = 1e-4f;    // of a row's part (1 KB written and read
 
 // One workgroup: groups, keys per split, item classes (as tree_attn_plan_kernel),
 // then the lists.  A thread of a batch has at most one group or sequence of 1024 at a
-// time, and lists its items if they are few; a wave at a time lists the others.
-// (A wave for every sequence took 19 us for 256 of them, 12 so.)
+// time, and lists its items if they are few (with a wave for every sequence a plan for
+// 256 of them took 19 us, with 16 waves 12, and with four 10).
 template <int kPlanThreads>
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a, PlanArgs p) {
   constexpr int kPlanWaves = kPlanThreads / SRT_WAVE, kGroups = kGroupsEach * kPlanThreads;
@@ -750,15 +754,15 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a,
       }
     }
     __syncthreads();
-    for (int i = wv; i < n_left; i += kPlanWaves) {
+    for (int i = tid / kListLanes; i < n_left; i += kPlanThreads / kListLanes) {
       const Listing l = left[i];
       const int rbs = row_blocks(l.nodes), per = a.Hkv * rbs, full = l.keys >> cshift, splits = splits_of(l.keys);
-      for (int y = lane; y < splits * per; y += SRT_WAVE) {
+      for (int y = tid % kListLanes; y < splits * per; y += kListLanes) {
         const int s = y / per, r = y - s * per, g = r / rbs;
         write(s < full ? l.at0 + y : l.at1 + y - full * per, l.id, g, s, r - g * rbs);
       }
       if (l.list >= 0)
-        for (int y = lane; y < l.nodes; y += SRT_WAVE) a.node_of[l.list + y] = l.id << 8 | y;
+        for (int y = tid % kListLanes; y < l.nodes; y += kListLanes) a.node_of[l.list + y] = l.id << 8 | y;
     }
     __syncthreads();
   }
