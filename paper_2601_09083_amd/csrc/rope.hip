@@ -7,15 +7,18 @@
 // The pair (x0, x1) m of a head turns by the angle position * inv_freq[m]:
 //   y0 = x0 cos - x1 sin,   y1 = x1 cos + x0 sin.
 //
-// GPU design: one read and one write of every vector, bound by HBM.  A wave takes
-// a token (or a part of its heads where the batch is small).  Its lanes work out an
-// angle each while the first heads' loads are under way, and hand them round through
-// LDS: a lane keeps one 16-byte piece of the pairs for all heads that it visits, and
-// the 8 (halves) or 4 (neighbouring dims) angles of it.  (Every lane working out its
-// own took a third of the time of 7000 tokens: 42 us a pass, 31 so.)  Angles are formed
-// in 64 bits and reduced to a part of a turn there -- in fp32 position 10^6 would
-// be off by 0.03 of a radian -- and their sine and cosine in fp32; products and
-// sums are fp32 and a result is rounded to bf16 once.
+// GPU design: one read and one write of every vector, bound by HBM (16 prompts of up to
+// 4096 tokens, 32 + 8 heads: 206 us a pass, 1.04 GB at 5.1 TB/s, the rate of a copy;
+// 256 trees of up to 64 nodes, 28 + 4 heads: 38.6 us, 132 MB at 3.4 TB/s).  A wave
+// takes a token.  Its lanes work out an angle each while the first heads' loads are
+// under way, and hand them round through LDS: a lane keeps one 16-byte piece of the
+// pairs for all heads that it visits, and the 8 (halves) or 4 (neighbouring dims)
+// angles of it.  (Every lane working out its own: 42 us for those trees.  Two or four
+// waves to a token work its angles out as often: the trees 43 and 52 us, prompts of
+// 12 + 2 heads 73 against 94 and 143, and of one token per sequence no less than one.)
+// Angles are formed in 64 bits and reduced to a part of a turn there -- in fp32
+// position 10^6 would be off by 0.03 of a radian -- and their sine and cosine in fp32;
+// products and sums are fp32 and a result is rounded to bf16 once.
 #include <cmath>
 
 #include "common.h"
@@ -27,9 +30,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / SRT_WAVE;
 constexpr int kMaxDims = 512;
-constexpr int kMaxSplit = 4;    // waves that share a token, at most
 constexpr int kBatch = 4;       // heads of a lane whose loads are under way together
-constexpr int kManyWaves = 4096;  // waves from which a token is one wave's
 
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
@@ -46,7 +47,7 @@ struct RopeArgs {
   const int32_t* ctx_len;
   const int32_t* bt;
   int64_t ldq, ldk, ldo, num_pages;
-  int32_t B, T, Hq, Hkv, d, rot, page, max_pages, split;
+  int32_t B, T, Hq, Hkv, d, rot, page, max_pages;
   float factor;
 };
 
@@ -60,12 +61,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   const int lane = threadIdx.x % SRT_WAVE;
   // (a launch has fewer than 2^32 threads)
   const uint32_t wave = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / SRT_WAVE);
-  const uint32_t token32 = wave / static_cast<uint32_t>(a.split);
-  const int part = static_cast<int>(wave - token32 * a.split);
-  const int b = static_cast<int>(token32 / static_cast<uint32_t>(a.T));
+  const int b = static_cast<int>(wave / static_cast<uint32_t>(a.T));
   if (b >= a.B) return;
-  const int i = static_cast<int>(token32 - static_cast<uint32_t>(b) * a.T);
-  const int64_t token = token32;
+  const int i = static_cast<int>(wave - static_cast<uint32_t>(b) * a.T);
+  const int64_t token = wave;
   if (i >= a.counts[b]) return;
   const int64_t L = a.ctx_len[b];
   const double pos = static_cast<double>(L + (a.depth ? a.depth[token] : i));
@@ -96,14 +95,14 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   auto load = [&](int h0) {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      const int h = h0 + j * abreast * a.split + hs;
+      const int h = h0 + j * abreast + hs;
       if (hs >= abreast || h >= heads) continue;
       const uint16_t* src = h < a.Hq ? q + h * a.d : k + (h - a.Hq) * a.d;
       x0[j] = *reinterpret_cast<const u16x8*>(src + at0);
       if (!kNeighbours) x1[j] = *reinterpret_cast<const u16x8*>(src + at1);
     }
   };
-  load(part * abreast);
+  load(0);
   // The angles' sines and cosines: a lane works out every 64th, and takes its own.
   // (The wave's part of LDS is its own: its writes come before its reads.)
   float2* turn = turns_of[threadIdx.x / SRT_WAVE];
@@ -121,11 +120,11 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     cs[e] = t.x;
     sn[e] = t.y;
   }
-  for (int h0 = part * abreast; h0 < heads; h0 += kBatch * abreast * a.split) {
-    if (h0 != part * abreast) load(h0);
+  for (int h0 = 0; h0 < heads; h0 += kBatch * abreast) {
+    if (h0 > 0) load(h0);
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      const int h = h0 + j * abreast * a.split + hs;
+      const int h = h0 + j * abreast + hs;
       if (hs >= abreast || h >= heads) continue;
       u16x8 y0, y1;
 #pragma unroll
@@ -149,9 +148,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   }
 
   // Dims that do not turn, and the values.
-  const int first = part * SRT_WAVE + lane, step = a.split * SRT_WAVE;
   const int rest = (a.d - a.rot) / 8;
-  for (int x = first; x < heads * rest; x += step) {
+  for (int x = lane; x < heads * rest; x += SRT_WAVE) {
     const int h = x / rest, at = a.rot + 8 * (x - h * rest);
     if (h >= a.Hq && !stored) continue;
     const uint16_t* src = h < a.Hq ? q + h * a.d : k + (h - a.Hq) * a.d;
@@ -161,7 +159,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   if constexpr (kCache) {
     const int per = a.d / 8;
     if (!stored) return;
-    for (int x = first; x < a.Hkv * per; x += step) {
+    for (int x = lane; x < a.Hkv * per; x += SRT_WAVE) {
       const int h = x / per;
       *reinterpret_cast<u16x8*>(a.v_out + k_at + h * k_step + 8 * (x - h * per)) =
           *reinterpret_cast<const u16x8*>(a.v + token * a.ldk + 8 * x);
@@ -189,8 +187,7 @@ int launch(RopeArgs& a, const srt_rope& rope, bool cache, void* stream) {
   a.rot = rope.rot;
   a.factor = rope.factor;
   const int64_t tokens = static_cast<int64_t>(a.B) * a.T;
-  a.split = tokens <= kManyWaves / kMaxSplit ? kMaxSplit : 1;
-  const int64_t grid = (tokens * a.split + kWaves - 1) / kWaves;
+  const int64_t grid = (tokens + kWaves - 1) / kWaves;
   if (!launchable(grid, kThreads)) return SRT_ERR_UNSUPPORTED;
   hipStream_t s = as_stream(stream);
   const unsigned n = static_cast<unsigned>(grid);
@@ -221,7 +218,7 @@ extern "C" int srt_rope_append(const srt_rope* rope, int32_t B, int32_t T, int32
     return SRT_ERR_INVALID;
   RopeArgs a = {q,      k,   v,    q_out, k_cache, v_cache,   nullptr, depth, counts, ctx_len, block_table,
                 ldq,    ldkv, 0,   num_pages, B,   T,         Hq,      Hkv,   d,      0,       page,
-                max_pages, 1, 0.f};
+                max_pages, 0.f};
   return launch(a, *rope, true, stream);
 }
 
@@ -237,6 +234,6 @@ extern "C" int srt_rope_rows(const srt_rope* rope, int32_t B, int32_t T, int32_t
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return SRT_ERR_INVALID;
   RopeArgs a = {q,   k,    nullptr, q_out, k_out, nullptr, nullptr, depth, counts, ctx_len, nullptr,
                 ldq, ldk,  ldo,     0,     B,     T,       Hq,      Hkv,   d,      0,       1,
-                1,   1,    0.f};
+                1,   0.f};
   return launch(a, *rope, false, stream);
 }
