@@ -12,19 +12,24 @@
 // whatever order the sums are taken in -- only the place of the top-p cut depends
 // on sums, and those are held in 64 bits.
 //
-// GPU design.  One workgroup walks one sequence; what bounds it is reading the
-// visited rows (608 KB of a 152k vocabulary).  A row is read from HBM once: its
-// maximum, its sum of exp(z - max), and the maximum of every thread's every few
-// entries (a segment) are taken in one pass.  A count and a lower bound of the mass
-// over the segments' maxima give a score below which nothing can be kept; segments
-// that reach it are read again, which a row that is sure of its tokens has few of,
-// and their entries from that score up are sorted in LDS, most often a hundred.
-// There the cuts are prefix sums, and noise is read at the kept tokens alone.
-// Rows with more candidates than the list holds are narrowed down by histograms
-// over ever smaller ranges of the score (counts, and masses in fixed point, so
-// that the order of the atomics does not matter) to the one list that the last
-// kept token is in.  Sequences that cut nothing, or without noise, take the plain
-// arg-max in one pass.
+// GPU design.  One workgroup walks one sequence, and its levels follow one another, so
+// what bounds a batch is one CU's time for a row times the longest walk's levels: of a
+// 152k vocabulary (608 KB) 15 us a row for the arg-max alone, 16 with min-p, 18 to 20
+// with a top-k, 24 with a top-p, 27 with a top-k of 200 and a top-p; 256 sequences of up
+// to 12 levels 410 us.  Of the 15 us the vector unit is busy for 10 to 12.  A row is read
+// from HBM once: its maximum, its sum of exp(z - max), and the maximum of every thread's
+// every few entries (a segment) are taken in one pass.  A count and a lower bound of the
+// mass over the segments' maxima give a score below which nothing can be kept; segments
+// that reach it are read again, which a row that is sure of its tokens has few of, and
+// their entries from that score up are listed in LDS, most often a hundred.
+//
+// The choice from a list or from the row is drawn: the best of all of them is the
+// choice if it is kept itself, which takes the mass before it in the order, a sum
+// without a sort; if it is not, the kept ones lie before it, and the best of those is
+// next.  A list is sorted only where the mass of its first top_k is asked for.  Noise is
+// read at the listed tokens alone, or once a draw.  (Long lists narrowed down by
+// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass, drawn from 147.)
+// Sequences that cut nothing, or without noise, take the plain arg-max in one pass.
 #include "rules.h"
 
 namespace {
@@ -34,7 +39,9 @@ constexpr int kDraws = 12;        // of a long list's choice, before the last ke
 constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
-constexpr int kStage = 2;         // batches after which a sum over a row is looked at
+// Batches after which a sum over a row is looked at (64 flat rows of 152k with a top-p of
+// 0.999, 0.9, 0.5: 77, 146, 280 us; 2: 76, 149, 290; at the row's end alone 91, 150, 275).
+constexpr int kStage = 4;
 constexpr int kMost = 512;        // threads
 constexpr int kSegBins = 512;     // of the segments' maxima, 1 / 8 of the score wide
 constexpr int kMassBits = 44;     // of a bin's word: mass in units of 2^-24 below, count above
@@ -42,7 +49,9 @@ constexpr int64_t kMaxVocab = int64_t(1) << 21;
 constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LDS
 constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
 constexpr int kApart = kSaid + 512;  // and with them those of the path and of the bias list
-constexpr int kShortVocab = 4096;  // rows up to which 256 threads walk
+// Rows up to which 256 threads walk (4 walks of 1024 entries: 38 us a pass, 40 with 512
+// threads; 256 of 152k: 608 us, 410 with 512).
+constexpr int kShortVocab = 4096;
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct SampleArgs : RulesArgs {
@@ -235,8 +244,9 @@ struct Walker {
   }
 
   // Lists the tokens with a count word.  A penalty costs a division, which one such
-  // token in a wave's 64 entries makes it take for all: of a row with one in 50 most
-  // of the time went there (64 sequences, 9 levels: 617 us, and 516 with the list).
+  // token in a wave's 64 entries makes it take for all, and the words are half as much
+  // to read as the logits: with them in the stream 64 walks of a 152k vocabulary, one
+  // token in 50 said, take 726 us, and 418 so.
   __device__ __forceinline__ void list_said() {
     if (tid == 0) s.n = 0;
     __syncthreads();
@@ -350,8 +360,8 @@ struct Walker {
   // The tokens of score `least` and more as the list, and how many there are (more
   // than kList: at least that many).  The segments that reach it are listed first and
   // their quartets dealt out to all threads: where a thread reads its own ones again,
-  // nearly every wave has one in each batch, and waits for each in turn (15 us of a
-  // 152k row's 27).  s.n and s.m have been cleared.
+  // nearly every wave has one in each batch, and waits for each in turn (of a 152k row's
+  // 27 us that took 15).  s.n and s.m have been cleared.
   __device__ __forceinline__ int collect(float least) {
     const int per = kUnroll * seg_batches / batch_segs;  // quartets of a segment
     const int segs = (batches() + seg_batches - 1) / seg_batches * batch_segs;
@@ -880,7 +890,8 @@ struct Walker {
     double count, mass;
   };
   __device__ __forceinline__ Above above(u64 place, bool before, bool weigh) {
-    const float least = score_of(place);
+    float least = score_of(place);
+    if (!(least == least)) least = -INFINITY;  // (behind every score)
     double mass = 0.0;
     int count = 0;  // of the wave
     auto counts = [&](float z, int j) {
@@ -907,8 +918,8 @@ struct Walker {
     return {all_sum(c + (lane == 0 ? count : 0)), weigh ? all_sum(mass) : 0.0};
   }
 
-  // The choice among more tokens than the list holds, of which those below `least`
-  // are not kept.  The best of a set that has the kept ones is the choice if it is
+  // The choice among more tokens than the list holds, of which those below `lowest` and
+  // `by_min` are not kept.  The best of a set that has the kept ones is the choice if it is
   // kept itself, for which what lies before it in the order is summed; if it is not,
   // the kept ones lie before it.  A draw from a set's distribution is one of the kept
   // ones' share of it, so a top-p of 0.9 takes 1.1 draws, and a kept set of a
@@ -918,12 +929,18 @@ struct Walker {
   // `best`, at `place`: the first draw, if it has been made.  (One loop, so that each
   // pass over the row stands in the code once: what a walk runs fits the instruction
   // cache.)
-  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float least, u64 best, u64 place) {
+  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float lowest, float by_min, u64 best, u64 place) {
+    const float least = __builtin_fmaxf(lowest, by_min);
     const bool by_k = k < a.V, by_p = p < 1.f;
     bool searching = by_k && by_p, summing = false, last = false;  // the k-th place; its mass; the last kept place is known
     double target = by_p && !by_k ? static_cast<double>(p) * mass : INFINITY;
-    u64 found = 0;
-    for (int bit = 63, draw = 0;;) {
+    // The places searched for lie between the row's first and that of `lowest`, whose
+    // common bits they share.
+    const u64 first = pack_key(M, 0), ends = first ^ pack_key(lowest, a.V - 1);
+    const int top_bit = 63 - __clzll(static_cast<long long>(ends | 1));
+    const u64 common = first & ~((2ull << top_bit) - 1);
+    u64 found = common;
+    for (int bit = top_bit, draw = 0;;) {
       u64 at = place;
       if (searching) {
         at = found | 1ull << bit;
@@ -946,13 +963,14 @@ struct Walker {
       const Above x = above(at, !searching && !summing, searching ? target < INFINITY : by_p);
       if (searching) {
         if (x.count >= k || x.mass >= target) found = at;
+        if (x.count == k && draw == 0) bit = 0;  // (the first k tokens: only their mass is asked for)
         if (--bit >= 0) continue;
         searching = false;
         if (draw == 0) {  // the k-th place
           summing = true;
         } else {          // the last kept place: its best is the choice
           last = true;
-          place = found ? found - 1 : 0;
+          place = max(found, 1ull) - 1;
         }
       } else if (summing) {
         summing = false;
@@ -961,8 +979,8 @@ struct Walker {
         if (score_of(place) >= least && x.count < k && (x.count == 0.0 || x.mass < target)) return best;
         if (++draw == kDraws) {
           searching = true;
-          bit = 63;
-          found = 0;
+          bit = top_bit;
+          found = common;
         }
       }
     }
@@ -1017,7 +1035,7 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   const int count = M == INFINITY ? kList + 1 : x.collect(least);
   if (count <= kList) return x.from_list(count, k, by_p ? static_cast<double>(p) : 1.0, mass, by_min);
   x.long_row = true;
-  return x.from_row(k, p, mass, __builtin_fmaxf(least, by_min), draw, place);
+  return x.from_row(k, p, mass, least, by_min, draw, place);
 }
 
 template <bool kRules, bool kNoise>

@@ -224,6 +224,25 @@ def test_masks_that_leave_little_or_nothing():
         assert got["n_emitted"][0].item() == 0 and got["out_tokens"][2, 0].item() == V - 1
 
 
+@pytest.mark.parametrize("shift", [0.0, -1.0, -60.0, 1e5])
+def test_the_mass_of_the_first_of_many(shift):
+    """More than a list's tokens under a top-k and a top-p: the k-th place is searched for."""
+    c = Case(14, 6, 3, 60001, 2, a=(0.4, 1.0), cuts=[(6000, 0.9, 0.0), (20000, 0.5, 0.0), (59000, 0.99, 0.3), (30000, 0.999, 0.9)])
+    c.logits += np.float32(shift)
+    c.check(c.run())
+
+
+def test_fewer_tokens_than_the_first_k():
+    c = Case(15, 6, 3, 60001, 2, a=(0.4, 1.0), cuts=[(50000, 0.9, 0.0), (60000, 0.5, 0.0), (59000, 0.99, 0.3)])
+    rng = np.random.default_rng(16)
+    gone = rng.random(c.logits.shape) < np.array([0.5, 0.9, 0.3])[None, :, None]
+    for b in range(c.B):
+        for i in range(1, int(c.n[b])):
+            gone[b, c.par[b, i], c.tok[b, i]] = False
+    c.logits[gone] = -np.inf
+    c.check(c.run())
+
+
 def test_the_same_again_and_many_sequences():
     """Sums and lists do not depend on the order of atomics."""
     c = Case(10, 300, 4, 6000, 3, a=(0.4, 1.4))
