@@ -10,8 +10,13 @@
 // GPU design.  The tile kernel is that of tree_attn.hip, whose comments describe it;
 // its items are of two kinds: the rows of one sequence against a split of its own
 // keys, and the rows of a whole group, 256 at a time, against a split of the prefix,
-// where no key is masked.  Read by
-// every sequence, the prefixes of a batch of single tokens are most of its bytes.
+// where no key is masked.  Single tokens are bound by the bytes of the keys that are
+// left to read: 32 prompts of 2k to 8k, eight answers each, 28 + 4 heads of 128 take
+// 177 us a pass, 822 MB at 4.6 TB/s (5.0 in the tile kernel's 163 us), where
+// srt_tree_attn reads every prefix eight times and takes 314.  Trees are bound by the
+// tile kernel's rate: 64 trees of 8 nodes over one prompt of 32k 158 us, 126 GFLOP at
+// 0.8 PFLOP/s (srt_tree_attn, whose 256-row tiles are a quarter full, 608); 128 of 1 to
+// 64 nodes, 12 + 2 heads, 129 us (153), 28 of them the plan and the parts' join.
 // A plan kernel (one workgroup) finds the groups' members, the keys that they can
 // share -- whole pages, no further than the shortest member's context -- and the
 // items, longest first; the combine kernel of attn.h joins the parts.
@@ -88,7 +93,9 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
   }
   const int rows = si.n * a.G;
   if (rb * kRowsPerBlock >= rows) return;
-  const bool once = rows <= kRowsPerBlock;  // no other item reads these keys
+  // No other item reads these keys: they are loaded past the caches (single tokens as
+  // above 187 us without, 177 so; where trees read most keys often no difference).
+  const bool once = rows <= kRowsPerBlock;
   const int k_begin = k0 + s * chunk;
   if (k_begin >= si.total) return;
   const int k_end = min(k_begin + chunk, si.total);
@@ -468,7 +475,8 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
 constexpr int kMaxGroups = 4096;   // groups of a batch, whose counts are held in LDS
 constexpr int kGroupsEach = 4;     // of a thread of the plan kernel
 // Sequences and groups up to which the plan kernel has 256 threads: a wave to a SIMD
-// runs the steps that do not depend on the batch's size in a quarter of the time.
+// runs the steps that do not depend on the batch's size in a quarter of the time (256
+// single tokens 177 us a call, 180 with 1024 threads; 128 trees 129 and 131).
 constexpr int kSmallPlan = 512;
 constexpr int kFew = 16;           // items or nodes up to which a thread lists them by itself
 // Lanes that list the items and nodes of one group or sequence otherwise (64: 13.6 us
@@ -516,10 +524,10 @@ struct Load {
   }
 };
 constexpr float kItemTiles = 2.f;      // of an item's start and end
-constexpr float kPartTiles = 1e-4f;    // of a row's part (1 KB written and read, by all CUs), times CUs
+constexpr float kPartTiles = 1e-4f;    // of a row's part: 1 KB written and read at 5 TB/s, tiles being 2 us
 
 // One workgroup: groups, keys per split, item classes (as tree_attn_plan_kernel),
-// then the lists.  A thread of a batch has at most one group or sequence of 1024 at a
+// then the lists.  A thread of a batch has at most one group or sequence at a
 // time, and lists its items if they are few (with a wave for every sequence a plan for
 // 256 of them took 19 us, with 16 waves 12, and with four 10).
 template <int kPlanThreads>
@@ -701,7 +709,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a,
     a.plan[kPlanChunk] = chunk;
   }
   __syncthreads();
-  // The lists, 1024 groups and then 1024 sequences at a time.
+  // The lists, a thread to a group and then to a sequence at a time.
   int wide = 0;
   const int group_steps = (p.n_groups + kPlanThreads - 1) / kPlanThreads;
   const int seq_steps = (a.B + kPlanThreads - 1) / kPlanThreads;
