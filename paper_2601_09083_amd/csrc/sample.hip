@@ -38,6 +38,8 @@ constexpr int kList = 4096;       // candidates that are sorted in LDS
 constexpr int kDraws = 12;        // of a long list's choice, before the last kept token is searched for
 constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
+constexpr int kAhead = 3;         // batches whose registers are loaded or used
+constexpr int kAheadNoise = 2;    // the same with the noise's
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
 // Batches after which a sum over a row is looked at (64 flat rows of 152k with a top-p of
 // 0.999, 0.9, 0.5: 77, 146, 280 us; 2: 76, 149, 290; at the row's end alone 91, 150, 275).
@@ -49,6 +51,7 @@ constexpr int64_t kMaxVocab = int64_t(1) << 21;
 constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LDS
 constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
 constexpr int kApart = kSaid + 512;  // and with them those of the path and of the bias list
+constexpr int kStaged = 512;      // entries of a bias list that are held in LDS
 // Rows up to which 256 threads walk (4 walks of 1024 entries: 38 us a pass, 40 with 512
 // threads; 256 of 152k: 608 us, 410 with 512).
 constexpr int kShortVocab = 4096;
@@ -115,6 +118,19 @@ __device__ __forceinline__ float score_of(u64 key) {
   return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
+// Loads past the buffer's bytes read 0.  (`base` is the same for all lanes.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const float* base, int bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(at));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ f32x4 load_quartet(__amdgpu_buffer_rsrc_t row, uint32_t at) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const i32x4 x = __builtin_amdgcn_raw_buffer_load_b128(row, at, 0, 0);
+  return __builtin_bit_cast(f32x4, x);
+}
+
 // What the workgroup shares.
 struct Lds {
   u64 list[kList];  // packed candidates (score, token)
@@ -140,6 +156,7 @@ struct Walker {
   uint32_t* skip;
   int32_t* apart;
   float* apart_z;
+  uint16_t* said_word;
   int n_said, n_special;
   Row w;
   int n;                 // tokens emitted on this walk
@@ -168,9 +185,12 @@ struct Walker {
   };
 
   // Score of a logit under the rules; a NaN counts as -inf.
-  __device__ __forceinline__ float scored(float l, int word) const {
+  __device__ __forceinline__ float scored_raw(float l, int word) const {  // (may be a NaN, but a quiet one)
     if (kRules && word) l = penalised(w, l, word & kPrompt, word & kCount);
-    return __builtin_fmaxf(mul_rounded(l, w.invT), -INFINITY);
+    return mul_rounded(l, w.invT);
+  }
+  __device__ __forceinline__ float scored(float l, int word) const {
+    return __builtin_fmaxf(scored_raw(l, word), -INFINITY);
   }
   __device__ __forceinline__ bool streams_words() const { return w.seen && n_said < 0; }
   __device__ __forceinline__ bool marked(int j) const { return kRules && ((skip[j >> 5] >> (j & 31)) & 1u); }
@@ -182,24 +202,47 @@ struct Walker {
   __device__ __forceinline__ int first_of(int b) const { return b * kUnroll * threads + tid; }
   __device__ __forceinline__ int batches() const { return full + (full * kUnroll * threads < e4); }
 
-  // The batch's loads.  Quartets behind the row's end read the thread's first one's line.
-  template <bool kNoise>
-  __device__ __forceinline__ void load(int b, Batch& t) const {
-    const f32x4u* r4 = reinterpret_cast<const f32x4u*>(w.logits);
-    const f32x4u* g4 = reinterpret_cast<const f32x4u*>(w.noise);
-    const int i = first_of(b);
-    if (i >= e4) return;
+  // Calls f(batch number, batch, on(batch number)) for the row's batches in turn until it
+  // returns true, the loads of the next kAhead - 1 under way: each in registers of its
+  // own, the loop unrolled over them (to move a batch from one to the next would wait for
+  // its loads).  Only threads with on() load.  Quartets behind the row's end read as 0.
+  template <bool kNoise, int kAhead, typename On, typename Fn>
+  __device__ __forceinline__ void stream(On on, Fn f) const {
+    const int n_b = __builtin_amdgcn_readfirstlane(batches()), bytes = 16 * e4;
+    const uint32_t step = 16 * threads;
+    const __amdgpu_buffer_rsrc_t row = buffer_of(w.logits, bytes);
+    const __amdgpu_buffer_rsrc_t noise = buffer_of(kNoise ? w.noise : w.logits, bytes);
+    Batch t[kAhead];
+    bool mine[kAhead];
+    auto load = [&](int b, int r) {
+      mine[r] = b < n_b && on(b);
+      const uint32_t at = mine[r] ? 16 * tid + b * kUnroll * step : 1u << 30;
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      const int at = i + k * threads < e4 ? i + k * threads : i;
-      t.x[k] = r4[at];
-      if (kNoise) t.g[k] = g4[at];
+      for (int k = 0; k < kUnroll; ++k) {
+        t[r].x[k] = load_quartet(row, at + k * step);
+        if (kNoise) t[r].g[k] = load_quartet(noise, at + k * step);
+      }
+    };
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) load(r, r);
+    for (int b = 0;;) {
+#pragma unroll
+      for (int r = 0; r < kAhead; ++r, ++b) {
+        if (b >= n_b || f(b, t[r], mine[r])) return;
+        load(b + kAhead, r);
+      }
     }
   }
-  // Its scores (-inf: none, or marked).
-  __device__ __forceinline__ void scores(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
+  // Its scores (-inf or a NaN: none, or marked).
+  __device__ __forceinline__ void raw_scores(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
     if (kRules && streams_words()) scores_of<true>(b, t, z);
     else scores_of<false>(b, t, z);
+  }
+  // The same without a NaN.
+  __device__ __forceinline__ void scores(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
+    raw_scores(b, t, z);
+#pragma unroll
+    for (int q = 0; q < 4 * kUnroll; ++q) z[q] = __builtin_fmaxf(z[q], -INFINITY);
   }
   template <bool kWords>
   __device__ __forceinline__ void scores_of(int b, const Batch& t, float (&z)[4 * kUnroll]) const {
@@ -220,7 +263,7 @@ struct Walker {
                                  static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(out), e, 1)));
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) z[4 * k + e] = scored(x[e], kWords ? c[e] : 0);
+      for (int e = 0; e < 4; ++e) z[4 * k + e] = scored_raw(x[e], kWords ? c[e] : 0);
     }
   }
   __device__ __forceinline__ int token(int b, int q) const { return 4 * (first_of(b) + q / 4 * threads) + q % 4; }
@@ -251,13 +294,16 @@ struct Walker {
     if (tid == 0) s.n = 0;
     __syncthreads();
     const u16x4* s4 = reinterpret_cast<const u16x4*>(w.seen);
-    for (int i0 = 0; i0 < e4; i0 += kUnroll * threads) {
-      u16x4 c[kUnroll];
+    constexpr int kWords = 8;  // quartets of a thread in a batch
+    auto load = [&](int i0, u16x4 (&c)[kWords]) {
+      if (i0 >= e4) return;
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) c[k] = s4[min(i0 + tid + k * threads, e4 - 1)];
+      for (int k = 0; k < kWords; ++k) c[k] = s4[min(i0 + tid + k * threads, e4 - 1)];
+    };
+    auto list = [&](int i0, const u16x4 (&c)[kWords]) {
       uint32_t said = 0;  // bit 4 k + e: the batch's entry has a word
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k)
+      for (int k = 0; k < kWords; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) said |= (i0 + tid + k * threads < e4 && c[k][e] ? 1u : 0u) << (4 * k + e);
       const int m = __popc(said), upto = static_cast<int>(wave_scan(static_cast<u64>(m)));
@@ -268,6 +314,16 @@ struct Walker {
         const int q = __ffs(said) - 1;
         if (at < kSaid) apart[at] = 4 * (i0 + tid + q / 4 * threads) + q % 4;
       }
+    };
+    const int step = kWords * threads;
+    u16x4 c0[kWords], c1[kWords];
+    load(0, c0);
+    for (int i0 = 0; i0 < e4; i0 += 2 * step) {  // (each in registers of its own)
+      load(i0 + step, c1);
+      list(i0, c0);
+      if (i0 + step >= e4) break;
+      load(i0 + 2 * step, c0);
+      list(i0 + step, c1);
     }
     const int j = 4 * e4 + tid;
     if (j < a.V && w.seen[j]) {
@@ -276,27 +332,40 @@ struct Walker {
     }
     __syncthreads();
     n_said = s.n <= kSaid ? s.n : -1;
+    for (int i = tid; i < n_said; i += threads) said_word[i] = w.seen[apart[i]];
   }
 
   // Marks the row's entries that the stream passes over.
   __device__ __forceinline__ void mark_row() {
     const int words = (a.V + 31) / 32, at = w.bias0 + tid, bias = at < w.bias1 ? a.bias_tokens[at] : -1;
-    for (int i0 = 0; i0 < words; i0 += kUnroll * threads) {
-      uint32_t x[kUnroll];
+    typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
+    for (int i0 = 4 * tid; i0 < words; i0 += 4 * kUnroll * threads) {
+      u32x4u x[kUnroll];
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) {
-        const int i = i0 + k * threads + tid;
-        x[k] = w.mask && i < words ? ~w.mask[i] : 0u;
+        const int i = i0 + 4 * k * threads;
+        if (w.mask && i + 4 <= words) x[k] = *reinterpret_cast<const u32x4u*>(w.mask + i);
       }
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k)
-        if (i0 + k * threads + tid < words) skip[i0 + k * threads + tid] = x[k];
+      for (int k = 0; k < kUnroll; ++k) {
+        const int i = i0 + 4 * k * threads;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (i + e < words) skip[i + e] = !w.mask ? 0u : i + 4 <= words ? ~x[k][e] : ~w.mask[i + e];
+      }
     }
     mark_special(a, w, s.path, n, 0, a.V, skip, threads, at, bias);
     // One with a count word that is marked by now is forbidden, or scored as a special one.
-    for (int i = tid; i < n_said; i += threads) {
-      const uint32_t t = apart[i], bit = 1u << (t & 31);
-      apart_z[i] = atomicOr(&skip[t >> 5], bit) & bit ? -INFINITY : 0.f;
+    for (int i0 = tid; i0 < n_said; i0 += kUnroll * threads) {
+      uint32_t t[kUnroll], was[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) t[k] = apart[min(i0 + k * threads, n_said - 1)];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k)
+        if (i0 + k * threads < n_said) was[k] = atomicOr(&skip[t[k] >> 5], 1u << (t[k] & 31));
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k)
+        if (i0 + k * threads < n_said) apart_z[i0 + k * threads] = (was[k] >> (t[k] & 31)) & 1u ? -INFINITY : 0.f;
     }
     __syncthreads();
   }
@@ -306,20 +375,15 @@ struct Walker {
   // 152k vocabulary with one token in 50 said: 478 us, and 418 behind it).
   __device__ __forceinline__ void score_apart() {
     if constexpr (!kRules) return;
-    for (int i0 = tid; i0 < n_said; i0 += kUnroll * threads) {
-      int t[kUnroll], word[kUnroll];
-      float l[kUnroll];
+    constexpr int kGather = 8;
+    for (int i0 = tid; i0 < n_said; i0 += kGather * threads) {
+      float l[kGather];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) t[k] = apart[min(i0 + k * threads, n_said - 1)];
+      for (int k = 0; k < kGather; ++k) l[k] = w.logits[apart[min(i0 + k * threads, n_said - 1)]];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        l[k] = w.logits[t[k]];
-        word[k] = w.seen[t[k]];
-      }
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
+      for (int k = 0; k < kGather; ++k) {
         const int i = i0 + k * threads;
-        if (i < n_said && apart_z[i] == 0.f) apart_z[i] = scored(l[k], word[k]);
+        if (i < n_said && apart_z[i] == 0.f) apart_z[i] = scored(l[k], said_word[i]);
       }
     }
     const int room = kApart - max(n_said, 0), first = max(n_said, 0);
@@ -441,25 +505,18 @@ struct Walker {
     if (x > -INFINITY) key = max(key, pack_key(x, j));
   }
 
-  // arg-max of score (or of the logit, without noise) plus noise over the row.  The
-  // loads of a batch are under way while the one before is scored.
+  // arg-max of score (or of the logit, without noise) plus noise over the row.
   template <bool kNoise>
   __device__ __forceinline__ u64 plain() {
     Top best;
     u64 key = 0;
-    Batch t;
-    load<kNoise>(0, t);
-    const int n_b = batches();
-    for (int b = 0; b < n_b; ++b) {
-      Batch next;
-      if (b + 1 < n_b) load<kNoise>(b + 1, next);
-      __builtin_amdgcn_sched_barrier(0);  // (no load waits for the scores)
+    stream<kNoise, kNoise ? kAheadNoise : kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
       float z[4 * kUnroll];
-      scores(b, t, z);
+      raw_scores(b, t, z);
 #pragma unroll
       for (int q = 0; q < 4 * kUnroll; ++q) best.ascending(kNoise ? add_rounded(z[q], t.g[q / 4][q % 4]) : z[q], token(b, q));
-      t = next;
-    }
+      return false;
+    });
     score_apart();
     extras([&](float z, int j) {
       if (z > -INFINITY) take(key, z, j);
@@ -479,59 +536,57 @@ struct Walker {
         m = top;
       }
     };
-    Batch t, next;
-    load<kDraw>(0, t);
-    const int n_b = batches();
-    Batch third;
-    if (!kDraw && n_b > 1) load<kDraw>(1, next);
-    if (!kDraw && n_b > 2) load<kDraw>(2, third);
-    for (int b = 0; b < n_b; ++b) {
-      Batch later;  // (two batches ahead, or one where the noise's take as many registers)
-      if (kDraw && b + 1 < n_b) load<kDraw>(b + 1, next);
-      if (!kDraw && b + 3 < n_b) load<kDraw>(b + 3, later);
-      __builtin_amdgcn_sched_barrier(0);
-      if (first_of(b) < e4) {
-        float z[4 * kUnroll];
-        scores(b, t, z);
-        float top = z[0];
+    const int n_b = __builtin_amdgcn_readfirstlane(batches());
+    int seg_at = tid, seg_left = seg_batches;  // the segment's place; its batches that are to come
+    stream<kDraw, kDraw ? kAheadNoise : kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
+      float z[4 * kUnroll], four[kUnroll], top = -INFINITY;
+      raw_scores(b, t, z);
 #pragma unroll
-        for (int q = 1; q < 4 * kUnroll; ++q) top = larger_of(top, z[q]);
-        add(top);
-        if (kMass) {
-          // (the difference first: a large score's product with log2(e) has lost what parts it from the maximum)
-          const float ref = m == -INFINITY ? 0.f : m;
-          float part[2] = {0.f, 0.f};
+      for (int k = 0; k < kUnroll; ++k) {  // (a maximum passes over a NaN)
+        four[k] = __builtin_fmaxf(__builtin_fmaxf(z[4 * k], z[4 * k + 1]), __builtin_fmaxf(z[4 * k + 2], z[4 * k + 3]));
+        top = __builtin_fmaxf(top, four[k]);
+      }
+      add(top);
+      if (kMass) {
+        // exp(z - ref) as 2^(z log2(e) - c), one operation before the power; c is rounded,
+        // which all terms share and the last factor takes back.
+        const float ref = m == -INFINITY ? 0.f : m, c = ref * kLog2e, off = __builtin_fmaf(ref, kLog2e, -c);
+        float part[2] = {0.f, 0.f};
 #pragma unroll
-          for (int q = 0; q < 4 * kUnroll; ++q) part[q & 1] += exp_of(z[q] - ref);
-          sum += part[0] + part[1];
+        for (int q = 0; q < 4 * kUnroll; ++q) part[q & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(z[q], kLog2e, -c));
+        float both = (part[0] + part[1]) * __builtin_amdgcn_exp2f(-off);
+        if (!(both < INFINITY) || !(__builtin_fabsf(ref) < 65536.f)) {
+          // a NaN, or a score whose product with log2(e) has lost what parts it from the maximum
+          both = 0.f;
+#pragma unroll
+          for (int q = 0; q < 4 * kUnroll; ++q) both += exp_of(__builtin_fmaxf(z[q], -INFINITY) - ref);
         }
-        if (kDraw)
+        sum += both;
+      }
+      if (kDraw)
 #pragma unroll
-          for (int q = 0; q < 4 * kUnroll; ++q) d.ascending(z[q], add_rounded(z[q], t.g[q / 4][q % 4]), token(b, q));
-        if (batch_segs == 1) seg = larger_of(seg, top);
-        else
+        for (int q = 0; q < 4 * kUnroll; ++q) d.ascending(z[q], add_rounded(z[q], t.g[q / 4][q % 4]), token(b, q));
+      if (batch_segs == 1) {
+        seg = larger_of(seg, top);
+        if (--seg_left == 0 || b + 1 == n_b) {
+          s.seg[seg_at] = seg;
+          seg_at += threads;
+          seg_left = seg_batches;
+          seg = -INFINITY;
+        }
+      } else {
 #pragma unroll
-          for (int k = 0; k < kUnroll; ++k) {
-            const float four = larger_of(larger_of(z[4 * k], z[4 * k + 1]), larger_of(z[4 * k + 2], z[4 * k + 3]));
-            seg = larger_of(seg, four);
-            if ((k + 1) * batch_segs % kUnroll == 0) {
-              s.seg[(b * batch_segs + k * batch_segs / kUnroll) * threads + tid] = seg;
-              seg = -INFINITY;
-            }
+        for (int k = 0; k < kUnroll; ++k) {
+          seg = __builtin_fmaxf(seg, four[k]);
+          if ((k + 1) * batch_segs % kUnroll == 0) {
+            s.seg[seg_at] = seg;
+            seg_at += threads;
+            seg = -INFINITY;
           }
-      } else if (batch_segs > 1) {
-        for (int g = 0; g < batch_segs; ++g) s.seg[(b * batch_segs + g) * threads + tid] = -INFINITY;
+        }
       }
-      if (batch_segs == 1 && ((b + 1) % seg_batches == 0 || b + 1 == n_b)) {
-        s.seg[b / seg_batches * threads + tid] = seg;
-        seg = -INFINITY;
-      }
-      t = next;
-      if (!kDraw) {
-        next = third;
-        third = later;
-      }
-    }
+      return false;
+    });
     score_apart();
     extras([&](float z, int j) {
       add(z);
@@ -572,19 +627,20 @@ struct Walker {
       x[i] = s.segbin[lane * kPer + i];
       sum += x[i];  // (16 segments of 512 threads: neither field runs over)
     }
-    u64 before = wave_scan(sum) - sum;
+    const u64 before = wave_scan(sum) - sum;
     // (a margin for the weights' roundings)
     const u64 want = mass < 1e6 ? static_cast<u64>(mass * 16777216.0 * 1.00001) + 1 : ~0ull;
     int found = kSegBins;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      before += x[i];
-      if (found == kSegBins && (static_cast<int64_t>(before >> kMassBits) >= k || (before & kMassMask) >= want))
-        found = lane * kPer + i;
+    for (int i = kPer - 1; i >= 0; --i) {
+      const u64 upto = before + sum;
+      if (static_cast<int64_t>(upto >> kMassBits) >= k || (upto & kMassMask) >= want) found = lane * kPer + i;
+      sum -= x[i];
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) found = min(found, shfl_xor(found, off));
-    return found < kSegBins ? M - (found + 1.01f) * 0.125f : -INFINITY;
+    const u64 lanes = __ballot(found < kSegBins);
+    if (!lanes) return -INFINITY;
+    found = __builtin_amdgcn_readlane(found, __ffsll(static_cast<long long>(lanes)) - 1);
+    return M - (found + 1.01f) * 0.125f;
   }
 
   // Sorts the list's first `count` entries, largest first.  A wave's 64 pairs at a
@@ -794,23 +850,13 @@ struct Walker {
   }
 
   // Calls f(batch number, batch, whether it is the thread's) in a wave for the batches
-  // that have a score of `least` or more in one of its threads, the next one's loads
-  // under way.
+  // that have a score of `least` or more in one of its threads.
   template <bool kNoise, typename Fn>
   __device__ __forceinline__ void batches_from(float least, Fn f) {
-    const int n_b = batches();
-    Batch t;
-    bool on = reaches(0, least);
-    if (on) load<kNoise>(0, t);
-    for (int b = 0; b < n_b; ++b) {
-      Batch next;
-      const bool more = b + 1 < n_b && reaches(b + 1, least);
-      if (more) load<kNoise>(b + 1, next);
-      __builtin_amdgcn_sched_barrier(0);
+    stream<kNoise, kNoise ? kAheadNoise : kAhead>([&](int b) { return reaches(b, least); }, [&](int b, const Batch& t, bool on) {
       if (__ballot(on)) f(b, t, on);
-      t = next;
-      on = more;
-    }
+      return false;
+    });
   }
 
   // The best of the tokens of `least` and more before `after` in the order.
@@ -845,44 +891,34 @@ struct Walker {
       read += x;
       if (pack_key(z, j) > place) mass += x;
     });
-    Batch t;
-    if (first_of(0) < e4) load<false>(0, t);
-    for (int b = 0; b < n_b; ++b) {
-      Batch next;
-      if (b + 1 < n_b && first_of(b + 1) < e4) load<false>(b + 1, next);
-      __builtin_amdgcn_sched_barrier(0);
-      if (first_of(b) < e4) {
-        float z[4 * kUnroll], in = 0.f, out = 0.f;
-        scores(b, t, z);
-        bool equal = false;
+    bool less = false, decided = false;
+    stream<false, kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
+      float z[4 * kUnroll], in = 0.f, out = 0.f;
+      scores(b, t, z);
+      bool equal = false;
 #pragma unroll
-        for (int q = 0; q < 4 * kUnroll; ++q) {
-          const float x = exp_of(z[q] - M);
-          in += z[q] > edge ? x : 0.f;
-          out += z[q] > edge ? 0.f : x;
-          equal |= z[q] == edge;
-        }
-        if (equal)  // ties with the token at the place, itself among them: seldom
+      for (int q = 0; q < 4 * kUnroll; ++q) {
+        const float x = exp_of(z[q] - M);
+        in += z[q] > edge ? x : 0.f;
+        out += z[q] > edge ? 0.f : x;
+        equal |= z[q] == edge;
+      }
+      if (equal)  // ties with the token at the place, itself among them: seldom
 #pragma unroll
-          for (int q = 0; q < 4 * kUnroll; ++q)
-            if (z[q] == edge && token(b, q) < last) {
-              const float x = exp_of(z[q] - M);
-              mass += x;
-              read -= x;
-            }
-        mass += in;
-        read += static_cast<double>(in) + out;
-      }
-      t = next;
-      if ((b + 1) % kStage == 0 || b + 1 == n_b) {
-        const double before = all_sum(mass);
-        if (b + 1 == n_b) return before < target;
-        const double rest = all - all_sum(read);
-        if (before >= target) return false;
-        if (before + rest + 1e-5 * all < target) return true;  // (a margin for the sums' roundings)
-      }
-    }
-    return all_sum(mass) < target;  // (a row of extras alone)
+        for (int q = 0; q < 4 * kUnroll; ++q)
+          if (z[q] == edge && token(b, q) < last) {
+            const float x = exp_of(z[q] - M);
+            mass += x;
+            read -= x;
+          }
+      mass += in;
+      read += static_cast<double>(in) + out;
+      if ((b + 1) % kStage != 0 || b + 1 == n_b) return false;
+      const double before = all_sum(mass), rest = all - all_sum(read);
+      less = before + rest + 1e-5 * all < target;  // (a margin for the sums' roundings)
+      return decided = less || before >= target;
+    });
+    return decided ? less : all_sum(mass) < target;
   }
 
   // How many tokens lie up to a place in the order, and what they weigh.
@@ -1044,6 +1080,9 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   __shared__ uint32_t skip[kRules ? kMaxRuled / 32 : 1];
   __shared__ int32_t apart[kRules ? kApart : 1];
   __shared__ float apart_z[kRules ? kApart : 1];
+  __shared__ uint16_t said_word[kRules ? kSaid : 1];
+  __shared__ int32_t bias_tok[kRules ? kStaged : 1];
+  __shared__ float bias_val[kRules ? kStaged : 1];
   const int b = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
   const int64_t tr = static_cast<int64_t>(b) * a.N, orow = static_cast<int64_t>(b) * (a.Dmax + 1);
   const int n = min(max(a.n_nodes[b], 1), a.N);
@@ -1053,7 +1092,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   }
   const int lane = tid % SRT_WAVE, wave = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE), e4 = a.V / 4;
   const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
-  Walker<kRules> walker = {a, s, skip, apart, apart_z, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
+  Walker<kRules> walker = {a, s, skip, apart, apart_z, said_word, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
                            max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f, false};
   static_assert(kSegs % kUnroll == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
   while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
@@ -1070,7 +1109,24 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
     if constexpr (kRules) {
       // (penalties that change nothing: no counts are read)
       if (walker.w.r == 1.f && walker.w.f == 0.f && walker.w.p == 0.f) walker.w.seen = nullptr;
-      if (k == 0 && walker.w.seen) walker.list_said();
+      const int listed = walker.w.bias1 - walker.w.bias0;
+      if (k == 0) {
+        if (listed <= kStaged)
+          for (int i = tid; i < listed; i += threads) {
+            bias_tok[i] = a.bias_tokens[walker.w.bias0 + i];
+            bias_val[i] = a.bias_values[walker.w.bias0 + i];
+          }
+        if (walker.w.seen) walker.list_said();
+        else __syncthreads();
+        if (listed <= kStaged) {
+          a.bias_tokens = bias_tok;
+          a.bias_values = bias_val;
+        }
+      }
+      if (listed <= kStaged) {
+        walker.w.bias0 = 0;
+        walker.w.bias1 = listed;
+      }
       walker.mark_row();
     }
     const u64 key = choose<kRules, kNoise>(walker, top_k, p, mp);
