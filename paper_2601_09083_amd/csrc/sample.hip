@@ -14,9 +14,11 @@
 //
 // GPU design.  One workgroup walks one sequence, and its levels follow one another, so
 // what bounds a batch is one CU's time for a row times the longest walk's levels: of a
-// 152k vocabulary (608 KB) 15 us a row for the arg-max alone, 16 with min-p, 18 to 20
-// with a top-k, 24 with a top-p, 27 with a top-k of 200 and a top-p; 256 sequences of up
-// to 12 levels 410 us.  Of the 15 us the vector unit is busy for 10 to 12.  A row is read
+// 152k vocabulary (608 KB) 18 us a row for the arg-max with noise, 15 with min-p, 17 to
+// 18 with a top-k, 22 with a top-p, 26 with a top-k of 200 and a top-p, and under rules 5
+// to 10 more; 256 sequences of up to 13 rows 377 us.  A CU's loads come at 75 to 80 GB/s,
+// with two batches under way as with eight, which is 8 us of a row; the sum for a top-p
+// is bound by the vector unit (one operation of every entry takes 1 us).  A row is read
 // from HBM once: its maximum, its sum of exp(z - max), and the maximum of every thread's
 // every few entries (a segment) are taken in one pass.  A count and a lower bound of the
 // mass over the segments' maxima give a score below which nothing can be kept; segments
@@ -28,7 +30,7 @@
 // without a sort; if it is not, the kept ones lie before it, and the best of those is
 // next.  A list is sorted only where the mass of its first top_k is asked for.  Noise is
 // read at the listed tokens alone, or once a draw.  (Long lists narrowed down by
-// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass, drawn from 147.)
+// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass, drawn from 140.)
 // Sequences that cut nothing, or without noise, take the plain arg-max in one pass.
 #include "rules.h"
 
@@ -38,11 +40,14 @@ constexpr int kList = 4096;       // candidates that are sorted in LDS
 constexpr int kDraws = 12;        // of a long list's choice, before the last kept token is searched for
 constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
-constexpr int kAhead = 3;         // batches whose registers are loaded or used
-constexpr int kAheadNoise = 2;    // the same with the noise's
+// Batches whose registers are loaded or used, and the same with the noise's (256 walks of
+// 152k entries: 387 us a pass; 2 and 2 393, 4 and 3 395, 6 and 3 438, of which the code
+// has a copy of a batch's work each, and does not stay in the instruction cache).
+constexpr int kAhead = 3;
+constexpr int kAheadNoise = 2;
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
 // Batches after which a sum over a row is looked at (64 flat rows of 152k with a top-p of
-// 0.999, 0.9, 0.5: 77, 146, 280 us; 2: 76, 149, 290; at the row's end alone 91, 150, 275).
+// 0.999, 0.9, 0.5: 65, 125, 243 us; at the row's end alone 77, 130, 244).
 constexpr int kStage = 4;
 constexpr int kMost = 512;        // threads
 constexpr int kSegBins = 512;     // of the segments' maxima, 1 / 8 of the score wide
@@ -52,8 +57,8 @@ constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LD
 constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
 constexpr int kApart = kSaid + 512;  // and with them those of the path and of the bias list
 constexpr int kStaged = 512;      // entries of a bias list that are held in LDS
-// Rows up to which 256 threads walk (4 walks of 1024 entries: 38 us a pass, 40 with 512
-// threads; 256 of 152k: 608 us, 410 with 512).
+// Rows up to which 256 threads walk (4 walks of 1024 entries: 36 us a pass, 41 with 512
+// threads; 256 of 152k: 515 us, 377 with 512).
 constexpr int kShortVocab = 4096;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -165,16 +170,12 @@ struct Walker {
   int seg_batches, batch_segs;  // batches of a segment, or segments of a batch
   int parity;            // of the reductions' arrays: the next one's writes meet no reads of the last one's
   float M;               // largest score of the row
-  bool long_row;         // the row before had more candidates than the list holds
 
   // The best of a set of tokens by score and noise (packed, 0 if there is none), and
   // its place in the order.
   struct Draw {
     u64 best = 0, at = 0;
     float most = -INFINITY;
-    __device__ __forceinline__ void ascending(float z, float x, int j) {
-      if (x > most) any(z, x, j);
-    }
     __device__ __forceinline__ void any(float z, float x, int j) {
       const u64 key = pack_key(x, j);
       if (!(x > -INFINITY) || key <= best) return;
@@ -289,7 +290,7 @@ struct Walker {
   // Lists the tokens with a count word.  A penalty costs a division, which one such
   // token in a wave's 64 entries makes it take for all, and the words are half as much
   // to read as the logits: with them in the stream 64 walks of a 152k vocabulary, one
-  // token in 50 said, take 726 us, and 418 so.
+  // token in 50 said, take 695 us, and 412 so.
   __device__ __forceinline__ void list_said() {
     if (tid == 0) s.n = 0;
     __syncthreads();
@@ -526,8 +527,8 @@ struct Walker {
 
   // The pass over the row: M (-inf where nothing is left), the segments' maxima and,
   // if it is asked for, the row's mass in units of the largest weight.
-  template <bool kMass, bool kDraw>
-  __device__ __forceinline__ double first_pass(Draw& d) {
+  template <bool kMass>
+  __device__ __forceinline__ double first_pass() {
     float m = -INFINITY, seg = -INFINITY;
     double sum = 0.0;  // of parts of a batch each
     auto add = [&](float top) {  // the running maximum goes up to `top`
@@ -538,7 +539,7 @@ struct Walker {
     };
     const int n_b = __builtin_amdgcn_readfirstlane(batches());
     int seg_at = tid, seg_left = seg_batches;  // the segment's place; its batches that are to come
-    stream<kDraw, kDraw ? kAheadNoise : kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
+    stream<false, kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
       float z[4 * kUnroll], four[kUnroll], top = -INFINITY;
       raw_scores(b, t, z);
 #pragma unroll
@@ -563,9 +564,6 @@ struct Walker {
         }
         sum += both;
       }
-      if (kDraw)
-#pragma unroll
-        for (int q = 0; q < 4 * kUnroll; ++q) d.ascending(z[q], add_rounded(z[q], t.g[q / 4][q % 4]), token(b, q));
       if (batch_segs == 1) {
         seg = larger_of(seg, top);
         if (--seg_left == 0 || b + 1 == n_b) {
@@ -591,7 +589,6 @@ struct Walker {
     extras([&](float z, int j) {
       add(z);
       if (kMass && z > -INFINITY) sum += exp_of(z - m);
-      if (kDraw && z > -INFINITY) d.any(z, add_rounded(z, w.noise[j]), j);
     });
     // Join: first the wave's lanes, then the waves.
     const float top = wave_largest(m);
@@ -962,10 +959,10 @@ struct Walker {
   // millionth a dozen.  Noise that is none could be arranged to take one for every
   // token; after kDraws the last kept place is found bit by bit, as is the place of the
   // k-th token where the mass of the first k is asked for.
-  // `best`, at `place`: the first draw, if it has been made.  (One loop, so that each
+  // (One loop, so that each
   // pass over the row stands in the code once: what a walk runs fits the instruction
   // cache.)
-  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float lowest, float by_min, u64 best, u64 place) {
+  __device__ __forceinline__ u64 from_row(int k, float p, double mass, float lowest, float by_min) {
     const float least = __builtin_fmaxf(lowest, by_min);
     const bool by_k = k < a.V, by_p = p < 1.f;
     bool searching = by_k && by_p, summing = false, last = false;  // the k-th place; its mass; the last kept place is known
@@ -975,7 +972,7 @@ struct Walker {
     const u64 first = pack_key(M, 0), ends = first ^ pack_key(lowest, a.V - 1);
     const int top_bit = 63 - __clzll(static_cast<long long>(ends | 1));
     const u64 common = first & ~((2ull << top_bit) - 1);
-    u64 found = common;
+    u64 found = common, best = 0, place = 0;
     for (int bit = top_bit, draw = 0;;) {
       u64 at = place;
       if (searching) {
@@ -983,11 +980,9 @@ struct Walker {
       } else if (summing) {
         at = found;
       } else {
-        if (!best || draw > 0) {
-          best = candidate(place, least);
-          if (!best) return 0;
-          place = at = s.found;
-        }
+        best = candidate(place, least);
+        if (!best) return 0;
+        place = at = s.found;
         if (last || !(by_k || by_p)) return best;
         if (!by_k) {
           if (score_of(place) >= least && weighs_less(place, target, mass)) return best;  // (nothing lies before the first)
@@ -1035,19 +1030,8 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   for (int i = x.tid; i < kSegBins; i += x.threads) s.segbin[i] = 0;
   if (x.tid == 0) s.n = s.m = 0;
   double mass = 0.0;
-  // Where the row before had a long list, this one's first draw is made along with the pass.
-  u64 draw = 0, place = 0;
-  typename Walker<kRules>::Draw d;
-  if (by_p && !by_k && x.long_row) {
-    mass = x.template first_pass<true, true>(d);
-    draw = x.drawn(d);
-    place = s.found;
-  } else if (by_p && !by_k) {
-    mass = x.template first_pass<true, false>(d);
-  } else {
-    x.template first_pass<false, false>(d);
-  }
-  x.long_row = false;
+  if (by_p && !by_k) mass = x.template first_pass<true>();
+  else x.template first_pass<false>();
   const float M = x.M;
   if (M == -INFINITY) return 0;
   // (infinite scores: the lowest token of them, which is always kept)
@@ -1070,8 +1054,7 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
     least = __builtin_fmaxf(least, x.least_kept(by_k ? k : 0x7fffffff, by_k ? INFINITY : static_cast<double>(p) * mass));
   const int count = M == INFINITY ? kList + 1 : x.collect(least);
   if (count <= kList) return x.from_list(count, k, by_p ? static_cast<double>(p) : 1.0, mass, by_min);
-  x.long_row = true;
-  return x.from_row(k, p, mass, least, by_min, draw, place);
+  return x.from_row(k, p, mass, least, by_min);
 }
 
 template <bool kRules, bool kNoise>
@@ -1093,7 +1076,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   const int lane = tid % SRT_WAVE, wave = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE), e4 = a.V / 4;
   const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
   Walker<kRules> walker = {a, s, skip, apart, apart_z, said_word, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
-                           max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f, false};
+                           max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f};
   static_assert(kSegs % kUnroll == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
   while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
   const float p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
