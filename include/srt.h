@@ -600,12 +600,15 @@ int srt_rope_rows(const srt_rope* rope, int32_t B, int32_t T, int32_t Hq, int32_
  * results are those of the first one's pages.  Members need not be next to each
  * other; groups of one member share nothing.  n_groups 0: no sequence shares
  * (group_ids and prefix_len may be NULL).  Sharing changes where the splits of the
- * keys lie, and so the results by rounding only.
+ * keys lie, and so the results by rounding only; where it would save nothing (a
+ * batch of so few keys that every split has a compute unit of its own, trees whose
+ * rows fill the tiles by themselves) keys are read as srt_tree_attn reads them.
  * group_ids [B], prefix_len [n_groups] int32; everything else as srt_tree_attn.
  * scratch: srt_tree_attn_shared_scratch_bytes(...) bytes (0 for arguments that the
  * call refuses), 256-byte aligned, else SRT_ERR_CAPACITY / SRT_ERR_INVALID.
- * Unsupported (SRT_ERR_UNSUPPORTED): B > 65535, n_groups > 4096, Hkv > 255,
- * max_pages * page > 2^30, or B * N * Hq / Hkv beyond 2^23 rows.
+ * Unsupported (SRT_ERR_UNSUPPORTED): what srt_tree_attn does not support (of it
+ * B > 65535, Hkv > 255, more than 4095 splits of 8192 positions), n_groups > 4096,
+ * or B * N * Hq / Hkv beyond 2^23 rows.
  * ---------------------------------------------------------------------- */
 size_t srt_tree_attn_shared_scratch_bytes(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t d,
                                           int32_t page, int32_t max_pages, int32_t n_groups);

@@ -826,9 +826,10 @@ bool each_alone(int32_t B, int32_t Hkv, int64_t rb, int64_t cap, int cus) {
   return static_cast<int64_t>(B) * Hkv * splits_for(cap, c) * rb <= cus;
 }
 
-// Work-list packing: 16 bits of a sequence or group, 15 of a row block, 8 of a KV head, 24 of a split.
+// Work-list packing: 16 bits of a sequence or group, 15 of a row block, 8 of a KV head, 24 of
+// a split; and that of srt_tree_attn, which takes some of the calls.
 bool fits(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int64_t cap, int32_t n_groups) {
-  if (B > 65535 || n_groups > kMaxGroups || Hkv > 255 || cap > (int64_t(1) << 30)) return false;
+  if (n_groups > kMaxGroups || cap > (int64_t(1) << 30) || !packs(B, N, Hq, Hkv, cap, false)) return false;
   const int64_t rows = static_cast<int64_t>(B) * N * (Hq / Hkv);
   if (rows / kRowsPerBlock > 32766) return false;
   const Sizes z = sizes_for(B, N, Hq, Hkv, 128, cap, n_groups);

@@ -2,6 +2,8 @@
 touched (no GPU; pointers are never followed)."""
 import ctypes
 
+import pytest
+
 from paper_2601_09083_amd import srt as S
 from tests.test_abi_quant_rules import P, built_library  # noqa: F401
 
@@ -33,3 +35,14 @@ def test_pointers_and_scratch():
     assert attn(scratch=None) == S.SRT_ERR_CAPACITY and attn(size=need() - 1) == S.SRT_ERR_CAPACITY
     assert attn(scratch=ctypes.c_void_p(4096 + 16)) == S.SRT_ERR_INVALID
     assert attn(n_groups=0, ids=None, prefix=None, size=0) == S.SRT_ERR_CAPACITY  # (further on, without groups)
+
+
+@pytest.mark.parametrize("n_groups", [0, 2])
+def test_calls_that_the_plain_attention_refuses(n_groups):
+    """Some calls go to srt_tree_attn: what it cannot pack is refused by both, before anything is read."""
+    for B, pages in ((4, 1 << 22), (1, 1 << 22), (512, 1 << 22)):
+        assert S.srt_tree_attn_scratch_bytes(B, 8, 4, 2, 128, 16, pages) > 0
+        assert need(B=B, max_pages=pages, n_groups=n_groups) == 0
+        assert attn(B=B, max_pages=pages, n_groups=n_groups) == S.SRT_ERR_UNSUPPORTED
+    # (4095 splits of 8192 positions are the most that one packs)
+    assert need(B=4, max_pages=4095 * 512, n_groups=n_groups) > 0 and need(B=4, max_pages=4095 * 512 + 1, n_groups=n_groups) == 0
