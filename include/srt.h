@@ -596,8 +596,8 @@ int srt_rope_rows(const srt_rope* rope, int32_t B, int32_t T, int32_t Hq, int32_
  * prefix_len[g] positions, as far as whole pages go: the pages are the same ones.
  * What is taken as shared is prefix_len[g] or the shortest member's context, if
  * that is shorter, rounded down to whole pages, and read through the block table
- * of the group's first sequence; where the tables do not agree there, the others'
- * results are those of the first one's pages.  Members need not be next to each
+ * of the group's first sequence or the member's own: where the tables do not agree
+ * there, a result is that of either's pages.  Members need not be next to each
  * other; groups of one member share nothing.  n_groups 0: no sequence shares
  * (group_ids and prefix_len may be NULL).  Sharing changes where the splits of the
  * keys lie, and so the results by rounding only; where it would save nothing (a

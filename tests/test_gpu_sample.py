@@ -211,6 +211,63 @@ def test_long_bias_lists_and_tokens_listed_again():
         c.check(c.run())
 
 
+def test_bias_lists_beyond_their_room():
+    """Longer than what is staged, and than what is scored apart together with the counted tokens."""
+    for V, n in ((9001, 513), (20000, 5000), (20000, 12000)):
+        c = Case(17, 4, 6, V, 3, ruled=True, bias=0, cuts=[(10, 1.0, 0.0), (0, 0.8, 0.0), (0, 1.0, 0.1), (0, 1.0, 0.0)])
+        rng = np.random.default_rng(18)
+        for b in (0, 1, 2):
+            c.bias[b] = sorted((int(t), float(np.float32(x))) for t, x in zip(rng.integers(-2, V + 3, n), rng.normal(0, 2, n)))
+        c.check(c.run())
+
+
+@pytest.mark.parametrize("V,ruled", [(1 << 21, False), (1 << 18, True)])
+def test_the_largest_vocabularies(V, ruled):
+    c = Case(19, 2, 2, V, 1, a=(0.5, 1.5), cuts=[(0, 0.9, 0.0), (50, 0.9, 0.0)], ruled=ruled)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("ruled", [False, True])
+def test_the_deepest_walks_of_the_widest_trees(ruled):
+    c = Case(20, 4, 256, 200, 63, cuts=[(1, 1.0, 0.0), (0, 1e-6, 0.0), (2, 1.0, 0.99), (0, 1.0, 0.0)])
+    for b in range(c.B):
+        c.n[b] = 256
+        for i in range(1, 256):  # a chain of 64 levels, and side branches of other tokens
+            c.par[b, i] = i - 1 if i < 64 else i % 64
+            c.tok[b, i] = (3 * i) % 100 if i < 64 else 100 + i % 100
+        top = c.logits[b].max() + 60  # (above the tokens that Case has planted)
+        for i in range(63):
+            c.logits[b, i, c.tok[b, i + 1]] = top
+    if ruled:
+        c.words = np.zeros((c.B, c.V), dtype=np.uint16)
+        c.f = np.full(c.B, 0.25, dtype=np.float32)
+        c.r = c.q = None
+    assert c.check(c.run()) == 63
+
+
+@pytest.mark.parametrize("V", [700, 30000])
+def test_inverse_temperatures_that_turn_or_flatten_the_order(V):
+    """Of 0 all scores are equal, of a negative one the least logit is the first."""
+    c = Case(21, 12, 3, V, 2, invT=(0.0, -1.0, 1e-30, 1e30), cuts=[(7, 1.0, 0.0), (0, 0.5, 0.0), (V // 2, 0.5, 0.0)])
+    c.check(c.run())
+
+
+def test_two_walks_at_once():
+    cs = [Case(22, 32, 8, 20483, 4), Case(23, 16, 8, 9000, 4, ruled=True)]
+    want = [c.run() for c in cs]
+    args = [(c.args(), c.rules()) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for (a, rules), s in zip(args, streams):
+            with torch.cuda.stream(s):
+                got.append(srt.srt_accept_sample(*a, rules=rules))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(g[k], want[i % 2][k]) for k in g)
+
+
 def test_masks_that_leave_little_or_nothing():
     for V in (40, 30000):
         c = Case(9, 8, 6, V, 3, ruled=True, bias=0, cuts=[(5, 0.9, 0.0), (0, 0.8, 0.0)])
