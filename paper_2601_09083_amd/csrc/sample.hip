@@ -39,6 +39,7 @@ namespace {
 constexpr int kList = 4096;       // candidates that are sorted in LDS
 constexpr int kDraws = 12;        // of a long list's choice, before the last kept token is searched for
 constexpr int kSegs = 16;         // segments of a thread, at most
+constexpr int kSegsAt = 4;        // of them looked at together
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
 // Batches whose registers are loaded or used, and the same with the noise's (256 walks of
 // 152k entries: 387 us a pass; 2 and 2 393, 4 and 3 395, 6 and 3 438, of which the code
@@ -112,10 +113,19 @@ __device__ __forceinline__ double wave_scan(double x) {
 __device__ __forceinline__ double last_lane(double x) {
   return __builtin_bit_cast(double, last_lane(__builtin_bit_cast(u64, x)));
 }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float larger_of_lane(float x) {  // (where there is none, x)
+  const int y = __float_as_int(x);
+  return larger_of(x, __int_as_float(__builtin_amdgcn_update_dpp(y, y, kCtrl, kRows, 0xf, false)));
+}
 __device__ __forceinline__ float wave_largest(float x) {
-  const u64 key = wave_top(pack_key(x, 0));
-  const uint32_t u = static_cast<uint32_t>(key >> 32);
-  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+  x = larger_of_lane<0x111, 0xf>(x);
+  x = larger_of_lane<0x112, 0xf>(x);
+  x = larger_of_lane<0x114, 0xf>(x);
+  x = larger_of_lane<0x118, 0xf>(x);
+  x = larger_of_lane<0x142, 0xa>(x);
+  x = larger_of_lane<0x143, 0xc>(x);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), SRT_WAVE - 1));
 }
 
 __device__ __forceinline__ float score_of(u64 key) {
@@ -410,6 +420,12 @@ struct Walker {
     return any;
   }
 
+  // The maxima of the thread's segments from i0 on (-inf: none).
+  __device__ __forceinline__ void segments(int i0, int segs, float (&x)[kSegsAt]) const {
+#pragma unroll
+    for (int k = 0; k < kSegsAt; ++k) x[k] = i0 + k < segs ? s.seg[(i0 + k) * threads + tid] : -INFINITY;
+  }
+
   // Appends a token to the list where `in`; s.n counts all, also those that find no room.
   __device__ __forceinline__ void append(bool in, float z, int j) const {
     const u64 lanes = __ballot(in);
@@ -430,17 +446,27 @@ struct Walker {
   __device__ __forceinline__ int collect(float least) {
     const int per = kUnroll * seg_batches / batch_segs;  // quartets of a segment
     const int segs = (batches() + seg_batches - 1) / seg_batches * batch_segs;
-    for (int i = 0; i < segs; ++i) {
-      const int id = i * threads + tid;
-      const float top = s.seg[id];
-      const u64 lanes = __ballot(top >= least && top > -INFINITY);
-      if (!lanes) continue;
+    for (int i0 = 0; i0 < segs; i0 += kSegsAt) {
+      float top[kSegsAt];
+      segments(i0, segs, top);
+      u64 lanes[kSegsAt];
+      int total = 0;
+#pragma unroll
+      for (int k = 0; k < kSegsAt; ++k) {
+        lanes[k] = __ballot(top[k] >= least && top[k] > -INFINITY);
+        total += __popcll(lanes[k]);
+      }
+      if (!total) continue;
       int at = 0;
-      if (lane == 0) at = atomicAdd(&s.m, __popcll(lanes));
-      at = __builtin_amdgcn_readfirstlane(at) +
-           static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32),
-                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0)));
-      if (((lanes >> lane) & 1) && at < kList) s.work[at] = static_cast<uint16_t>(id);
+      if (lane == 0) at = atomicAdd(&s.m, total);
+      at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+      for (int k = 0; k < kSegsAt; ++k) {
+        const int to = at + static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes[k] >> 32),
+                                                                       __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes[k]), 0)));
+        if (((lanes[k] >> lane) & 1) && to < kList) s.work[to] = static_cast<uint16_t>((i0 + k) * threads + tid);
+        at += __popcll(lanes[k]);
+      }
     }
     __syncthreads();
     const int m = s.m;
@@ -610,10 +636,15 @@ struct Walker {
   // The bins have been cleared; every wave takes the sums by itself.
   __device__ __forceinline__ float least_kept(int k, double mass) {
     const int segs = (batches() + seg_batches - 1) / seg_batches * batch_segs;
-    for (int i = 0; i < segs; ++i) {
-      const float x = s.seg[i * threads + tid], d = (M - x) * 8.f;
-      if (d < kSegBins)  // (not where x is -inf)
-        atomicAdd(&s.segbin[static_cast<int>(d)], (1ull << kMassBits) + static_cast<u64>(exp_of(x - M) * 16777216.f));
+    for (int i0 = 0; i0 < segs; i0 += kSegsAt) {
+      float x[kSegsAt];
+      segments(i0, segs, x);
+#pragma unroll
+      for (int k = 0; k < kSegsAt; ++k) {
+        const float d = (M - x[k]) * 8.f;
+        if (d < kSegBins)  // (not where x is -inf)
+          atomicAdd(&s.segbin[static_cast<int>(d)], (1ull << kMassBits) + static_cast<u64>(exp_of(x[k] - M) * 16777216.f));
+      }
     }
     __syncthreads();
     constexpr int kPer = kSegBins / SRT_WAVE;
@@ -1020,7 +1051,7 @@ struct Walker {
 
 // The choice at the node that the row belongs to: packed (score with noise, token), 0 if none.
 template <bool kRules, bool kNoise>
-__device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float mp) {
+__device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float mp, double edge) {
   Lds& s = x.s;
   const int V = x.a.V;
   if (!(p > 0.f) || !(mp <= 1.f)) k = 1, p = 1.f, mp = 0.f;  // (a NaN too)
@@ -1038,8 +1069,7 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   if (M == INFINITY) k = V, p = 1.f, by_k = by_p = by_m = false;
   // The scores below which nothing is kept.
   float by_min = -INFINITY;
-  if (by_m) {  // the smallest float whose distance from M is no more than log(min_p)
-    const double edge = log(static_cast<double>(mp));
+  if (by_m) {  // the smallest float whose distance from M is no more than log(min_p), `edge`
     by_min = static_cast<float>(static_cast<double>(M) + edge);
     if (static_cast<double>(by_min) - static_cast<double>(M) < edge) by_min = nextafterf(by_min, INFINITY);
   }
@@ -1047,8 +1077,8 @@ __device__ __forceinline__ u64 choose(Walker<kRules>& x, int k, float p, float m
   float least = M == INFINITY ? M : by_k && by_p ? M - 104.f : by_min;
   if (by_p && !by_k) {
     // tokens below this weigh no more than 1 - p of the row together
-    const double d = log(static_cast<double>(V) / ((1.0 - static_cast<double>(p)) * mass));
-    least = __builtin_fmaxf(least, M - static_cast<float>(d) - 0.01f);
+    const float d = __logf(static_cast<float>(V / ((1.0 - static_cast<double>(p)) * mass)));
+    least = __builtin_fmaxf(least, M - d - 0.01f);
   }
   if (by_k || by_p)
     least = __builtin_fmaxf(least, x.least_kept(by_k ? k : 0x7fffffff, by_k ? INFINITY : static_cast<double>(p) * mass));
@@ -1081,6 +1111,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
   while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
   const float p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
+  const double edge = mp > 0.f ? log(static_cast<double>(mp)) : 0.0;
   int u = 0, k = 0, tok;
   for (;; ++k) {
     walker.w = rules_of(a, b, k);
@@ -1112,7 +1143,7 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
       }
       walker.mark_row();
     }
-    const u64 key = choose<kRules, kNoise>(walker, top_k, p, mp);
+    const u64 key = choose<kRules, kNoise>(walker, top_k, p, mp, edge);
     tok = key ? key_token(key) : -1;
     __syncthreads();  // (the staged tree, at the first step; LDS is the next row's from here on)
     int child = -1;
