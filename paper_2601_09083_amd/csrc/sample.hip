@@ -700,8 +700,7 @@ struct Walker {
 
   // The choice from a list of up to 64 R tokens, by wave 0 in registers: R a lane,
   // place 64 r + lane.  Drawn from as a long list is (weighs_less); it is sorted, and
-  // its weights summed in order, where the mass of the first k is asked for and more
-  // than k are there, or no draw was kept.
+  // its weights summed in order, where no draw was kept.
   template <int R>
   __device__ __forceinline__ u64 from_short(int count, int k, double p, double row_mass, float least) {
     if (wave == 0) {
@@ -709,7 +708,21 @@ struct Walker {
 #pragma unroll
       for (int r = 0; r < R; ++r) x[r] = SRT_WAVE * r + lane < count ? s.list[SRT_WAVE * r + lane] : 0ull;
       bool done = false;
-      if (!(k < count && p < 1.0)) {
+      if (k < count && p < 1.0) {  // the k-th place, bit by bit until k tokens lie up to one
+        u64 kth = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+          const u64 at = kth | 1ull << bit;
+          int n_at = 0;
+#pragma unroll
+          for (int r = 0; r < R; ++r) n_at += __popcll(__ballot(x[r] >= at));
+          if (n_at >= k) kth = at;
+          if (n_at == k) break;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (x[r] < kth) x[r] = 0;
+      }
+      {
         u64 key[R], place = 0;
         double wt[R], all = 0.0;
 #pragma unroll
