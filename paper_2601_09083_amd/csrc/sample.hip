@@ -426,18 +426,6 @@ struct Walker {
     for (int k = 0; k < kSegsAt; ++k) x[k] = i0 + k < segs ? s.seg[(i0 + k) * threads + tid] : -INFINITY;
   }
 
-  // Appends a token to the list where `in`; s.n counts all, also those that find no room.
-  __device__ __forceinline__ void append(bool in, float z, int j) const {
-    const u64 lanes = __ballot(in);
-    if (!lanes) return;
-    int at = 0;
-    if (lane == __ffsll(static_cast<long long>(lanes)) - 1) at = atomicAdd(&s.n, __popcll(lanes));
-    at = __shfl(at, __ffsll(static_cast<long long>(lanes)) - 1, SRT_WAVE) +
-         static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32),
-                                                    __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0)));
-    if (in && at < kList) s.list[at] = pack_key(z, j);
-  }
-
   // The tokens of score `least` and more as the list, and how many there are (more
   // than kList: at least that many).  The segments that reach it are listed first and
   // their quartets dealt out to all threads: where a thread reads its own ones again,
@@ -485,18 +473,29 @@ struct Walker {
         }
         if (at[k] < e4) x[k] = r4[at[k]];
       }
+      float z[4 * kAgain];
+      int mine = 0;
 #pragma unroll
       for (int k = 0; k < kAgain; ++k) {
         const bool on = at[k] < e4;
         const uint32_t out = kRules && on ? skip[at[k] >> 3] >> ((4 * at[k]) & 31) : 0u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int j = 4 * at[k] + e;
           const bool in = on && !((out >> e) & 1u);
-          const float z = in ? scored(x[k][e], kRules && streams_words() ? w.seen[j] : 0) : -INFINITY;
-          append(z >= least && z > -INFINITY, z, j);
+          z[4 * k + e] = in ? scored(x[k][e], kRules && streams_words() ? w.seen[4 * at[k] + e] : 0) : -INFINITY;
+          mine += z[4 * k + e] >= least && z[4 * k + e] > -INFINITY;
         }
       }
+      const int upto = static_cast<int>(wave_scan(static_cast<u64>(mine)));
+      int to = 0;
+      if (lane == SRT_WAVE - 1 && upto > 0) to = atomicAdd(&s.n, upto);
+      to = __builtin_amdgcn_readlane(to, SRT_WAVE - 1) + upto - mine;
+#pragma unroll
+      for (int q = 0; q < 4 * kAgain; ++q)
+        if (z[q] >= least && z[q] > -INFINITY) {
+          if (to < kList) s.list[to] = pack_key(z[q], 4 * at[q / 4] + q % 4);
+          ++to;
+        }
       if (*const_cast<volatile int32_t*>(&s.n) > kList) break;  // (each wave by itself)
     }
     extras([&](float z, int j) {
@@ -699,15 +698,13 @@ struct Walker {
   __device__ __forceinline__ double weight(float z) const { return exp(static_cast<double>(z) - static_cast<double>(M)); }
 
   // The choice from a list of up to 64 R tokens, by wave 0 in registers: R a lane,
-  // place 64 r + lane.  Drawn from as a long list is (weighs_less); it is sorted, and
-  // its weights summed in order, where no draw was kept.
+  // place 64 r + lane, drawn from as a long list is (weighs_less) until a draw is kept.
   template <int R>
   __device__ __forceinline__ u64 from_short(int count, int k, double p, double row_mass, float least) {
     if (wave == 0) {
       u64 x[R], best = 0;
 #pragma unroll
       for (int r = 0; r < R; ++r) x[r] = SRT_WAVE * r + lane < count ? s.list[SRT_WAVE * r + lane] : 0ull;
-      bool done = false;
       if (k < count && p < 1.0) {  // the k-th place, bit by bit until k tokens lie up to one
         u64 kth = 0;
         for (int bit = 63; bit >= 0; --bit) {
@@ -722,82 +719,38 @@ struct Walker {
         for (int r = 0; r < R; ++r)
           if (x[r] < kth) x[r] = 0;
       }
-      {
-        u64 key[R], place = 0;
-        double wt[R], all = 0.0;
+      u64 key[R], place = 0;
+      double wt[R], all = 0.0;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          key[r] = 0;
-          if (x[r] && score_of(x[r]) >= least) take(key[r], score_of(x[r]), key_token(x[r]));
-          wt[r] = p < 1.0 && x[r] ? weight(score_of(x[r])) : 0.0;
-          all += wt[r];
-        }
-        const double target = p < 1.0 ? p * (k < a.V ? last_lane(wave_scan(all)) : row_mass) : INFINITY;
-        for (int draw = 0; draw < kDraws && !done; ++draw) {
-          u64 mine = 0, at = 0;
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            if (key[r] > mine && x[r] > place) {
-              mine = key[r];
-              at = x[r];
-            }
-          best = wave_top(mine);
-          if (!best) break;
-          const int owner = __ffsll(static_cast<long long>(__ballot(mine == best))) - 1;
-          place = static_cast<u64>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at >> 32), owner))) << 32 |
-                  static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), owner));
-          int before = 0;
-          double mass = 0.0;
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const bool in = x[r] > place;
-            before += __popcll(__ballot(in));
-            mass += in ? wt[r] : 0.0;
-          }
-          done = before == 0 || (before < k && (p >= 1.0 || last_lane(wave_scan(mass)) < target));
-        }
-        done = done || !best;
+      for (int r = 0; r < R; ++r) {
+        key[r] = 0;
+        if (x[r] && score_of(x[r]) >= least) take(key[r], score_of(x[r]), key_token(x[r]));
+        wt[r] = p < 1.0 && x[r] ? weight(score_of(x[r])) : 0.0;
+        all += wt[r];
       }
-      if (!done) {
-        best = 0;
+      const double target = p < 1.0 ? p * (k < a.V ? last_lane(wave_scan(all)) : row_mass) : INFINITY;
+      for (;;) {  // (each draw's place lies before the last one's)
+        u64 mine = 0, at = 0;
 #pragma unroll
-        for (int run = 2; run <= SRT_WAVE * R; run *= 2) {
-#pragma unroll
-          for (int d = run / 2; d >= SRT_WAVE; d /= 2)  // pairs in one lane
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const int o = r ^ (d / SRT_WAVE);
-              if (o < r) continue;
-              const bool falls = ((SRT_WAVE * r) & run) == 0;
-              const u64 hi = max(x[r], x[o]), lo = min(x[r], x[o]);
-              x[r] = falls ? hi : lo;
-              x[o] = falls ? lo : hi;
-            }
-          for (int d = min(run / 2, SRT_WAVE / 2); d >= 1; d /= 2)
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const u64 y = shfl_xor_u64(x[r], d);
-              const bool larger = ((lane & d) == 0) == (((SRT_WAVE * r + lane) & run) == 0);
-              x[r] = (x[r] > y) == larger ? x[r] : y;
-            }
-        }
-        double before = 0.0, incl[R], wt[R];
-        if (p < 1.0)
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            wt[r] = x[r] && SRT_WAVE * r + lane < k ? weight(score_of(x[r])) : 0.0;
-            incl[r] = wave_scan(wt[r]) + before;
-            before = last_lane(incl[r]);
+        for (int r = 0; r < R; ++r)
+          if (key[r] > mine && x[r] > place) {
+            mine = key[r];
+            at = x[r];
           }
-        const double target = p * (k < a.V ? before : row_mass);
+        best = wave_top(mine);
+        if (!best) break;
+        const int owner = __ffsll(static_cast<long long>(__ballot(mine == best))) - 1;
+        place = static_cast<u64>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at >> 32), owner))) << 32 |
+                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), owner));
+        int before = 0;
+        double mass = 0.0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const int i = SRT_WAVE * r + lane;
-          const float z = score_of(x[r]);
-          const bool keep = x[r] && i < k && (i == 0 || ((p >= 1.0 || incl[r] - wt[r] < target) && z >= least));
-          if (keep) take(best, z, key_token(x[r]));
+          const bool in = x[r] > place;
+          before += __popcll(__ballot(in));
+          mass += in ? wt[r] : 0.0;
         }
-        best = wave_top(best);
+        if (before == 0 || (before < k && (p >= 1.0 || last_lane(wave_scan(mass)) < target))) break;
       }
       if (lane == 0) s.found = best;
     }
