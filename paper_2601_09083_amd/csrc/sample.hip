@@ -219,7 +219,7 @@ struct Walker {
   // its loads).  Only threads with on() load.  Quartets behind the row's end read as 0.
   template <bool kNoise, int kAhead, typename On, typename Fn>
   __device__ __forceinline__ void stream(On on, Fn f) const {
-    const int n_b = __builtin_amdgcn_readfirstlane(batches()), bytes = 16 * e4;
+    const int n_b = batches(), bytes = 16 * e4;
     const uint32_t step = 16 * threads;
     const __amdgpu_buffer_rsrc_t row = buffer_of(w.logits, bytes);
     const __amdgpu_buffer_rsrc_t noise = buffer_of(kNoise ? w.noise : w.logits, bytes);
@@ -233,6 +233,7 @@ struct Walker {
         t[r].x[k] = load_quartet(row, at + k * step);
         if (kNoise) t[r].g[k] = load_quartet(noise, at + k * step);
       }
+      __builtin_amdgcn_sched_barrier(0);  // (loads end in their order: one that is moved back is waited for with all)
     };
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) load(r, r);
@@ -562,7 +563,7 @@ struct Walker {
         m = top;
       }
     };
-    const int n_b = __builtin_amdgcn_readfirstlane(batches());
+    const int n_b = batches();
     int seg_at = tid, seg_left = seg_batches;  // the segment's place; its batches that are to come
     stream<false, kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
       float z[4 * kUnroll], four[kUnroll], top = -INFINITY;
@@ -1069,12 +1070,15 @@ __global__ __launch_bounds__(kMost) void sample_walk_kernel(SampleArgs a) {
     s.par[c] = a.tree_parent[tr + c];
     s.tok[c] = a.tree_tokens[tr + c];
   }
-  const int lane = tid % SRT_WAVE, wave = __builtin_amdgcn_readfirstlane(tid / SRT_WAVE), e4 = a.V / 4;
-  const int batches = (e4 + kUnroll * threads - 1) / (kUnroll * threads);
-  Walker<kRules> walker = {a, s, skip, apart, apart_z, said_word, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, e4 / (kUnroll * threads),
-                           max(1, (batches + kSegs - 1) / kSegs), 1, 0, 0.f};
+  // (a division's result is the same for all lanes, and said to be: the loops over batches are to be scalar ones)
+  auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int lane = tid % SRT_WAVE, wave = scalar(tid / SRT_WAVE), e4 = a.V / 4;
+  const int full = scalar(e4 / (kUnroll * threads)), batches = scalar((e4 + kUnroll * threads - 1) / (kUnroll * threads));
+  int batch_segs = 1;
   static_assert(kSegs % kUnroll == 0 && kSegs * kMost <= 65536, "a batch's segments are of 8, 4, 2 or 1 quartets");
-  while (walker.batch_segs < kUnroll && 2 * walker.batch_segs * batches <= kSegs) walker.batch_segs *= 2;
+  while (batch_segs < kUnroll && 2 * batch_segs * batches <= kSegs) batch_segs *= 2;
+  Walker<kRules> walker = {a, s, skip, apart, apart_z, said_word, 0, 0, {}, 0, tid, threads, lane, wave, threads / SRT_WAVE, e4, full,
+                           max(1, scalar((batches + kSegs - 1) / kSegs)), scalar(batch_segs), 0, 0.f};
   const float p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
   const double edge = mp > 0.f ? log(static_cast<double>(mp)) : 0.0;
