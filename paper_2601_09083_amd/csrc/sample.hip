@@ -237,11 +237,12 @@ struct Walker {
     };
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) load(r, r);
-    for (int b = 0;;) {
+    bool stop = false;
+    for (int b = 0; b < n_b && !stop; b += kAhead) {
 #pragma unroll
-      for (int r = 0; r < kAhead; ++r, ++b) {
-        if (b >= n_b || f(b, t[r], mine[r])) return;
-        load(b + kAhead, r);
+      for (int r = 0; r < kAhead; ++r) {  // (no way out of the middle, which would be one of another order of loads)
+        if (b + r < n_b && !stop) stop = f(b + r, t[r], mine[r]);
+        load(b + r + kAhead, r);
       }
     }
   }
