@@ -14,10 +14,10 @@
 //
 // GPU design.  One workgroup walks one sequence, and its levels follow one another, so
 // what bounds a batch is one CU's time for a row times the longest walk's levels: of a
-// 152k vocabulary (608 KB) 18 us a row for the arg-max with noise, 15 with min-p, 17 to
-// 18 with a top-k, 22 with a top-p, 26 with a top-k of 200 and a top-p, and under rules 5
-// to 10 more; 256 sequences of up to 13 rows 377 us.  A CU's loads come at 75 to 80 GB/s,
-// with two batches under way as with eight, which is 8 us of a row; the sum for a top-p
+// 152k vocabulary (608 KB) 18 us a row for the arg-max with noise, 14 with min-p, 16 with
+// a top-k, 20 with a top-p or a top-k of 200 and a top-p, and under rules 5 to 15 more; 256
+// sequences of up to 13 rows 309 us.  A CU's loads come at 75 to 80 GB/s, with one batch
+// under way as with seven, which is 8 us of a row; the sum for a top-p
 // is bound by the vector unit (one operation of every entry takes 1 us).  A row is read
 // from HBM once: its maximum, its sum of exp(z - max), and the maximum of every thread's
 // every few entries (a segment) are taken in one pass.  A count and a lower bound of the
@@ -30,7 +30,7 @@
 // without a sort; if it is not, the kept ones lie before it, and the best of those is
 // next.  A list is sorted only where the mass of its first top_k is asked for.  Noise is
 // read at the listed tokens alone, or once a draw.  (Long lists narrowed down by
-// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass, drawn from 140.)
+// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass; 119 now.)
 // Sequences that cut nothing, or without noise, take the plain arg-max in one pass.
 #include "rules.h"
 
@@ -41,14 +41,14 @@ constexpr int kDraws = 12;        // of a long list's choice, before the last ke
 constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kSegsAt = 4;        // of them looked at together
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
-// Batches whose registers are loaded or used, and the same with the noise's (256 walks of
-// 152k entries: 387 us a pass; 2 and 2 393, 4 and 3 395, 6 and 3 438, of which the code
-// has a copy of a batch's work each, and does not stay in the instruction cache).
-constexpr int kAhead = 3;
-constexpr int kAheadNoise = 2;
+// Batches whose registers are loaded or used (256 walks of 152k entries, 64 under rules,
+// 64 of flat rows, 4 of 1024 entries: 309, 377, 119, 33.1 us a pass; 3: 317, 380, 123,
+// 33.3; 4 of them, or 3 where there is noise: 321, 386, 123, 34.5.  The code has a copy of
+// a batch's work for each).
+constexpr int kAhead = 2;
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
 // Batches after which a sum over a row is looked at (64 flat rows of 152k with a top-p of
-// 0.999, 0.9, 0.5: 65, 125, 243 us; at the row's end alone 77, 130, 244).
+// 0.999, 0.9, 0.5: 60, 117, 230 us; at the row's end alone 71, 123, 231).
 constexpr int kStage = 4;
 constexpr int kMost = 512;        // threads
 constexpr int kSegBins = 512;     // of the segments' maxima, 1 / 8 of the score wide
@@ -58,8 +58,8 @@ constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LD
 constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
 constexpr int kApart = kSaid + 512;  // and with them those of the path and of the bias list
 constexpr int kStaged = 512;      // entries of a bias list that are held in LDS
-// Rows up to which 256 threads walk (4 walks of 1024 entries: 36 us a pass, 41 with 512
-// threads; 256 of 152k: 515 us, 377 with 512).
+// Rows up to which 256 threads walk (4 walks of 1024 entries: 33 us a pass, 38 with 512
+// threads; 256 of 152k: 371 us, 309 with 512).
 constexpr int kShortVocab = 4096;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -217,7 +217,7 @@ struct Walker {
   // returns true, the loads of the next kAhead - 1 under way: each in registers of its
   // own, the loop unrolled over them (to move a batch from one to the next would wait for
   // its loads).  Only threads with on() load.  Quartets behind the row's end read as 0.
-  template <bool kNoise, int kAhead, typename On, typename Fn>
+  template <bool kNoise, typename On, typename Fn>
   __device__ __forceinline__ void stream(On on, Fn f) const {
     const int n_b = batches(), bytes = 16 * e4;
     const uint32_t step = 16 * threads;
@@ -302,7 +302,7 @@ struct Walker {
   // Lists the tokens with a count word.  A penalty costs a division, which one such
   // token in a wave's 64 entries makes it take for all, and the words are half as much
   // to read as the logits: with them in the stream 64 walks of a 152k vocabulary, one
-  // token in 50 said, take 695 us, and 412 so.
+  // token in 50 said, take 669 us, and 377 so.
   __device__ __forceinline__ void list_said() {
     if (tid == 0) s.n = 0;
     __syncthreads();
@@ -538,7 +538,7 @@ struct Walker {
   __device__ __forceinline__ u64 plain() {
     Top best;
     u64 key = 0;
-    stream<kNoise, kNoise ? kAheadNoise : kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
+    stream<kNoise>([](int) { return true; }, [&](int b, const Batch& t, bool) {
       float z[4 * kUnroll];
       raw_scores(b, t, z);
 #pragma unroll
@@ -566,7 +566,7 @@ struct Walker {
     };
     const int n_b = batches();
     int seg_at = tid, seg_left = seg_batches;  // the segment's place; its batches that are to come
-    stream<false, kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
+    stream<false>([](int) { return true; }, [&](int b, const Batch& t, bool) {
       float z[4 * kUnroll], four[kUnroll], top = -INFINITY;
       raw_scores(b, t, z);
 #pragma unroll
@@ -849,7 +849,7 @@ struct Walker {
   // that have a score of `least` or more in one of its threads.
   template <bool kNoise, typename Fn>
   __device__ __forceinline__ void batches_from(float least, Fn f) {
-    stream<kNoise, kNoise ? kAheadNoise : kAhead>([&](int b) { return reaches(b, least); }, [&](int b, const Batch& t, bool on) {
+    stream<kNoise>([&](int b) { return reaches(b, least); }, [&](int b, const Batch& t, bool on) {
       if (__ballot(on)) f(b, t, on);
       return false;
     });
@@ -888,7 +888,7 @@ struct Walker {
       if (pack_key(z, j) > place) mass += x;
     });
     bool less = false, decided = false;
-    stream<false, kAhead>([](int) { return true; }, [&](int b, const Batch& t, bool) {
+    stream<false>([](int) { return true; }, [&](int b, const Batch& t, bool) {
       float z[4 * kUnroll], in = 0.f, out = 0.f;
       scores(b, t, z);
       bool equal = false;
