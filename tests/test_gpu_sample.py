@@ -252,6 +252,16 @@ def test_inverse_temperatures_that_turn_or_flatten_the_order(V):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("V", [700, 30000])
+def test_noise_of_tokens_that_are_not_kept(V):
+    """None of these cuts keeps a token of a row's lower half."""
+    c = Case(24, 16, 1, V, 0, a=(0.3, 1.5), cuts=[(20, 1.0, 0.0), (0, 0.5, 0.0), (0, 1.0, 0.9), (V // 3, 0.9, 0.0)])
+    rng = np.random.default_rng(25)
+    low = c.logits < np.median(c.logits, axis=2, keepdims=True)
+    c.gumbel = np.where(low, rng.choice([np.nan, np.inf, -np.inf, 3e38], c.gumbel.shape), c.gumbel).astype(np.float32)
+    c.check(c.run())
+
+
 def test_two_walks_at_once():
     cs = [Case(22, 32, 8, 20483, 4), Case(23, 16, 8, 9000, 4, ruled=True)]
     want = [c.run() for c in cs]
