@@ -261,12 +261,19 @@ class VerifyState:
 
     def use_rope(self, inv_freq, projected, interleaved: bool = False, factor: float = 1.0):
         """The tree's vectors of the steps that follow are ``projected``: queries
-        [B, N, Hq, d], keys and values [B, N, Hkv, d], turned by their positions."""
+        [B, N, Hq, d], keys and values [B, N, Hkv, d], turned by their positions.  Every
+        step reads them as they are then: a step rewrites them in place."""
         self.rope = srt.Rope(inv_freq, interleaved, factor)
         self.projected = tuple(projected)
         if self.kv is not None:
-            self.k_new = torch.zeros_like(self.projected[1], memory_format=torch.contiguous_format)
-            self.v_new = self.projected[2].contiguous()
+            k, v = self.projected[1:]
+            self.v_new, lead = v, srt.row_lead(v)
+            if lead < 0 or lead % 8 or v.data_ptr() % 16:  # (not as the 8-bit cache's calls take rows: write_tree copies them)
+                self.v_new, lead = torch.zeros_like(v, memory_format=torch.contiguous_format), v.shape[2] * v.shape[3]
+            # the turned keys, a row as far from the next as the values', which stay where they are
+            B, N, H, d = k.shape
+            self.k_new = torch.zeros(B * N * lead, dtype=k.dtype, device=k.device).as_strided(
+                k.shape, (N * lead, lead, d, 1))
 
     def make_logits(self, boost: Optional[str] = None, sampled: bool = True, sigma: Optional[float] = None):
         """Per-node logits (boosting each node's first drafted child) and
@@ -290,6 +297,8 @@ class VerifyState:
         q, k, v = self.projected
         n, depth = self.tree["n_nodes"], self.tree["tree_depth"]
         if self.kv is not None:
+            if self.v_new is not v:
+                self.v_new.copy_(v)
             srt.srt_rope_rows(self.rope, q, k, n, self.kv.ctx_len, depth=depth, q_out=self.q, k_out=self.k_new)
         else:
             srt.srt_rope_append(self.rope, q, k, v, n, self.k_cache, self.v_cache, self.block_table, self.attn_len,

@@ -510,6 +510,12 @@ def _lead(s, B, T, H, d):
     return -1 if s[3] != 1 or (H > 1 and s[2] != d) or (B > 1 and s[0] != T * ld) or ld < H * d else ld
 
 
+def row_lead(x) -> int:
+    """Elements from one token to the next of rows [B,T,H,d] as the calls take them (a
+    token's heads side by side, sequences T tokens apart), -1 where they do not lie so."""
+    return _lead(x.stride(), *x.shape)
+
+
 def srt_tree_attn_quant_scratch_bytes(kv: KvQuant, N: int, Hq: int) -> int:
     return int(lib().srt_tree_attn_quant_scratch_bytes(kv._ref, kv.B, N, Hq))
 

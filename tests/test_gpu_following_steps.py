@@ -1,0 +1,121 @@
+"""Steps that follow one another: what changes between them reaches the next one, and
+what does not stays."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_quant as KQ
+from paper_2601_09083_amd import srt
+from paper_2601_09083_amd import workload as W
+from paper_2601_09083_amd.pipeline import VerifyState
+from tests.gpu_util import say, tree_to_np
+from tests.test_gpu_group_step import INV, config
+from tests.test_gpu_quant_step import attention_tolerance, history
+
+pytestmark = pytest.mark.gpu
+
+
+def make_policy(st, step, sampled=True):
+    tree = tree_to_np(st.tree)
+    st.logits = W.make_logits(st.cfg, tree["tree_tokens"], tree["tree_parent"], tree["n_nodes"], device="cuda", boost="top",
+                              seed=300 + step)
+    st.gumbel = W.make_gumbel(st.cfg, st.tokens.batch, device="cuda", seed=400 + step) if sampled else None
+    return tree
+
+
+# --------------------------------------------------------------------------- a projection rewritten in place
+
+class Projection:
+    """Queries, keys and values of a step in buffers that every step rewrites: parts of one
+    projection, packed, or (values only) heads that do not lie side by side."""
+
+    def __init__(self, cfg, B, layout):
+        N, hq, hkv, d = cfg.n_nodes, cfg.hq, cfg.hkv, cfg.head_dim
+        new = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+        if layout == "fused":
+            x = new(B, N, hq + 2 * hkv, d)
+            self.parts = x[:, :, :hq], x[:, :, hq:hq + hkv], x[:, :, hq + hkv:]
+        else:
+            v = new(B, N, hkv, d) if layout == "packed" else new(B, hkv, N, d).transpose(1, 2)
+            self.parts = new(B, N, hq, d), new(B, N, hkv, d), v
+
+    def rewrite(self, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for x in self.parts:
+            x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+
+
+@pytest.mark.parametrize("layout", ["fused", "packed", "scattered"])
+@pytest.mark.parametrize("kv", ["int8", "e4m3"])
+def test_values_of_each_step_over_the_8_bit_cache(kv, layout):
+    """Attention and the committed keys and values of three steps, whose projection is rewritten in between."""
+    cfg = config(3, 2).scaled(hkv=2)
+    plain = VerifyState.build(cfg, kv_headroom=64)
+    hist = [history(plain, b) for b in range(6)]
+    st = VerifyState.build(cfg, kv=kv, kv_headroom=64)
+    proj = Projection(cfg, 6, layout)
+    proj.rewrite(1)
+    st.use_rope(torch.as_tensor(INV, device="cuda"), proj.parts)
+    for step in range(3):
+        say(f"following steps: {kv} {layout} step {step}")
+        proj.rewrite(10 + step)
+        tree = tree_to_np(st.draft())
+        st.write_tree()
+        out, q = (x.double().cpu().numpy() for x in (st.attention(), st.q))
+        make_policy(st, step)
+        new = [x.float().cpu().numpy() for x in (st.k_new, proj.parts[2])]
+        acc = {k: x.cpu().numpy() for k, x in st.accept().items()}
+        st.commit()
+        for b in range(6):
+            n, L = int(tree["n_nodes"][b]), len(hist[b][0])
+            K, V = (np.concatenate([KQ.context(hist[b][i], kv, cfg.page)[0], new[i][b, :n].astype(np.float64)]) for i in range(2))
+            ref, tol = attention_tolerance(q[b], K, V, tree["tree_parent"][b], n, L, st.scale)
+            assert (np.abs(out[b, :n] - ref) <= tol).all(), (step, b)
+            rows = [0] + acc["out_nodes"][b, :int(acc["n_accepted"][b])].tolist()
+            hist[b] = [np.concatenate([hist[b][i], new[i][b, rows]]) for i in range(2)]
+        upto = max(len(x[0]) for x in hist)
+        got = srt.srt_kv_read(st.kv, torch.zeros(6, dtype=torch.int32, device="cuda"), upto)
+        for b in range(6):
+            for i in range(2):
+                want = torch.from_numpy(KQ.context(hist[b][i], kv, cfg.page)[0].astype(np.float32)).to(torch.bfloat16)
+                assert torch.equal(got[i][b, :len(want)].cpu(), want), (step, b, "kv"[i])
+
+
+@pytest.mark.parametrize("layout", ["fused", "scattered"])
+def test_a_replayed_step_reads_the_projection_as_it_is(layout):
+    cfg = config(3, 2).scaled(hkv=2)
+    states, projs = [], []
+    for _ in range(2):
+        st, proj = VerifyState.build(cfg, kv="int8", kv_headroom=64), Projection(cfg, 6, layout)
+        proj.rewrite(1)
+        st.use_rope(torch.as_tensor(INV, device="cuda"), proj.parts)
+        st.draft()
+        make_policy(st, 0)
+        st.accept()  # (allocates its outputs before the capture)
+        st.attn_out.zero_()
+        states.append(st)
+        projs.append(proj)
+
+    def step(st):
+        st.write_tree()
+        st.attention()
+        st.accept()
+        st.commit()
+
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(states[0])
+    a, b = states
+    before = None
+    for i in range(4):
+        for proj in projs:
+            proj.rewrite(20 + i)
+        g.replay()
+        step(b)
+        torch.randn(1 << 18, device="cuda").sum().item()
+        assert torch.equal(b.v_new, projs[1].parts[2]) and (before is None or not torch.equal(b.v_new, before))
+        before = b.v_new.clone()
+        for x, y in ((a.attn_out, b.attn_out), (a.kv.ctx_len, b.kv.ctx_len), (a.kv.k_tail, b.kv.k_tail), (a.kv.v_tail, b.kv.v_tail),
+                     (a.kv.k_pages, b.kv.k_pages), (a.kv.v_pages, b.kv.v_pages), (a.kv.v_scale, b.kv.v_scale)):
+            assert torch.equal(x, y), i
