@@ -116,6 +116,21 @@ def make_kv_quant(B: int, num_pages: int, hkv: int, page: int, d: int, block_tab
     return srt.KvQuant(*pages, *scales, *tails, block_table, torch.zeros(B, dtype=torch.int32, device=device))
 
 
+def share_prefix(block_table, seq_prompt, prefix, ctx_len, page: int) -> np.ndarray:
+    """Gives the sequences of prompt p the pages of their first prefix[p] positions in
+    common, as far as whole pages go in the shortest of their contexts, and returns the
+    positions [n_prompts] that they have in common from then on: contexts grow in pages
+    of their own, so what may be shared never becomes more."""
+    shared = np.zeros(len(prefix), dtype=np.int32)
+    for p in range(len(prefix)):
+        own = np.flatnonzero(seq_prompt == p)
+        whole = min([int(prefix[p]), *(int(ctx_len[b]) for b in own)]) // page
+        for b in own[1:]:
+            block_table[b, :whole] = block_table[own[0], :whole]
+        shared[p] = whole * page
+    return shared
+
+
 def bias_lists(biases: List[Dict[int, float]], device="cuda") -> dict:
     """Per-sequence {token: bias} as the bias arguments of ``srt.Rules``."""
     rows = [sorted(x.items()) for x in biases]
@@ -165,7 +180,8 @@ class VerifyState:
     def build(cls, cfg: W.Config, device="cuda", tokens: Optional[W.TokenWorkload] = None,
               steps_headroom: int = 64, with_seqs: bool = True, kv_headroom: int = 0, kv: str = "bf16", prefix=None):
         """``prefix`` [n_prompts]: the sequences of a prompt have the keys and values of
-        their first prefix[p] positions in the same pages, as far as whole pages go."""
+        their first prefix[p] positions in the same pages, as far as whole pages go
+        in the shortest of their contexts."""
         tw = W.make_tokens(cfg) if tokens is None else tokens
         B = tw.batch
         streams, sp = [], []
@@ -191,11 +207,7 @@ class VerifyState:
             if kv != "bf16":
                 raise ValueError("a shared prefix is of the bf16 cache")
             bt = bt.to(torch.int32)
-            for p in range(cfg.n_prompts):
-                own = np.flatnonzero(tw.seq_prompt == p)
-                whole = min([int(prefix[p]), *(int(tw.ctx_len[b]) for b in own)]) // cfg.page
-                for b in own[1:]:
-                    bt[b, :whole] = bt[own[0], :whole]
+            prefix = share_prefix(bt, tw.seq_prompt, prefix, tw.ctx_len, cfg.page)
         st = cls(cfg=cfg, tokens=tw, caches=caches, seq_stream=seq_stream.astype(np.int32), device=device,
                  prompt_ids=_dev(tw.seq_prompt, device), ctx_tail=_dev(tw.ctx_tail(), device),
                  draft_len=_dev(tw.draft_len(), device), attn_len=_dev(tw.ctx_len, device), q=q, k_cache=k,
@@ -209,7 +221,7 @@ class VerifyState:
             st._quantise(kv)
             need = srt.srt_tree_attn_quant_scratch_bytes(st.kv, cfg.n_nodes, cfg.hq)
         if prefix is not None:
-            st.prefix_len = _dev(np.asarray(prefix), device)
+            st.prefix_len = _dev(prefix, device)
             need = srt.srt_tree_attn_shared_scratch_bytes(B, cfg.n_nodes, cfg.hq, cfg.hkv, cfg.head_dim, cfg.page,
                                                           int(bt.shape[1]), cfg.n_prompts)
         st.scratch = torch.empty(max(need, 1), dtype=torch.uint8, device=device)

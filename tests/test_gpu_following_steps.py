@@ -9,7 +9,7 @@ from paper_2601_09083_amd import srt
 from paper_2601_09083_amd import workload as W
 from paper_2601_09083_amd.pipeline import VerifyState
 from tests.gpu_util import say, tree_to_np
-from tests.test_gpu_group_step import INV, config
+from tests.test_gpu_group_step import INV, config, positions_of
 from tests.test_gpu_quant_step import attention_tolerance, history
 
 pytestmark = pytest.mark.gpu
@@ -119,3 +119,40 @@ def test_a_replayed_step_reads_the_projection_as_it_is(layout):
         for x, y in ((a.attn_out, b.attn_out), (a.kv.ctx_len, b.kv.ctx_len), (a.kv.k_tail, b.kv.k_tail), (a.kv.v_tail, b.kv.v_tail),
                      (a.kv.k_pages, b.kv.k_pages), (a.kv.v_pages, b.kv.v_pages), (a.kv.v_scale, b.kv.v_scale)):
             assert torch.equal(x, y), i
+
+
+# --------------------------------------------------------------------------- contexts that grow past the shared pages
+
+def test_contexts_grow_past_the_pages_that_a_prompt_shares():
+    """Prefixes beyond the shortest contexts share what those have whole pages of, then and later:
+    steps until a group's shortest context has another whole page, then attention of its members."""
+    cfg = config(20, 16)
+    st = VerifyState.build(cfg, kv_headroom=160, prefix=[400] * 20)
+    ids, page = st.tokens.seq_prompt, cfg.page
+    of = lambda p: np.flatnonzero(ids == p)
+    shared = [min(400, int(st.tokens.ctx_len[of(p)].min())) // page for p in range(20)]
+    assert min(shared) < 400 // page
+    for p in range(20):
+        assert (st.block_table[of(p), :shared[p]] == st.block_table[of(p)[0], :shared[p]]).all()
+        assert (st.block_table[of(p)[1:], shared[p]] != st.block_table[of(p)[0], shared[p]]).all()
+    checked = set()
+    for step in range(3 * page):
+        st.draft()
+        now = st.attn_len.cpu().numpy()
+        grown = [p for p in range(20) if min(400, int(now[of(p)].min())) // page > shared[p] and p not in checked]
+        if grown:
+            tree, out, q = tree_to_np(st.tree), st.attention().double().cpu().numpy(), st.q.double().cpu().numpy()
+            p = grown[0]
+            checked.add(p)
+            say(f"following steps: prompt {p} after {step} steps: {shared[p]} pages shared, contexts {now[of(p)].tolist()}")
+            for b in of(p):
+                n, L = int(tree["n_nodes"][b]), int(now[b])
+                ref, tol = attention_tolerance(q[b], *positions_of(st, b, L + n), tree["tree_parent"][b], n, L, st.scale)
+                assert (np.abs(out[b, :n] - ref) <= tol).all(), (step, b)
+        if len(checked) == 2:
+            break
+        make_policy(st, step)
+        st.accept()
+        st.insert()
+        st.commit()
+    assert len(checked) == 2
