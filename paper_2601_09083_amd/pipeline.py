@@ -124,7 +124,7 @@ def share_prefix(block_table, seq_prompt, prefix, ctx_len, page: int) -> np.ndar
     shared = np.zeros(len(prefix), dtype=np.int32)
     for p in range(len(prefix)):
         own = np.flatnonzero(seq_prompt == p)
-        whole = min([int(prefix[p]), *(int(ctx_len[b]) for b in own)]) // page
+        whole = max(0, min([int(prefix[p]), *(int(ctx_len[b]) for b in own)])) // page
         for b in own[1:]:
             block_table[b, :whole] = block_table[own[0], :whole]
         shared[p] = whole * page

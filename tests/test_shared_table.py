@@ -31,3 +31,10 @@ def test_prompts_apart_and_prompts_with_few_sequences():
     assert shared.tolist() == [64, 48, 64, 64]
     assert torch.equal(after[[0, 1, 3]], before[[0, 1, 3]])
     assert torch.equal(after[2, :3], before[0, :3]) and torch.equal(after[2, 3:], before[2, 3:])
+
+
+@pytest.mark.parametrize("prefix", [-1, -5, -16, -300])
+def test_a_negative_prefix_shares_nothing(prefix):
+    """As the attention takes it; no row's pages become another one's."""
+    before, after, shared = tables([0, 0, 0], [prefix], [200, 150, 300])
+    assert torch.equal(after, before) and shared.tolist() == [0]
