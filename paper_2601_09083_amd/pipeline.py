@@ -169,7 +169,7 @@ class VerifyState:
     v_new: Optional[torch.Tensor] = None
     rules: Optional[srt.Rules] = None
     seen: Optional[torch.Tensor] = None    # count rows [B, V] that the penalties read
-    ended: Optional[torch.Tensor] = None   # [B] bool: under rules, sequences whose walk found every token forbidden
+    ended: Optional[torch.Tensor] = None   # [B] bool: under rules or sampling, sequences whose walk found no token
     sampling: Optional[srt.Sampling] = None
     prefix_len: Optional[torch.Tensor] = None  # [n_prompts] positions that the sequences of a prompt share
     rope: Optional[srt.Rope] = None
@@ -265,7 +265,11 @@ class VerifyState:
 
     def use_sampling(self, inv_temperature=None, top_k=None, top_p=None, min_p=None):
         """Sampling parameters (lists or arrays [B], or None) for the steps that
-        follow; the temperatures take the place of the steps' own."""
+        follow; the temperatures take the place of the steps' own.  A sequence whose walk
+        finds nothing to choose (every logit NaN or -inf) ends with that step, as under
+        rules (``ended``)."""
+        if self.ended is None:
+            self.ended = torch.zeros(self.tokens.batch, dtype=torch.bool, device=self.device)
         f = lambda x, d: None if x is None else _dev(np.asarray(x), self.device, d)
         self.sampling = srt.Sampling(f(inv_temperature, torch.float32), f(top_k, torch.int32), f(top_p, torch.float32),
                                      f(min_p, torch.float32))

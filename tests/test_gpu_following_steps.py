@@ -4,7 +4,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import commit as CO
 from oracle import kv_quant as KQ
+from oracle import sampling as SA
 from paper_2601_09083_amd import srt
 from paper_2601_09083_amd import workload as W
 from paper_2601_09083_amd.pipeline import VerifyState
@@ -156,3 +158,56 @@ def test_contexts_grow_past_the_pages_that_a_prompt_shares():
         st.insert()
         st.commit()
     assert len(checked) == 2
+
+
+# --------------------------------------------------------------------------- walks that end without a token
+
+@pytest.mark.parametrize("kv", ["bf16", "int8"])
+def test_sequences_that_end_without_rules_stay_as_they_are(kv):
+    """Sequence 1 finds nothing to choose at its root in step 1 (a constraint that the caller has put
+    into the logits), sequence 2 NaN at its root in step 2; they emit and commit no more, 0 and 3 go on."""
+    cfg = W.CONFIGS["tiny"]
+    st = VerifyState.build(cfg, kv=kv, kv_headroom=128)
+    B, cuts = 4, (np.float32(1.0), 50, np.float32(0.9), np.float32(0.0))
+    st.use_sampling(top_k=[50] * B, top_p=[0.9] * B)
+    tails, t_len, ctx = st.ctx_tail.cpu().numpy(), st.draft_len.tolist(), st.attn_len.tolist()
+    ended = [False] * B
+    for step in range(6):
+        st.draft()
+        st.attention()
+        tree = make_policy(st, step)
+        if step >= 1:
+            st.logits[1, 0] = -float("inf") if step == 1 else 0.5  # (what it would choose afterwards does not matter)
+        if step == 2:
+            st.logits[2, 0] = float("nan")
+        acc = {k: x.cpu().numpy() for k, x in st.accept().items()}
+        st.insert()
+        st.commit()
+        lg, gu = st.logits.cpu().numpy(), st.gumbel.cpu().numpy()
+        for b in range(B):
+            if ended[b]:
+                assert (int(acc["n_accepted"][b]), int(acc["n_emitted"][b])) == (0, 0)
+                assert (acc["out_tokens"][b] == -1).all() and (acc["out_nodes"][b] == -1).all()
+                continue
+            k, toks, nodes, e = SA.walk(lambda u: lg[b, u], lambda s: gu[b, s], *cuts, tree["tree_tokens"][b], tree["tree_parent"][b],
+                                        int(tree["n_nodes"][b]), cfg.max_depth)
+            assert acc["out_tokens"][b, :len(toks)].tolist() == toks and int(acc["n_emitted"][b]) == e
+            tails[b], t_len[b] = CO.commit_tail(tails[b], t_len[b], toks[:e])
+            ctx[b] += k + 1
+            ended[b] = e == k
+        assert st.ended.tolist() == ended
+        assert st.attn_len.tolist() == ctx, step
+        assert np.array_equal(st.ctx_tail.cpu().numpy(), tails) and st.draft_len.tolist() == t_len
+    assert ended == [False, True, True, False]
+
+
+def test_sampling_given_anew_leaves_ended_sequences_ended():
+    st = VerifyState.build(W.CONFIGS["tiny"], kv_headroom=64)
+    st.use_sampling(top_p=[0.9] * 4)
+    st.draft()
+    make_policy(st, 0)
+    st.logits[3] = -float("inf")
+    st.accept()
+    st.commit()
+    st.use_sampling(top_p=[0.5] * 4)
+    assert st.ended.tolist() == [False, False, False, True]
