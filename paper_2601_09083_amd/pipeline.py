@@ -265,7 +265,7 @@ class VerifyState:
 
     def use_sampling(self, inv_temperature=None, top_k=None, top_p=None, min_p=None):
         """Sampling parameters (lists or arrays [B], or None) for the steps that
-        follow; the temperatures take the place of the steps' own.  A sequence whose walk
+        follow; temperatures, if given, take the place of the steps' own.  A sequence whose walk
         finds nothing to choose (every logit NaN or -inf) ends with that step, as under
         rules (``ended``)."""
         if self.ended is None:
@@ -337,9 +337,9 @@ class VerifyState:
             self.accept_scratch = torch.empty(max(srt.srt_accept_scratch_bytes(self.tokens.batch), 1),
                                               dtype=torch.uint8, device=self.device)
         if self.sampling is not None:
-            self.acc = srt.srt_accept_sample(self.logits, self.gumbel, self.sampling, self.tree["tree_tokens"],
-                                             self.tree["tree_parent"], self.tree["n_nodes"], self.cfg.max_depth,
-                                             rules=self.rules, out=self.acc or None)
+            self.acc = srt.srt_accept_sample(self.logits, self.gumbel, self._sampling_at(inv_temperature),
+                                             self.tree["tree_tokens"], self.tree["tree_parent"], self.tree["n_nodes"],
+                                             self.cfg.max_depth, rules=self.rules, out=self.acc or None)
         elif self.rules is not None:
             self.acc = srt.srt_accept_rules(self.logits, self.gumbel, inv_temperature, self.rules,
                                             self.tree["tree_tokens"], self.tree["tree_parent"], self.tree["n_nodes"],
@@ -354,6 +354,16 @@ class VerifyState:
             for k in ("out_tokens", "out_nodes"):
                 self.acc[k].masked_fill_(self.ended[:, None], -1)
         return self.acc
+
+    def _sampling_at(self, inv_temperature: float):
+        """The sampling parameters of a step: its temperature is every sequence's where they have none of their own."""
+        own = self.sampling.tensors
+        if own["inv_temperature"] is not None or inv_temperature == 1.0:
+            return self.sampling
+        if math.isnan(inv_temperature):
+            raise ValueError("inv_temperature must be a number")
+        each = torch.full((self.tokens.batch,), inv_temperature, dtype=torch.float32, device=self.device)
+        return srt.Sampling(**{**own, "inv_temperature": each})
 
     def insert(self):
         srt.srt_trie_insert(self.caches.ws, self.prompt_ids, self.seq_stream_dev, self.acc["out_tokens"],

@@ -211,3 +211,58 @@ def test_sampling_given_anew_leaves_ended_sequences_ended():
     st.commit()
     st.use_sampling(top_p=[0.5] * 4)
     assert st.ended.tolist() == [False, False, False, True]
+
+
+# --------------------------------------------------------------------------- the step's temperature
+
+@pytest.mark.parametrize("ruled", [False, True])
+def test_the_steps_temperature_where_sampling_has_none(ruled):
+    """It is every sequence's; temperatures of the sequences' own take its place."""
+    cfg = W.CONFIGS["tiny"]
+    st = VerifyState.build(cfg, kv_headroom=64)
+    if ruled:
+        st.use_rules([1.2] * 4, [0.3] * 4, [0.1] * 4)
+    st.draft()
+    tree = make_policy(st, 0)
+    lg, gu = st.logits.cpu().numpy(), st.gumbel.cpu().numpy()
+    rest = lambda b: dict(word=st.seen[b].cpu().numpy().view(np.uint16), r=np.float32(1.2), f=np.float32(0.3),
+                          q=np.float32(0.1)) if ruled else {}
+    results = []
+    for own, given in ((None, 1.0), (None, 0.3), (None, 4), ([0.3, 0.5, 4.0, 1.0], 2.0), ([0.3] * 4, 1.0)):
+        st.use_sampling(own, top_k=[200] * 4, min_p=[1e-4] * 4)
+        acc = {k: x.cpu().numpy() for k, x in (st.accept(given) if given != 1.0 else st.accept()).items()}
+        for b in range(4):
+            t = np.float32(given if own is None else own[b])
+            k, toks, nodes, e = SA.walk(lambda u: lg[b, u], lambda s: gu[b, s], t, 200, np.float32(1), np.float32(1e-4),
+                                        tree["tree_tokens"][b], tree["tree_parent"][b], int(tree["n_nodes"][b]), cfg.max_depth, **rest(b))
+            assert acc["out_tokens"][b, :len(toks)].tolist() == toks and int(acc["n_accepted"][b]) == k, (own, given, b)
+        results.append(acc["out_tokens"].copy())
+    assert not np.array_equal(results[0], results[1]) and np.array_equal(results[1], results[4])
+
+
+def test_the_steps_temperature_in_a_graph():
+    """A captured step keeps its temperature, whatever eager steps are given in between."""
+    st = VerifyState.build(W.CONFIGS["tiny"], kv_headroom=64)
+    st.use_sampling(top_k=[500] * 4)
+    st.draft()
+    make_policy(st, 0)
+    want = {t: st.accept(t)["out_tokens"].clone() for t in (1.0, 0.2, 5.0)}
+    assert not torch.equal(want[0.2], want[5.0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        st.accept(0.2)
+    for t in (5.0, 1.0, 5.0):
+        assert torch.equal(st.accept(t)["out_tokens"], want[t])
+        g.replay()
+        torch.randn(1 << 18, device="cuda").sum().item()
+        assert torch.equal(st.acc["out_tokens"], want[0.2])
+
+
+def test_a_temperature_that_is_not_a_number_is_refused():
+    st = VerifyState.build(W.CONFIGS["tiny"])
+    st.use_sampling(top_k=[5] * 4)
+    st.draft()
+    make_policy(st, 0)
+    with pytest.raises(ValueError):
+        st.accept(float("nan"))
