@@ -635,9 +635,10 @@ int srt_tree_attn_shared(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t 
  *   the first one is kept whatever the parameters are (top_k 1 is greedy; so is a
  *   top_p of 0 or less, a min_p above 1, and a NaN in either);
  *   tok = arg-max over the kept ones of fl(z_j + gumbel[b, k, j]), lowest j on ties.
- * Masses are held in 64 bits, the weights they are sums of in 32 or more: the place
- * of the top-p cut is that of exact sums to about 1e-7 of the mass.  The noise of
- * tokens that are not kept does not matter (of kept ones it must be finite).  Where
+ * Masses are held in 64 bits, the weights they are sums of in 32 or more (each a power
+ * whose exponent is rounded to 32 bits): the place of the top-p cut is that of exact
+ * sums to about 1e-6 of the mass.  The noise of tokens that are not kept does not
+ * matter (of kept ones it must be finite).  Where
  * nothing takes part the walk ends without a bonus token, as srt_accept_rules' does.
  * Without noise (gumbel NULL) tok is the arg-max of y and the parameters are not used.
  * Any pointer of the parameters may be NULL: 1, off, off, off.  inv_temperature,
