@@ -902,11 +902,7 @@ struct Walker {
       if (equal)  // ties with the token at the place, itself among them: seldom
 #pragma unroll
         for (int q = 0; q < 4 * kUnroll; ++q)
-          if (z[q] == edge && token(b, q) < last) {
-            const float x = exp_of(z[q] - M);
-            mass += x;
-            read -= x;
-          }
+          if (z[q] == edge && token(b, q) < last) mass += exp_of(z[q] - M);
       mass += in;
       read += static_cast<double>(in) + out;
       if ((b + 1) % kStage != 0 || b + 1 == n_b) return false;
