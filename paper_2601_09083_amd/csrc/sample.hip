@@ -62,6 +62,8 @@ constexpr int kStaged = 512;      // entries of a bias list that are held in LDS
 // threads; 256 of 152k: 371 us, 309 with 512).
 constexpr int kShortVocab = 4096;
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr double kUnit = 1125899906842624.0;  // 2^50 units a weight of 1: a list of 4096 stays below 2^63
+static_assert(kList <= 4096, "sums of units");
 
 struct SampleArgs : RulesArgs {
   const float* inv_temperature;
@@ -302,49 +304,68 @@ struct Walker {
   // Lists the tokens with a count word.  A penalty costs a division, which one such
   // token in a wave's 64 entries makes it take for all, and the words are half as much
   // to read as the logits: with them in the stream 64 walks of a 152k vocabulary, one
-  // token in 50 said, take 669 us, and 377 so.
+  // token in 50 said, take 669 us, and 377 so.  A thread's place in the list decides
+  // with which others its tokens' weights are added, so the places follow from the words
+  // alone: each wave counts its batches, and lists them behind all that come before.
   __device__ __forceinline__ void list_said() {
-    if (tid == 0) s.n = 0;
-    __syncthreads();
     const u16x4* s4 = reinterpret_cast<const u16x4*>(w.seen);
     constexpr int kWords = 8;  // quartets of a thread in a batch
+    constexpr int kMostBatches = kMaxRuled / 4 / (kWords * kMost);
+    static_assert(kMostBatches * kMost * sizeof(uint32_t) <= sizeof(s.list) && kShortVocab <= 4 * kWords * 256,
+                  "a bit of every entry, in the place of the candidates");
+    static_assert(kMostBatches * (kMost / SRT_WAVE) <= 2 * SRT_WAVE && 2 * SRT_WAVE * sizeof(int32_t) <= sizeof(s.segbin),
+                  "two counts a lane");
+    uint32_t* said_bits = reinterpret_cast<uint32_t*>(s.list);
+    int32_t* counts = reinterpret_cast<int32_t*>(s.segbin);
+    const int step = kWords * threads, n_b = (e4 + step - 1) / step;
     auto load = [&](int i0, u16x4 (&c)[kWords]) {
       if (i0 >= e4) return;
 #pragma unroll
       for (int k = 0; k < kWords; ++k) c[k] = s4[min(i0 + tid + k * threads, e4 - 1)];
     };
-    auto list = [&](int i0, const u16x4 (&c)[kWords]) {
+    auto count = [&](int b, const u16x4 (&c)[kWords]) {
       uint32_t said = 0;  // bit 4 k + e: the batch's entry has a word
 #pragma unroll
       for (int k = 0; k < kWords; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) said |= (i0 + tid + k * threads < e4 && c[k][e] ? 1u : 0u) << (4 * k + e);
-      const int m = __popc(said), upto = static_cast<int>(wave_scan(static_cast<u64>(m)));
-      int at = 0;
-      if (lane == SRT_WAVE - 1) at = atomicAdd(&s.n, upto);
-      at = __builtin_amdgcn_readlane(at, SRT_WAVE - 1) + upto - m;
-      for (; said; said &= said - 1, ++at) {
-        const int q = __ffs(said) - 1;
-        if (at < kSaid) apart[at] = 4 * (i0 + tid + q / 4 * threads) + q % 4;
-      }
+        for (int e = 0; e < 4; ++e) said |= (b * step + tid + k * threads < e4 && c[k][e] ? 1u : 0u) << (4 * k + e);
+      said_bits[b * threads + tid] = said;
+      const int m = static_cast<int>(wave_scan(static_cast<u64>(__popc(said))));
+      if (lane == SRT_WAVE - 1) counts[b * waves + wave] = m;
     };
-    const int step = kWords * threads;
     u16x4 c0[kWords], c1[kWords];
     load(0, c0);
-    for (int i0 = 0; i0 < e4; i0 += 2 * step) {  // (each in registers of its own)
-      load(i0 + step, c1);
-      list(i0, c0);
-      if (i0 + step >= e4) break;
-      load(i0 + 2 * step, c0);
-      list(i0 + step, c1);
-    }
-    const int j = 4 * e4 + tid;
-    if (j < a.V && w.seen[j]) {
-      const int at = atomicAdd(&s.n, 1);
-      if (at < kSaid) apart[at] = j;
+    for (int b = 0; b < n_b; b += 2) {  // (each in registers of its own)
+      load((b + 1) * step, c1);
+      count(b, c0);
+      if (b + 1 >= n_b) break;
+      load((b + 2) * step, c0);
+      count(b + 1, c1);
     }
     __syncthreads();
-    n_said = s.n <= kSaid ? s.n : -1;
+    const int parts = n_b * waves;
+    const int x0 = 2 * lane < parts ? counts[2 * lane] : 0, x1 = 2 * lane + 1 < parts ? counts[2 * lane + 1] : 0;
+    const int upto = static_cast<int>(wave_scan(static_cast<u64>(x0 + x1)));
+    const int in_quartets = __builtin_amdgcn_readlane(upto, SRT_WAVE - 1);
+    const int j = 4 * e4 + lane;  // (the row's last one to three, which every wave counts)
+    const u64 rest = __ballot(j < a.V && w.seen[min(j, a.V - 1)]);
+    n_said = in_quartets + __popcll(rest);
+    if (n_said > kSaid) n_said = -1;
+    if (n_said > 0) {
+      for (int b = 0; b < n_b; ++b) {
+        const int part = b * waves + wave;
+        uint32_t said = said_bits[b * threads + tid];
+        const int m = __popc(said);
+        const int first = __builtin_amdgcn_readlane(part & 1 ? upto - x1 : upto - x1 - x0, part / 2);
+        int at = first + static_cast<int>(wave_scan(static_cast<u64>(m))) - m;
+        for (; said; said &= said - 1, ++at) {
+          const int q = __ffs(said) - 1;
+          apart[at] = 4 * (b * step + tid + q / 4 * threads) + q % 4;
+        }
+      }
+      if (wave == 0 && ((rest >> lane) & 1)) apart[in_quartets + __popcll(rest & ((1ull << lane) - 1))] = j;
+    }
+    __syncthreads();
     for (int i = tid; i < n_said; i += threads) said_word[i] = w.seen[apart[i]];
   }
 
@@ -518,7 +539,15 @@ struct Walker {
     parity ^= 1;
     return key;
   }
-  // The workgroup's sum; the terms are added in the same order always.
+  // The workgroup's sum, of whole units, and of terms that are added in the same order always.
+  __device__ __forceinline__ u64 all_units(u64 x) {
+    x = last_lane(wave_scan(x));
+    if (lane == 0) s.red[parity][wave] = x;
+    __syncthreads();
+    x = lane < waves ? s.red[parity][lane] : 0ull;
+    parity ^= 1;
+    return last_lane(wave_scan(x));
+  }
   __device__ __forceinline__ double all_sum(double x) {
     x = last_lane(wave_scan(x));
     if (lane == 0) s.redd[parity][wave] = x;
@@ -698,6 +727,9 @@ struct Walker {
   }
 
   __device__ __forceinline__ double weight(float z) const { return exp(static_cast<double>(z) - static_cast<double>(M)); }
+  // The same in whole units, whose sums are the same in any order: a list's places are
+  // as its waves came.
+  __device__ __forceinline__ u64 units(float z) const { return static_cast<u64>(weight(z) * kUnit); }
 
   // The choice from a list of up to 64 R tokens, by wave 0 in registers: R a lane,
   // place 64 r + lane, drawn from as a long list is (weighs_less) until a draw is kept.
@@ -722,15 +754,15 @@ struct Walker {
           if (x[r] < kth) x[r] = 0;
       }
       u64 key[R], place = 0;
-      double wt[R], all = 0.0;
+      u64 wt[R], all = 0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         key[r] = 0;
         if (x[r] && score_of(x[r]) >= least) take(key[r], score_of(x[r]), key_token(x[r]));
-        wt[r] = p < 1.0 && x[r] ? weight(score_of(x[r])) : 0.0;
+        wt[r] = p < 1.0 && x[r] ? units(score_of(x[r])) : 0ull;
         all += wt[r];
       }
-      const double target = p < 1.0 ? p * (k < a.V ? last_lane(wave_scan(all)) : row_mass) : INFINITY;
+      const double target = p < 1.0 ? p * (k < a.V ? static_cast<double>(last_lane(wave_scan(all))) : row_mass * kUnit) : INFINITY;
       for (;;) {  // (each draw's place lies before the last one's)
         u64 mine = 0, at = 0;
 #pragma unroll
@@ -745,14 +777,14 @@ struct Walker {
         place = static_cast<u64>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at >> 32), owner))) << 32 |
                 static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(at), owner));
         int before = 0;
-        double mass = 0.0;
+        u64 mass = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const bool in = x[r] > place;
           before += __popcll(__ballot(in));
-          mass += in ? wt[r] : 0.0;
+          mass += in ? wt[r] : 0ull;
         }
-        if (before == 0 || (before < k && (p >= 1.0 || last_lane(wave_scan(mass)) < target))) break;
+        if (before == 0 || (before < k && (p >= 1.0 || static_cast<double>(last_lane(wave_scan(mass))) < target))) break;
       }
       if (lane == 0) s.found = best;
     }
@@ -817,11 +849,10 @@ struct Walker {
       if (best == all) s.found = at;
       __syncthreads();
       place = s.found;
-      double mass = 0.0;
+      u64 mass = 0;
       for (int i = tid; i < count; i += threads)
-        if (s.list[i] > place) mass += weight(score_of(s.list[i]));
-      mass = all_sum(mass);
-      if (mass < target) return all;  // (nothing lies before the first)
+        if (s.list[i] > place) mass += units(score_of(s.list[i]));
+      if (static_cast<double>(all_units(mass)) < target * kUnit) return all;  // (nothing lies before the first)
     }
     sort(count);
     u64 best = 0;
