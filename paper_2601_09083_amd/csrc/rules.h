@@ -120,11 +120,10 @@ __device__ inline void mark(const RulesArgs& a, const Row& w, Path& path, int n,
   mark_special(a, w, path, n, lo, hi, skip, threads, at, bias);
 }
 
-// The logit of one marked token under the rules: its path count and, where `from`
-// >= 0, the run of its biases that starts at that entry of the list.
+// The logit l of one marked token under the rules, its count word given: its path count
+// and, where `from` >= 0, the run of its biases that starts at that entry of the list.
 __device__ inline float special_logit(const RulesArgs& a, const Row& w, const Path& path, int n, int t, int from,
-                                      float l) {
-  const int word = w.seen ? w.seen[t] : 0;
+                                      float l, int word) {
   int count = word & kCount;
   for (int i = 0; i < n; ++i) count += path.tok[i] == t;
   float y = penalised(w, l, word & kPrompt, count);

@@ -25,14 +25,15 @@ namespace {
 constexpr int kMaxChunk = 65536;                      // entries of a chunk, at most
 constexpr int64_t kMaxVocab = int64_t(kMaxChunk) * kMaxChunks;
 
-// Score of one marked token that is allowed.
+// Score of one marked token that is allowed.  (What it reads is loaded at once.)
 template <bool kNoise>
 __device__ inline void special(const RulesArgs& a, const Row& w, const Path& path, int n, int t, int from,
                                unsigned long long& key) {
-  const bool allowed = allowed_token(w, t);
+  const uint32_t allowed = w.mask ? w.mask[t >> 5] >> (t & 31) : 1u;
+  const int word = w.seen ? w.seen[t] : 0;
   const float l = w.logits[t], g = kNoise ? w.noise[t] : 0.f;
-  const float x = noisy<kNoise>(w, special_logit(a, w, path, n, t, from, l), g);
-  if (allowed && x > -INFINITY) key = max(key, pack_key(x, t));
+  const float x = noisy<kNoise>(w, special_logit(a, w, path, n, t, from, l, word), g);
+  if ((allowed & 1u) && x > -INFINITY) key = max(key, pack_key(x, t));
 }
 
 // This thread's best entry of [lo, hi) of one row, packed (0: none).  kUnroll

@@ -298,7 +298,8 @@ struct Walker {
   }
   __device__ __forceinline__ float special_score(int t, int from) const {
     if (!allowed_token(w, t)) return -INFINITY;
-    return __builtin_fmaxf(mul_rounded(special_logit(a, w, s.path, n, t, from, w.logits[t]), w.invT), -INFINITY);
+    const int word = w.seen ? w.seen[t] : 0;
+    return __builtin_fmaxf(mul_rounded(special_logit(a, w, s.path, n, t, from, w.logits[t], word), w.invT), -INFINITY);
   }
 
   // Lists the tokens with a count word.  A penalty costs a division, which one such
