@@ -9,7 +9,7 @@
 //
 // GPU design: one read and one write of every vector, bound by HBM (16 prompts of up to
 // 4096 tokens, 32 + 8 heads: 206 us a pass, 1.04 GB at 5.1 TB/s, the rate of a copy;
-// 256 trees of up to 64 nodes, 28 + 4 heads: 38.6 us, 132 MB at 3.4 TB/s).  A wave
+// 256 trees of up to 64 nodes, 28 + 4 heads: 37.2 us, 132 MB at 3.5 TB/s).  A wave
 // takes a token.  Its lanes work out an angle each while the first heads' loads are
 // under way, and hand them round through LDS: a lane keeps one 16-byte piece of the
 // pairs for all heads that it visits, and the 8 (halves) or 4 (neighbouring dims)

@@ -16,7 +16,7 @@
 // what bounds a batch is one CU's time for a row times the longest walk's levels: of a
 // 152k vocabulary (608 KB) 18 us a row for the arg-max with noise, 14 with min-p, 16 with
 // a top-k, 20 with a top-p or a top-k of 200 and a top-p, and under rules 5 to 15 more; 256
-// sequences of up to 13 rows 309 us.  A CU's loads come at 75 to 80 GB/s, with one batch
+// sequences of up to 13 rows 310 to 370 us, which goes by the inputs.  A CU's loads come at 75 to 80 GB/s, with one batch
 // under way as with seven, which is 8 us of a row; the sum for a top-p
 // is bound by the vector unit (one operation of every entry takes 1 us).  A row is read
 // from HBM once: its maximum, its sum of exp(z - max), and the maximum of every thread's
@@ -30,7 +30,7 @@
 // without a sort; if it is not, the kept ones lie before it, and the best of those is
 // next.  A list is sorted only where it is long and the mass of its first top_k is asked
 // for.  Noise is read at the listed tokens alone, or once a draw.  (Long lists narrowed down by
-// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass; 119 now.)
+// histograms of LDS atomics: flat rows of 64 sequences 226 us a pass; 111 to 128 now.)
 // Sequences that cut nothing, or without noise, take the plain arg-max in one pass.
 #include "rules.h"
 
@@ -42,7 +42,7 @@ constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kSegsAt = 4;        // of them looked at together
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
 // Batches whose registers are loaded or used (256 walks of 152k entries, 64 under rules,
-// 64 of flat rows, 4 of 1024 entries: 309, 377, 119, 33.1 us a pass; 3: 317, 380, 123,
+// 64 of flat rows, 4 of 1024 entries, the same inputs: 309, 377, 119, 33.1 us a pass; 3: 317, 380, 123,
 // 33.3; 4 of them, or 3 where there is noise: 321, 386, 123, 34.5.  The code has a copy of
 // a batch's work for each).
 constexpr int kAhead = 2;
@@ -58,8 +58,8 @@ constexpr int64_t kMaxRuled = int64_t(1) << 18;  // a row's marks are held in LD
 constexpr int kSaid = 4096;       // tokens with a count word that are scored apart from the stream
 constexpr int kApart = kSaid + 512;  // and with them those of the path and of the bias list
 constexpr int kStaged = 512;      // entries of a bias list that are held in LDS
-// Rows up to which 256 threads walk (4 walks of 1024 entries: 33 us a pass, 38 with 512
-// threads; 256 of 152k: 371 us, 309 with 512).
+// Rows up to which 256 threads walk (the same inputs: 4 walks of 1024 entries 33 us a pass,
+// 38 with 512 threads; 256 of 152k 371, 309 with 512).
 constexpr int kShortVocab = 4096;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr double kUnit = 1125899906842624.0;  // 2^50 units a weight of 1: a list of 4096 stays below 2^63
@@ -77,6 +77,10 @@ typedef unsigned long long u64;
 // The larger of two that are no NaN (fmaxf would quiet each operand first).
 __device__ __forceinline__ float larger_of(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
+// The weight of a score at distance x from the largest.  In 32 bits: the product is off by
+// half a unit in its last place, the weight by up to 1e-6 of itself (from a distance of 11 on;
+// nearer by less); a power in 64 bits is many operations, of which one for every entry of a
+// 152k row takes 1 us.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // Reductions and prefix sums over the wave by DPP moves, as wave_sum of common.h (a

@@ -14,9 +14,9 @@
 // left to read: 32 prompts of 2k to 8k, eight answers each, 28 + 4 heads of 128 take
 // 177 us a pass, 822 MB at 4.6 TB/s (5.0 in the tile kernel's 163 us), where
 // srt_tree_attn reads every prefix eight times and takes 314.  Trees are bound by the
-// tile kernel's rate: 64 trees of 8 nodes over one prompt of 32k 158 us, 126 GFLOP at
+// tile kernel's rate: 64 trees of 8 nodes over one prompt of 32k 158 to 160 us, 126 GFLOP at
 // 0.8 PFLOP/s (srt_tree_attn, whose 256-row tiles are a quarter full, 608); 128 of 1 to
-// 64 nodes, 12 + 2 heads, 129 us (153), 28 of them the plan and the parts' join.
+// 64 nodes, 12 + 2 heads, 129 to 132 us (153), 28 of them the plan and the parts' join.
 // A plan kernel (one workgroup) finds the groups' members, the keys that they can
 // share -- whole pages, no further than the shortest member's context -- and the
 // items, longest first; the combine kernel of attn.h joins the parts.
@@ -288,7 +288,9 @@ __global__ __launch_bounds__(kThreads, 1) void shared_attn_kernel(SharedArgs a) 
       }
     }
     // Probabilities exp2(score - mref0 - dm), rounded to bf16 for the second
-    // product (sacc holds score - mref0); returns this lane's sum of them
+    // product, as srt_tree_attn's (an fp32 product has a sixteenth of the matrix rate; the
+    // sum l takes the rounded ones, so that they still add up to 1, and an output moves by
+    // at most 2^-8 of itself and as much of the mean of |v|); sacc holds score - mref0.  Returns this lane's sum of them
     // (its 32 keys of the row, two bf16 pairs per dot2, two accumulators).
     // Contraction index 8 h + e of k-step ks <-> key 16 ks + 8 (e/4) + 4 h + e%4.
     auto probs = [&](auto dm_c, float dm) {
@@ -554,7 +556,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a,
     keys[g] = lead[g] = 0x7fffffff;
   }
   if (tid == 0) ncomb = widest = most = 0;
-  SeqInfo si = {0, 0, 0};  // of this thread's sequence of the current 1024, and its group
+  SeqInfo si = {0, 0, 0};  // of this thread's sequence of the current kPlanThreads, and its group
   int mine = -1;
   auto take = [&](int b) {
     si = seq_info(a, b);
