@@ -15,21 +15,22 @@
 // GPU design.  One workgroup walks one sequence, and its levels follow one another, so
 // what bounds a batch is one CU's time for a row times the longest walk's levels: of a
 // 152k vocabulary (608 KB) 18 us a row for the arg-max with noise, 14 with min-p, 16 with
-// a top-k, 20 with a top-p or a top-k of 200 and a top-p, and under rules 5 to 15 more; 256
-// sequences of up to 13 rows 310 to 370 us, which goes by the inputs.  A CU's loads come at 75 to 80 GB/s, with one batch
-// under way as with seven, which is 8 us of a row; the sum for a top-p
-// is bound by the vector unit (one operation of every entry takes 1 us).  A row is read
-// from HBM once: its maximum, its sum of exp(z - max), and the maximum of every thread's
-// every few entries (a segment) are taken in one pass.  A count and a lower bound of the
-// mass over the segments' maxima give a score below which nothing can be kept; segments
-// that reach it are read again, which a row that is sure of its tokens has few of, and
-// their entries from that score up are listed in LDS, most often a hundred.
+// a top-k, 20 with a top-p or a top-k of 200 and a top-p, and under rules 5 to 15 more;
+// 256 sequences of up to 13 rows 310 to 370 us, which goes by the inputs.  A CU's loads
+// come at 75 to 80 GB/s, with one batch under way as with seven, which is 8 us of a row;
+// the sum for a top-p is bound by the vector unit (one operation of every entry takes 1
+// us).  A row is read from HBM once: its maximum, its sum of exp(z - max), and the
+// maximum of every thread's every few entries (a segment) are taken in one pass.  A count
+// and a lower bound of the mass over the segments' maxima give a score below which
+// nothing can be kept; segments that reach it are read again, which a row that is sure of
+// its tokens has few of, and their entries from that score up are listed in LDS, most
+// often a hundred.
 //
-// The choice from a list or from the row is drawn: the best of all of them is the
-// choice if it is kept itself, which takes the mass before it in the order, a sum
-// without a sort; if it is not, the kept ones lie before it, and the best of those is
-// next.  A list is sorted only where it is long and the mass of its first top_k is asked
-// for.  Noise is read at the listed tokens alone, or once a draw.  (Long lists narrowed down by
+// The choice from a list or from the row is drawn: the best of all of them is the choice
+// if it is kept itself, which takes the mass before it in the order, a sum without a
+// sort; if it is not, the kept ones lie before it, and the best of those is next.  A list
+// is sorted only where it is long and the mass of its first top_k is asked for.  Noise is
+// read at the listed tokens alone, or once a draw.  (Long lists narrowed down by
 // histograms of LDS atomics: flat rows of 64 sequences 226 us a pass; 111 to 128 now.)
 // Sequences that cut nothing, or without noise, take the plain arg-max in one pass.
 #include "rules.h"
@@ -42,9 +43,9 @@ constexpr int kSegs = 16;         // segments of a thread, at most
 constexpr int kSegsAt = 4;        // of them looked at together
 constexpr int kUnroll = 4;        // quartets of a thread in a batch
 // Batches whose registers are loaded or used (256 walks of 152k entries, 64 under rules,
-// 64 of flat rows, 4 of 1024 entries, the same inputs: 309, 377, 119, 33.1 us a pass; 3: 317, 380, 123,
-// 33.3; 4 of them, or 3 where there is noise: 321, 386, 123, 34.5.  The code has a copy of
-// a batch's work for each).
+// 64 of flat rows, 4 of 1024 entries, the same inputs: 309, 377, 119, 33.1 us a pass; 3:
+// 317, 380, 123, 33.3; 4 of them, or 3 where there is noise: 321, 386, 123, 34.5.  The code
+// has a copy of a batch's work for each).
 constexpr int kAhead = 2;
 constexpr int kAgain = 4;         // quartets of a thread that are read again together
 // Batches after which a sum over a row is looked at (64 flat rows of 152k with a top-p of
